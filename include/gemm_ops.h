@@ -1,0 +1,159 @@
+/*
+ * gemm_ops.h -- C ABI of the operators around the products of a transformer
+ * layer (MI355X, gfx950), in the same library as gemm_f16.h: RMS norm with the
+ * residual's addition, quantisation to 8 bits, products of 8-bit matrices with
+ * block scales, and products grouped by expert.
+ *
+ * Conventions are those of gemm_f16.h: row-major matrices in device memory of
+ * the current HIP device, pitches in ELEMENTS, sizes from 0 to 2^31-1, work
+ * only enqueued on `stream` (a hipStream_t as void*), arguments checked on the
+ * host before anything is launched, the GEMM_F16_* return codes, nothing
+ * allocated, nothing thrown, no state kept.  An output must not overlap an
+ * input unless said otherwise.  No call writes between a row's end and the
+ * pitch; an aligned 16-byte fetch may read there.  All entry points may be
+ * captured into a HIP graph.
+ *
+ * Element types: GEMM_TYPE_F16 / _BF16 (16 bits), _F32 (results only).  "e4m3" is
+ * the 8-bit format with 4 exponent and 3 mantissa bits, no infinities, largest
+ * value 448 (OCP 8-bit floating point, torch.float8_e4m3fn).
+ *
+ * Quantised matrices: a value is (e4m3 element) * (f32 scale of its block).
+ *   rows form    X (M x K): one scale for 128 consecutive elements of a row,
+ *                that of (i, 128 b ..) at scale[b * ld_scale + i]; ceil(K/128)
+ *                rows of M scales, ld_scale >= M -- the scales of one block column
+ *                are contiguous, as the products read them.
+ *   blocks form  W (N x K): one scale for 128 x 128 elements, that of block
+ *                (a, b) at scale[a * ld_scale + b], ld_scale >= ceil(K/128).
+ * The last block of a row or column may be short.
+ */
+#ifndef GEMM_OPS_H
+#define GEMM_OPS_H
+
+#include <stdint.h>
+#include "gemm_f16.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { GEMM_TYPE_F16 = 0, GEMM_TYPE_BF16 = 1, GEMM_TYPE_F32 = 2 };
+enum { GEMM_OPS_ACT_NONE = 0, GEMM_OPS_ACT_RELU = 1, GEMM_OPS_ACT_SWIGLU = 2 };
+
+/*
+ * Quantise to e4m3.  For each block: scale = max(largest |x|, 2^-96) / 448 in
+ * f32, element = x * (448 / largest) rounded to nearest even.  A block that holds a NaN
+ * or an infinity gets the scale NaN and elements NaN, so that it shows in any
+ * product; nothing else is touched by it.  A block of zeros is zeros with the scale 2^-96 / 448.
+ *
+ * rows: X (M x N of `type`; M x 2N for SWIGLU) -> Q (M x N e4m3) and scales in
+ * the rows form.  act is applied first, in f32: NONE, RELU (x < 0 ? 0 : x), or
+ * SWIGLU: the first N columns are the gate g, the last N the values u, x =
+ * g / (1 + exp(-g)) * u.
+ * blocks: X (M x N) -> Q and scales in the blocks form.
+ * Pointers of X: 2-byte aligned; pitches of any size >= the row (any alignment
+ * runs, 16-byte aligned rows run fastest).
+ */
+int quantize_e4m3_rows(int64_t M, int64_t N, int64_t type, int64_t act,
+                       const void* X, int64_t ldx,
+                       void* Q, int64_t ldq, float* scale, int64_t ld_scale,
+                       void* stream);
+int quantize_e4m3_blocks(int64_t M, int64_t N, int64_t type,
+                         const void* X, int64_t ldx,
+                         void* Q, int64_t ldq, float* scale, int64_t ld_scale,
+                         void* stream);
+
+/*
+ * RMS norm of M rows of N elements with the residual's addition:
+ *     h = x + r                    rounded to `type`; r NULL: h = x
+ *     rstd = 1 / sqrt(mean(h^2) + eps)      of the rounded h, in f32
+ *     y = h * rstd * gamma
+ * Outputs, each of which may be NULL: H (h), Y (y in `type`), Q with scale (y in
+ * e4m3 with scales in the rows form, quantised from the f32 value), rstd (M
+ * f32, as rms_norm_grad takes it).  H may be X or R themselves.  gamma: N
+ * elements of `type`.  Q without scale or scale without Q is GEMM_F16_ERR_NULL;
+ * eps that is negative or no number is GEMM_F16_ERR_CONFIG.  N = 0 writes nothing.
+ */
+int rms_norm(int64_t M, int64_t N, int64_t type,
+             const void* X, int64_t ldx, const void* R, int64_t ldr,
+             const void* gamma, double eps,
+             void* H, int64_t ldh, void* Y, int64_t ldy,
+             void* Q, int64_t ldq, float* scale, int64_t ld_scale,
+             float* rstd, void* stream);
+
+/*
+ * Gradients of rms_norm's Y.  From dY, the stored H, gamma and rstd:
+ *     xhat = h * rstd,  g = dy * gamma
+ *     dX = rstd * (g - xhat * mean(g * xhat)) + dH        (of x and of r alike)
+ *     dgamma[j] = sum_i dy[i][j] * xhat[i][j]             (N f32)
+ * dH: the gradient that reaches h by the residual's own way, or NULL.  dX may be
+ * dY or dH themselves.  dgamma NULL: not formed, and no workspace needed; M = 0 gives zeros.  The
+ * rows are summed in a fixed order (two runs give the same bits) with the help of a
+ * workspace of rms_norm_grad_workspace_bytes(M, N) bytes (at most 256 rows of N
+ * floats), 16-byte aligned; smaller: GEMM_F16_ERR_WORKSPACE.
+ */
+int64_t rms_norm_grad_workspace_bytes(int64_t M, int64_t N);
+int rms_norm_grad(int64_t M, int64_t N, int64_t type,
+                  const void* dY, int64_t lddy, const void* H, int64_t ldh,
+                  const void* gamma, const float* rstd,
+                  const void* dH, int64_t lddh,
+                  void* dX, int64_t lddx, float* dgamma,
+                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Product of quantised matrices: C (M x N of c_type) = A * B^T, overwritten, with A
+ * (M x K e4m3, scales in the rows form) and B (N x K e4m3: a row for each output, as
+ * weights are stored; scales in the blocks form):
+ *     C[i][j] = sum_b a_scale[b][i] * b_scale[j/128][b] * sum_{k in block b} A[i][k] B[j][k]
+ * Sums of products, scaled sums and C before its one rounding are f32.  A
+ * NaN in a row of A or B reaches that row or column of C only.  K = 0 gives
+ * zeros.  Pointers of any alignment are accepted; A and B 16-byte aligned with pitches
+ * that are multiples of 16 run the fast kernels (K and N of any size).  The product
+ * dC * B for the gradient of A is this same operator on dC quantised in rows
+ * and B transposed, whose blocks' scales transpose with it.
+ */
+int gemm_e4m3_block(int64_t M, int64_t N, int64_t K,
+                    const void* A, int64_t lda, const float* a_scale, int64_t ld_as,
+                    const void* B, int64_t ldb, const float* b_scale, int64_t ld_bs,
+                    void* C, int64_t ldc, int64_t c_type, void* stream);
+
+/*
+ * Products grouped by expert.  Rows offsets[e] .. offsets[e+1]-1 of A (T rows)
+ * belong to expert e.  offsets: E + 1 int32 in device memory, not
+ * decreasing, from 0 to T -- read on the device, so that the router's result
+ * needs no copy to the host.  Rows in no group are left alone in C (dA), experts
+ * without rows cost nothing (their dB is zeros).  Offsets outside 0 .. T are
+ * taken as 0 or T, decreasing ones as empty groups: no access leaves the
+ * matrices.  What is then computed for groups that overlap is not specified.  E <= 65535.
+ *
+ * Matrices of expert e begin b_stride * e elements behind B (db_stride, and
+ * bs_stride for scales, alike).  db_stride is at least the matrix; what is only
+ * read may have any stride from 0 (one matrix for all experts) on.
+ *
+ * gemm_e4m3_block_grouped: as gemm_e4m3_block, with B[e] (N x K).
+ * gemm_grouped:        C (T x N) = A (T x K) * B[e] (K x N)
+ * gemm_grouped_grad_a: dA (T x K) = dC (T x N) * B[e]^T
+ * gemm_grouped_grad_b: dB[e] (K x N) = A_e^T * dC_e, a sum over the expert's rows
+ * The last three take A, B, dC of `type` (f16 or bf16), sum in f32 and round once
+ * to c_type (a_type, b_type): `type` itself or f32 (else GEMM_F16_ERR_CONFIG).
+ * Any 2-byte alignment is accepted; 16-byte aligned matrices with pitches
+ * and strides that are multiples of 8 run the fast kernels.
+ */
+int gemm_e4m3_block_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
+                            const void* A, int64_t lda, const float* a_scale, int64_t ld_as,
+                            const void* B, int64_t ldb, int64_t b_stride,
+                            const float* b_scale, int64_t ld_bs, int64_t bs_stride,
+                            void* C, int64_t ldc, int64_t c_type, void* stream);
+int gemm_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type,
+                 const void* A, int64_t lda, const void* B, int64_t ldb, int64_t b_stride,
+                 void* C, int64_t ldc, int64_t c_type, void* stream);
+int gemm_grouped_grad_a(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type,
+                        const void* dC, int64_t lddc, const void* B, int64_t ldb, int64_t b_stride,
+                        void* dA, int64_t ldda, int64_t a_type, void* stream);
+int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type,
+                        const void* A, int64_t lda, const void* dC, int64_t lddc,
+                        void* dB, int64_t lddb, int64_t db_stride, int64_t b_type, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* GEMM_OPS_H */

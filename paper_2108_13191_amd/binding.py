@@ -1,4 +1,4 @@
-"""Thin binding of the C ABI in include/gemm_f16.h: ctypes, and for the GEMM entry points themselves a small extension
+"""Thin binding of the C ABIs in include/gemm_f16.h and include/gemm_ops.h: ctypes, and for the GEMM entry points themselves a small extension
 (csrc/fastcall.c) in front of it that marshals the usual arguments in native code.
 
 Argument marshalling only: every step of the GEMM runs in the HIP kernels of
@@ -61,6 +61,20 @@ class GemmError(RuntimeError):
         super().__init__(f"gemm_f16 error {code}: {strerror(code)}")
 
 
+# The entry points of gemm_ops.h and the kinds of their arguments: "i" an int64_t, "p" a pointer, "d" a double.
+_OPS = {
+    "quantize_e4m3_rows": "iiiipipipip",
+    "quantize_e4m3_blocks": "iiipipipip",
+    "rms_norm": "iiipipipdpipipipipp",
+    "rms_norm_grad": "iiipipipppipippip",
+    "gemm_e4m3_block": "iiipipipipipiip",
+    "gemm_e4m3_block_grouped": "iiiippipipiipiipiip",
+    "gemm_grouped": "iiiipipipiipiip",
+    "gemm_grouped_grad_a": "iiiipipipiipiip",
+    "gemm_grouped_grad_b": "iiiipipipipiiip",
+}
+
+
 def load() -> ctypes.CDLL:
     """Load the active library (built in-tree); raise if it is missing."""
     if _active not in _libs:
@@ -94,6 +108,14 @@ def load() -> ctypes.CDLL:
         lib.gemm_f16_describe_config.restype = ci
         lib.gemm_f16_force_config.argtypes = [ci]
         lib.gemm_f16_force_config.restype = ci
+        kinds = {"i": i64, "p": vp, "d": ctypes.c_double}
+        for name, letters in _OPS.items():
+            f = getattr(lib, name)
+            f.argtypes = [kinds[k] for k in letters]
+            f.restype = ci
+            setattr(lib, name + "_address", ctypes.cast(f, vp).value)
+        lib.rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        lib.rms_norm_grad_workspace_bytes.restype = i64
         # where the entry points are, for _fastcall
         for name in ("gemm_f16_f32acc", "gemm_f16_f16acc", "gemm_f16_f16acc_static_workspace", "gemm_f16_f32acc_bias_act",
                      "gemm_f16_f16acc_bias_act", "gemm_f16_f16acc_workspace"):
@@ -117,6 +139,7 @@ def _no_fast_way(*args):
 # The entry points below first ask one of these, which takes ints, None and objects with data_ptr() and returns NotImplemented, having
 # called nothing, for anything else.
 _plain, _bias_act, _workspace = (_fastcall.plain, _fastcall.bias_act, _fastcall.workspace) if _fastcall else (_no_fast_way,) * 3
+_words, _norm = (_fastcall.words, _fastcall.norm) if _fastcall else (_no_fast_way,) * 2
 
 
 def gemm_f16_f32acc(M, N, K, A, lda, B, ldb, C, ldc, stream=0) -> int:
@@ -167,6 +190,75 @@ def gemm_f16_f16acc_bias_act(M, N, K, A, lda, B, ldb, C, ldc, bias, act, stream=
     lib = load()
     rc = _bias_act(lib.gemm_f16_f16acc_bias_act_address, M, N, K, A, lda, B, ldb, C, ldc, bias, act, stream)
     return rc if rc is not NotImplemented else lib.gemm_f16_f16acc_bias_act(M, N, K, _ptr(A), lda, _ptr(B), ldb, _ptr(C), ldc, _ptr(bias), act, _ptr(stream))
+
+
+# ---- include/gemm_ops.h: the operators around the products of a transformer layer.  Matrices and pitches in elements; every function
+# but the last returns the library's status code.
+
+TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
+ACT_SWIGLU = 2
+
+
+def _general(name, args) -> int:
+    """The way through ctypes, for what _fastcall leaves: pointers as ints, None or objects with data_ptr()."""
+    return getattr(load(), name)(*[_ptr(x) if k == "p" else x for x, k in zip(args, _OPS[name], strict=True)])
+
+
+def _call(name, *args) -> int:
+    rc = _words(getattr(load(), name + "_address"), _OPS[name], *args)
+    return rc if rc is not NotImplemented else _general(name, args)
+
+
+def quantize_e4m3_rows(M, N, type, act, X, ldx, Q, ldq, scale, ld_scale, stream=0) -> int:
+    """Q (e4m3), scale[k block][row] = X (M x N of `type`; M x 2N for ACT_SWIGLU) after `act`, a scale for 128 elements of a row."""
+    return _call("quantize_e4m3_rows", M, N, type, act, X, ldx, Q, ldq, scale, ld_scale, stream)
+
+
+def quantize_e4m3_blocks(M, N, type, X, ldx, Q, ldq, scale, ld_scale, stream=0) -> int:
+    """Q (e4m3), scale[row block][column block] = X (M x N of `type`), a scale for 128 x 128 elements."""
+    return _call("quantize_e4m3_blocks", M, N, type, X, ldx, Q, ldq, scale, ld_scale, stream)
+
+
+def rms_norm(M, N, type, X, ldx, R, ldr, gamma, eps, H, ldh, Y, ldy, Q, ldq, scale, ld_scale, rstd, stream=0) -> int:
+    """H = X + R, Y = H * rstd * gamma in 16 bits and / or quantised into Q and scale; R and any output may be None."""
+    args = (M, N, type, X, ldx, R, ldr, gamma, eps, H, ldh, Y, ldy, Q, ldq, scale, ld_scale, rstd, stream)
+    rc = _norm(load().rms_norm_address, *args)
+    return rc if rc is not NotImplemented else _general("rms_norm", args)
+
+
+def rms_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, rstd, dH, lddh, dX, lddx, dgamma, workspace, workspace_bytes, stream=0) -> int:
+    """dX (of x and of the residual alike) and dgamma (f32, None: not formed) from dY and dH (None: no gradient of h itself)."""
+    return _call("rms_norm_grad", M, N, type, dY, lddy, H, ldh, gamma, rstd, dH, lddh, dX, lddx, dgamma, workspace, workspace_bytes, stream)
+
+
+def gemm_e4m3_block(M, N, K, A, lda, a_scale, ld_as, B, ldb, b_scale, ld_bs, C, ldc, c_type, stream=0) -> int:
+    """C (M x N of `c_type`) = A (M x K e4m3, scales in rows) @ B (N x K e4m3, scales in blocks) transposed."""
+    return _call("gemm_e4m3_block", M, N, K, A, lda, a_scale, ld_as, B, ldb, b_scale, ld_bs, C, ldc, c_type, stream)
+
+
+def gemm_e4m3_block_grouped(T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb, b_stride, b_scale, ld_bs, bs_stride, C, ldc, c_type, stream=0) -> int:
+    """gemm_e4m3_block of rows offsets[e] .. offsets[e + 1] (int32 on the device) with B[e], for E experts."""
+    return _call("gemm_e4m3_block_grouped", T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb, b_stride, b_scale, ld_bs, bs_stride, C, ldc, c_type, stream)
+
+
+def gemm_grouped(T, N, K, E, offsets, type, A, lda, B, ldb, b_stride, C, ldc, c_type, stream=0) -> int:
+    """C (T x N) = rows of A (T x K) @ B[e] (K x N), rows offsets[e] .. offsets[e + 1] with expert e."""
+    return _call("gemm_grouped", T, N, K, E, offsets, type, A, lda, B, ldb, b_stride, C, ldc, c_type, stream)
+
+
+def gemm_grouped_grad_a(T, N, K, E, offsets, type, dC, lddc, B, ldb, b_stride, dA, ldda, a_type, stream=0) -> int:
+    """dA (T x K) = rows of dC (T x N) @ B[e] (K x N) transposed."""
+    return _call("gemm_grouped_grad_a", T, N, K, E, offsets, type, dC, lddc, B, ldb, b_stride, dA, ldda, a_type, stream)
+
+
+def gemm_grouped_grad_b(T, N, K, E, offsets, type, A, lda, dC, lddc, dB, lddb, db_stride, b_type, stream=0) -> int:
+    """dB[e] (K x N) = A_e transposed @ dC_e, summed over the expert's rows; zeros for an expert without rows."""
+    return _call("gemm_grouped_grad_b", T, N, K, E, offsets, type, A, lda, dC, lddc, dB, lddb, db_stride, b_type, stream)
+
+
+def rms_norm_grad_workspace_bytes(M, N) -> int:
+    """Bytes of workspace that rms_norm_grad needs to form dgamma."""
+    return load().rms_norm_grad_workspace_bytes(M, N)
 
 
 def strerror(code: int) -> str:

@@ -1,6 +1,6 @@
 """Build the HIP libraries in-tree for gfx950 with hipcc.
 
-libgemm_f16.so         the product: the C ABI of include/gemm_f16.h and the kernels it selects
+libgemm_f16.so         the product: the C ABIs of include/gemm_f16.h and include/gemm_ops.h and the kernels they select
 _fastcall.*.so         the binding's way into the product's entry points without ctypes (csrc/fastcall.c, host code only)
 libgemm_f16_ladder.so  the same sources compiled with -DGEMM_F16_LADDER plus csrc/ladder/*.hip: the
                        comparison kernels and ablation rows appended to the configuration table
@@ -24,7 +24,9 @@ LIB = os.path.join(HERE, "libgemm_f16.so")
 FASTCALL = os.path.join(HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 FASTCALL_CC = ("gcc", "cc", "amdclang", "clang")         # the first one that is there (hipcc would link the HIP runtime into it)
 LADDER_LIB = os.path.join(HERE, "libgemm_f16_ladder.so")
-SOURCES = ["gemm_api.hip", "gemm_generic.hip", "gemm_unaligned.hip", "gemm_unaligned_pp.hip", "gemm_kslice.hip", "gemm_tiled.hip", "gemm_pingpong.hip", "gemm_pp128.hip", "gemm_w4a.hip", "gemm_w4a128.hip", "gemm_splitk_f16.hip"]
+SOURCES = ["gemm_api.hip", "gemm_generic.hip", "gemm_unaligned.hip", "gemm_unaligned_pp.hip", "gemm_kslice.hip", "gemm_tiled.hip", "gemm_pingpong.hip", "gemm_pp128.hip", "gemm_w4a.hip", "gemm_w4a128.hip", "gemm_splitk_f16.hip",
+           "ops_api.hip", "ops_generic.hip", "ops_norm.hip"]
+PLAIN_SOURCES = {s for s in SOURCES if s.startswith("ops_")}           # the same in both libraries
 LADDER_SOURCES = ["ladder/gemm_w4.hip", "ladder/gemm_overlap.hip", "ladder/gemm_interleaved.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          # packed-f32 VALU forms are kept off for every HIP file of this library
@@ -72,13 +74,13 @@ def build(verbose: bool = False, ladder: bool = True, extra=()) -> str:
     jobs = [(s, os.path.join(OBJ, s.replace("/", "_") + ".o"), list(extra)) for s in SOURCES]
     if ladder:
         jobs += [(s, os.path.join(OBJ, s.replace("/", "_") + ".ladder.o"), ["-DGEMM_F16_LADDER", *extra])
-                 for s in SOURCES + LADDER_SOURCES]
+                 for s in SOURCES + LADDER_SOURCES if s not in PLAIN_SOURCES]
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
         logs = list(pool.map(lambda j: _compile(j[0], j[1], j[2], verbose), jobs))
     link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-Wno-unused-command-line-argument"]
     subprocess.run([*link, "-o", LIB, *[j[1] for j in jobs[:len(SOURCES)]]], check=True)
     if ladder:
-        subprocess.run([*link, "-o", LADDER_LIB, *[j[1] for j in jobs[len(SOURCES):]]], check=True)
+        subprocess.run([*link, "-o", LADDER_LIB, *[j[1] for j in jobs[len(SOURCES):]], *[j[1] for j in jobs[:len(SOURCES)] if j[0] in PLAIN_SOURCES]], check=True)
     build_fastcall()
     if verbose:
         print(resource_table("".join(logs[:len(SOURCES)])))

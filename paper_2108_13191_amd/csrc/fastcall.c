@@ -7,7 +7,10 @@
  * data_ptr().  Integers are converted as ctypes converts them (modulo 2^64, an int modulo 2^32).  Given anything else -- another
  * type, an object whose data_ptr() raises, another number of arguments -- it calls nothing and returns NotImplemented, and
  * the caller takes the general way, which accepts or refuses the arguments as it always has.  The GIL is released around the
- * call, as ctypes does. */
+ * call, as ctypes does.
+ *
+ * The entry points of gemm_ops.h take up to 19 arguments; `words` calls any of them whose arguments are all 64-bit integers and
+ * pointers, told by a text with a letter for each ("i", "p"), and `norm` is for rms_norm, which has a double among them. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -97,10 +100,62 @@ static PyObject* workspace(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
+#define MOST_WORDS 19
+/* 1: converted, 0: no arguments for this way */
+static int to_words(const char* kinds, PyObject* const* a, Py_ssize_t n, uint64_t* w)
+{
+    for (Py_ssize_t i = 0; i < n; i++) {
+        void* p;
+        if (kinds[i] == 'p') { if (!to_pointer(a[i], &p)) return 0; w[i] = (uint64_t)(uintptr_t)p; }
+        else if (kinds[i] != 'i' || !to_word(a[i], &w[i])) return 0;
+    }
+    return 1;
+}
+
+/* words(address, kinds, ...): int f(...) of as many 64-bit integers and pointers, which the calling convention passes alike.
+ * The C side's arguments are int64_t, pointers and nothing else; those behind the last are given as 0 and not looked at. */
+typedef int (*words_fn)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
+                        uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t);
+static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    uint64_t f, w[MOST_WORDS] = {0};
+    Py_ssize_t length;
+    int rc;
+    if (n < 2 || n - 2 > MOST_WORDS || !PyUnicode_Check(a[1]) || !to_word(a[0], &f)) return other_way();
+    const char* const kinds = PyUnicode_AsUTF8AndSize(a[1], &length);
+    if (!kinds) PyErr_Clear();
+    if (!kinds || length != n - 2 || !to_words(kinds, a + 2, n - 2, w)) return other_way();
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((words_fn)(uintptr_t)f)(w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15], w[16], w[17], w[18]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+typedef int (*norm_fn)(int64_t, int64_t, int64_t, const void*, int64_t, const void*, int64_t, const void*, double, void*, int64_t, void*, int64_t,
+                       void*, int64_t, void*, int64_t, void*, void*);
+static PyObject* norm(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    uint64_t f, b[8], c[10];
+    int rc;
+    if (n != 20 || !to_word(a[0], &f) || !to_words("iiipipip", a + 1, 8, b) || !PyFloat_CheckExact(a[9]) || !to_words("pipipipipp", a + 10, 10, c)) return other_way();
+    const double eps = PyFloat_AS_DOUBLE(a[9]);
+#define P(x) ((void*)(uintptr_t)(x))
+#define I(x) ((int64_t)(x))
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((norm_fn)(uintptr_t)f)(I(b[0]), I(b[1]), I(b[2]), P(b[3]), I(b[4]), P(b[5]), I(b[6]), P(b[7]), eps, P(c[0]), I(c[1]), P(c[2]), I(c[3]),
+                                 P(c[4]), I(c[5]), P(c[6]), I(c[7]), P(c[8]), P(c[9]));
+    Py_END_ALLOW_THREADS
+#undef P
+#undef I
+    return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {
     {"plain", (PyCFunction)(void (*)(void))plain, METH_FASTCALL, "plain(address, M, N, K, A, lda, B, ldb, C, ldc, stream)"},
     {"bias_act", (PyCFunction)(void (*)(void))bias_act, METH_FASTCALL, "bias_act(address, M, N, K, A, lda, B, ldb, C, ldc, bias, act, stream)"},
     {"workspace", (PyCFunction)(void (*)(void))workspace, METH_FASTCALL, "workspace(address, M, N, K, A, lda, B, ldb, C, ldc, workspace, workspace_bytes, stream)"},
+    {"words", (PyCFunction)(void (*)(void))words, METH_FASTCALL, "words(address, kinds, ...)"},
+    {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, "norm(address, M, N, type, X, ldx, R, ldr, gamma, eps, H, ldh, Y, ldy, Q, ldq, scale, ld_scale, rstd, stream)"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "Calls into the C ABI of libgemm_f16.so", -1, methods, NULL, NULL, NULL, NULL};

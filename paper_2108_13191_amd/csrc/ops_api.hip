@@ -1,0 +1,188 @@
+// The C ABI of include/gemm_ops.h: checks of arguments and the choice of kernel.
+#include "ops_common.h"
+#include "../../include/gemm_ops.h"
+
+namespace {
+
+bool bad_size(int64_t n) { return n < 0 || n > INT32_MAX; }
+bool bad_pitch(int64_t ld, int64_t row) { return ld < row || ld > INT32_MAX; }
+bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+int64_t blocks128(int64_t n) { return (n + 127) / 128; }
+bool is_16bit(int64_t type) { return type == GEMM_TYPE_F16 || type == GEMM_TYPE_BF16; }
+int type_size(int64_t type) { return type == GEMM_TYPE_F32 ? 4 : 2; }
+
+// The e4m3 products.  E < 0: one product, nothing grouped.
+int run_e4m3(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
+             const void* A, int64_t lda, const float* sa, int64_t ld_as, const void* B, int64_t ldb, int64_t b_stride,
+             const float* sb, int64_t ld_bs, int64_t bs_stride, void* C, int64_t ldc, int64_t c_type, void* stream)
+{
+    if (bad_size(M) || bad_size(N) || bad_size(K) || E > 65535) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(c_type) && c_type != GEMM_TYPE_F32) return GEMM_F16_ERR_CONFIG;
+    if (M == 0 || N == 0 || E == 0) return GEMM_F16_OK;
+    if (bad_pitch(lda, K) || bad_pitch(ldb, K) || bad_pitch(ldc, N) || b_stride < 0 || bs_stride < 0) return GEMM_F16_ERR_PITCH;
+    if (K > 0 && (bad_pitch(ld_as, M) || bad_pitch(ld_bs, blocks128(K)))) return GEMM_F16_ERR_PITCH;
+    if (!C || (E > 0 && !offsets) || (K > 0 && (!A || !B || !sa || !sb))) return GEMM_F16_ERR_NULL;
+    if (unaligned(C, type_size(c_type)) || unaligned(sa, 4) || unaligned(sb, 4) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
+    OpsGemm g = {};
+    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.E = E < 0 ? 1 : (int)E;
+    g.offsets = offsets;
+    g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride;
+    g.C = (char*)C; g.ldc = ldc;
+    g.sa = sa; g.ld_sa = ld_as; g.sb = sb; g.ld_sb = ld_bs; g.sb_stride = bs_stride;
+    g.elem = ELEM_E4M3; g.c_type = (int)c_type; g.a_kc = g.b_kc = true;
+    g.num_xcd = chip().xcds;
+    g.stream = (hipStream_t)stream;
+    return ops_launch_generic(g);
+}
+
+// The 16-bit products grouped by expert, with the checks they share done on what the caller calls its matrices.
+int run_grouped(const OpsGemm& g)
+{
+    return ops_launch_generic(g);
+}
+
+int check_grouped(int64_t T, int64_t N, int64_t K, int64_t E, int64_t type, int64_t out_type)
+{
+    if (bad_size(T) || bad_size(N) || bad_size(K) || E < 0 || E > 65535) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(type) || (out_type != type && out_type != GEMM_TYPE_F32)) return GEMM_F16_ERR_CONFIG;
+    return GEMM_F16_OK;
+}
+
+OpsGemm grouped_params(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, int64_t c_type, void* stream)
+{
+    OpsGemm g = {};
+    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.E = (int)E;
+    g.offsets = offsets;
+    g.elem = (int)type; g.c_type = (int)c_type;
+    g.num_xcd = chip().xcds;
+    g.stream = (hipStream_t)stream;
+    return g;
+}
+
+}  // namespace
+
+extern "C" {
+
+int quantize_e4m3_rows(int64_t M, int64_t N, int64_t type, int64_t act, const void* X, int64_t ldx,
+                       void* Q, int64_t ldq, float* scale, int64_t ld_scale, void* stream)
+{
+    if (bad_size(M) || bad_size(N)) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(type) || (act != GEMM_OPS_ACT_NONE && act != GEMM_OPS_ACT_RELU && act != GEMM_OPS_ACT_SWIGLU)) return GEMM_F16_ERR_CONFIG;
+    if (M == 0 || N == 0) return GEMM_F16_OK;
+    if (bad_pitch(ldx, act == GEMM_OPS_ACT_SWIGLU ? 2 * N : N) || bad_pitch(ldq, N) || bad_pitch(ld_scale, M)) return GEMM_F16_ERR_PITCH;
+    if (!X || !Q || !scale) return GEMM_F16_ERR_NULL;
+    if (unaligned(X, 2) || unaligned(scale, 4)) return GEMM_F16_ERR_ALIGN;
+    return ops_launch_quant_rows((int)type, {(int)M, (int)N, (int)act, X, ldx, (uint8_t*)Q, ldq, scale, ld_scale}, (hipStream_t)stream);
+}
+
+int quantize_e4m3_blocks(int64_t M, int64_t N, int64_t type, const void* X, int64_t ldx,
+                         void* Q, int64_t ldq, float* scale, int64_t ld_scale, void* stream)
+{
+    if (bad_size(M) || bad_size(N)) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(type)) return GEMM_F16_ERR_CONFIG;
+    if (M == 0 || N == 0) return GEMM_F16_OK;
+    if (bad_pitch(ldx, N) || bad_pitch(ldq, N) || bad_pitch(ld_scale, blocks128(N))) return GEMM_F16_ERR_PITCH;
+    if (!X || !Q || !scale) return GEMM_F16_ERR_NULL;
+    if (unaligned(X, 2) || unaligned(scale, 4)) return GEMM_F16_ERR_ALIGN;
+    return ops_launch_quant_blocks((int)type, {(int)M, (int)N, GEMM_OPS_ACT_NONE, X, ldx, (uint8_t*)Q, ldq, scale, ld_scale}, (hipStream_t)stream);
+}
+
+int rms_norm(int64_t M, int64_t N, int64_t type, const void* X, int64_t ldx, const void* R, int64_t ldr,
+             const void* gamma, double eps, void* H, int64_t ldh, void* Y, int64_t ldy,
+             void* Q, int64_t ldq, float* scale, int64_t ld_scale, float* rstd, void* stream)
+{
+    if (bad_size(M) || bad_size(N)) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(type) || !(eps >= 0.0)) return GEMM_F16_ERR_CONFIG;
+    if (M == 0 || N == 0) return GEMM_F16_OK;
+    if (bad_pitch(ldx, N) || (R && bad_pitch(ldr, N)) || (H && bad_pitch(ldh, N)) || (Y && bad_pitch(ldy, N)) ||
+        (Q && (bad_pitch(ldq, N) || bad_pitch(ld_scale, M)))) return GEMM_F16_ERR_PITCH;
+    if (!X || !gamma || !Q != !scale) return GEMM_F16_ERR_NULL;
+    if (unaligned(X, 2) || unaligned(R, 2) || unaligned(gamma, 2) || unaligned(H, 2) || unaligned(Y, 2) || unaligned(scale, 4) || unaligned(rstd, 4)) return GEMM_F16_ERR_ALIGN;
+    return ops_launch_norm((int)type, {(int)M, (int)N, X, R, gamma, ldx, ldr, H, Y, ldh, ldy, (uint8_t*)Q, ldq, scale, ld_scale, rstd, (float)eps}, (hipStream_t)stream);
+}
+
+int64_t rms_norm_grad_workspace_bytes(int64_t M, int64_t N)
+{
+    if (M <= 0 || N <= 0 || M > INT32_MAX || N > INT32_MAX) return 0;
+    return 4 * N * ops_norm_grad_parts(M, N);
+}
+
+int rms_norm_grad(int64_t M, int64_t N, int64_t type, const void* dY, int64_t lddy, const void* H, int64_t ldh,
+                  const void* gamma, const float* rstd, const void* dH, int64_t lddh, void* dX, int64_t lddx, float* dgamma,
+                  void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (bad_size(M) || bad_size(N)) return GEMM_F16_ERR_SIZE;
+    if (!is_16bit(type)) return GEMM_F16_ERR_CONFIG;
+    if (N == 0 || (M == 0 && !dgamma)) return GEMM_F16_OK;
+    if (M > 0) {
+        if (bad_pitch(lddy, N) || bad_pitch(ldh, N) || bad_pitch(lddx, N) || (dH && bad_pitch(lddh, N))) return GEMM_F16_ERR_PITCH;
+        if (!dY || !H || !gamma || !rstd || !dX || (dgamma && !workspace)) return GEMM_F16_ERR_NULL;
+        if (unaligned(dY, 2) || unaligned(H, 2) || unaligned(gamma, 2) || unaligned(dH, 2) || unaligned(dX, 2) || unaligned(rstd, 4) || (dgamma && unaligned(workspace, 16))) return GEMM_F16_ERR_ALIGN;
+        if (dgamma && workspace_bytes < rms_norm_grad_workspace_bytes(M, N)) return GEMM_F16_ERR_WORKSPACE;
+    }
+    if (unaligned(dgamma, 4)) return GEMM_F16_ERR_ALIGN;
+    return ops_launch_norm_grad((int)type, {(int)M, (int)N, dY, H, gamma, dH, rstd, lddy, ldh, lddh, dX, lddx, dgamma, (float*)workspace}, (hipStream_t)stream);
+}
+
+int gemm_e4m3_block(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* a_scale, int64_t ld_as,
+                    const void* B, int64_t ldb, const float* b_scale, int64_t ld_bs, void* C, int64_t ldc, int64_t c_type, void* stream)
+{
+    return run_e4m3(M, N, K, -1, nullptr, A, lda, a_scale, ld_as, B, ldb, 0, b_scale, ld_bs, 0, C, ldc, c_type, stream);
+}
+
+int gemm_e4m3_block_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, const void* A, int64_t lda, const float* a_scale, int64_t ld_as,
+                            const void* B, int64_t ldb, int64_t b_stride, const float* b_scale, int64_t ld_bs, int64_t bs_stride,
+                            void* C, int64_t ldc, int64_t c_type, void* stream)
+{
+    if (E < 0) return GEMM_F16_ERR_SIZE;
+    return run_e4m3(T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb, b_stride, b_scale, ld_bs, bs_stride, C, ldc, c_type, stream);
+}
+
+int gemm_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, const void* A, int64_t lda,
+                 const void* B, int64_t ldb, int64_t b_stride, void* C, int64_t ldc, int64_t c_type, void* stream)
+{
+    const int rc = check_grouped(T, N, K, E, type, c_type);
+    if (rc != GEMM_F16_OK) return rc;
+    if (T == 0 || N == 0 || E == 0) return GEMM_F16_OK;
+    if (bad_pitch(lda, K) || bad_pitch(ldb, N) || bad_pitch(ldc, N) || b_stride < 0) return GEMM_F16_ERR_PITCH;
+    if (!C || !offsets || (K > 0 && (!A || !B))) return GEMM_F16_ERR_NULL;
+    if (unaligned(A, 2) || unaligned(B, 2) || unaligned(C, type_size(c_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
+    OpsGemm g = grouped_params(T, N, K, E, offsets, type, c_type, stream);
+    g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)C; g.ldc = ldc;
+    g.a_kc = true; g.b_kc = false;
+    return run_grouped(g);
+}
+
+int gemm_grouped_grad_a(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, const void* dC, int64_t lddc,
+                        const void* B, int64_t ldb, int64_t b_stride, void* dA, int64_t ldda, int64_t a_type, void* stream)
+{
+    const int rc = check_grouped(T, N, K, E, type, a_type);
+    if (rc != GEMM_F16_OK) return rc;
+    if (T == 0 || K == 0 || E == 0) return GEMM_F16_OK;
+    if (bad_pitch(lddc, N) || bad_pitch(ldb, N) || bad_pitch(ldda, K) || b_stride < 0) return GEMM_F16_ERR_PITCH;
+    if (!dA || !offsets || (N > 0 && (!dC || !B))) return GEMM_F16_ERR_NULL;
+    if (unaligned(dC, 2) || unaligned(B, 2) || unaligned(dA, type_size(a_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
+    // rows of dC by rows of B[e]: the sum runs over the N that both have contiguous
+    OpsGemm g = grouped_params(T, K, N, E, offsets, type, a_type, stream);
+    g.A = (const char*)dC; g.lda = lddc; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)dA; g.ldc = ldda;
+    g.a_kc = true; g.b_kc = true;
+    return run_grouped(g);
+}
+
+int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, const void* A, int64_t lda,
+                        const void* dC, int64_t lddc, void* dB, int64_t lddb, int64_t db_stride, int64_t b_type, void* stream)
+{
+    const int rc = check_grouped(T, N, K, E, type, b_type);
+    if (rc != GEMM_F16_OK) return rc;
+    if (N == 0 || K == 0 || E == 0) return GEMM_F16_OK;
+    if (bad_pitch(lda, K) || bad_pitch(lddc, N) || bad_pitch(lddb, N) || (E > 1 && db_stride < (K - 1) * lddb + N)) return GEMM_F16_ERR_PITCH;
+    if (!dB || !offsets || (T > 0 && (!A || !dC))) return GEMM_F16_ERR_NULL;
+    if (unaligned(A, 2) || unaligned(dC, 2) || unaligned(dB, type_size(b_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
+    // columns of A by columns of dC: the sum runs over the group's rows
+    OpsGemm g = grouped_params(K, N, T, E, offsets, type, b_type, stream);
+    g.A = (const char*)A; g.lda = lda; g.B = (const char*)dC; g.ldb = lddc; g.C = (char*)dB; g.ldc = lddb; g.c_stride = db_stride;
+    g.a_kc = false; g.b_kc = false; g.k_ragged = true;
+    return run_grouped(g);
+}
+
+}  // extern "C"

@@ -1,0 +1,59 @@
+// Shared declarations of the operators of include/gemm_ops.h: parameters of the grouped and e4m3 products, launcher
+// prototypes.  gfx950 only.
+#pragma once
+#include "gemm_common.h"
+
+typedef __bf16 bf16_t;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+
+enum OpsElem { ELEM_E4M3 = 3, ELEM_F16 = 0, ELEM_BF16 = 1, ELEM_F32 = 2 };      // the 16- and 32-bit ones as GEMM_TYPE_*
+
+// One product C = A B in groups.  What is ragged:
+//   offsets == nullptr   nothing: one product of M x N x K
+//   !k_ragged            rows: group e multiplies rows offsets[e] .. offsets[e+1]-1 of A (M in all) by B[e]
+//   k_ragged             the sum: group e sums over k rows offsets[e] .. offsets[e+1]-1 (K in all) into C[e]
+// Operands lie either with the summed index contiguous in a row ("k rows": A M x K, B N x K) or with the other one
+// (A K x M, B K x N).
+struct OpsGemm {
+    int M, N, K, E;
+    const int32_t* offsets;
+    const char* A; int64_t lda;                          // pitches and strides in elements
+    const char* B; int64_t ldb, b_stride;
+    char* C; int64_t ldc, c_stride;
+    const float* sa; int64_t ld_sa;                      // e4m3: scales of A [k block][row], of B [column block][k block]
+    const float* sb; int64_t ld_sb, sb_stride;
+    int elem, c_type;                                    // OpsElem
+    bool a_kc, b_kc;                                     // summed index contiguous
+    bool k_ragged;
+    int num_xcd;
+    hipStream_t stream;
+};
+
+// ops_generic.hip: any alignment, any size
+int ops_launch_generic(const OpsGemm& g);
+
+// ops_norm.hip
+struct NormArgs {
+    int M, N;
+    const void *X, *R, *gamma; int64_t ldx, ldr;
+    void *H, *Y; int64_t ldh, ldy;
+    uint8_t* Q; int64_t ldq; float* scale; int64_t ld_scale;
+    float* rstd; float eps;
+};
+struct NormGradArgs {
+    int M, N;
+    const void *dY, *H, *gamma, *dH; const float* rstd; int64_t lddy, ldh, lddh;
+    void* dX; int64_t lddx;
+    float *dgamma, *ws;
+};
+struct QuantArgs {
+    int M, N, act;
+    const void* X; int64_t ldx;
+    uint8_t* Q; int64_t ldq; float* scale; int64_t ld_scale;
+};
+int ops_launch_norm(int type, const NormArgs& a, hipStream_t stream);
+int ops_norm_grad_parts(int64_t M, int64_t N);            // rows of N floats of workspace
+int ops_launch_norm_grad(int type, const NormGradArgs& a, hipStream_t stream);
+int ops_launch_quant_rows(int type, const QuantArgs& a, hipStream_t stream);
+int ops_launch_quant_blocks(int type, const QuantArgs& a, hipStream_t stream);

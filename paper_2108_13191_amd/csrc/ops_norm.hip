@@ -1,0 +1,438 @@
+// RMS norm with the residual's addition, its gradients, and quantisation to e4m3 with a scale for each block of 128
+// (include/gemm_ops.h).
+//
+// All of it is bound by memory: every element is read once and written once, in 16-byte accesses (8 elements of 16 bits a lane), and what a row's
+// sum needs again stays in registers.  A block of 128 is 16 neighbouring lanes, so its largest magnitude takes four
+// rotations within a row of lanes.  Accesses are at element alignment: rows of any pitch take the same path.
+#include "ops_device.h"
+#include "../../include/gemm_ops.h"
+
+namespace {
+
+using namespace ops_dev;
+
+// ---- 8 elements of a row of which `left` are there, zeros behind its end ----------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int left, float (&v)[8])
+{
+    if (left >= 8) {
+        const typename Vec8<T>::type x = *(const typename Vec8<T>::type*)p;
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = (float)x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int left, const float (&v)[8])
+{
+    if (left >= 8) {
+        typename Vec8<T>::type x;
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i] = (T)v[i];
+        *(typename Vec8<T>::type*)p = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) if (i < left) p[i] = (T)v[i];
+    }
+}
+typedef uintx2 uintx2_any __attribute__((aligned(1)));
+__device__ __forceinline__ void store_e4m3(uint8_t* p, int left, uintx2 q)
+{
+    if (left >= 8) {
+        *(uintx2_any*)p = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) if (i < left) p[i] = (uint8_t)((i < 4 ? q[0] : q[1]) >> (8 * (i & 3)));
+    }
+}
+template <typename T> __device__ __forceinline__ float rounded(float x) { return (float)(T)x; }
+
+// Sum over the W wavefronts that share a row.  `lds`: a float for each wavefront of the workgroup.
+template <int W>
+__device__ __forceinline__ float sum_row(float x, float* lds)
+{
+    x = sum64(x);
+    if constexpr (W > 1) {
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();                                 // the values of the sum before have been read
+        if ((threadIdx.x & 63) == 0) lds[wave] = x;
+        __syncthreads();
+        x = 0.0f;
+        const int first = wave / W * W;
+#pragma unroll
+        for (int i = 0; i < W; i++) x += lds[first + i];
+    }
+    return x;
+}
+
+// ---- the norm ---------------------------------------------------------------------------------------------------------------
+// W wavefronts a row, each lane with P chunks of 8 columns in registers; R rows a workgroup.  LOOP: rows of any length, the chunks
+// are gone through twice (the second time h comes from H, or is formed again).
+template <typename T, int W, int P, int R, bool LOOP>
+__global__ __launch_bounds__(64 * W * R) void rms_norm_kernel(const NormArgs a)
+{
+    __shared__ float lds[W * R];
+    const int lane = threadIdx.x % (64 * W);
+    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / (64 * W);
+    const bool live = row < a.M;
+    const T* const x = (const T*)a.X + row * a.ldx;
+    const T* const r = a.R ? (const T*)a.R + row * a.ldr : nullptr;
+    T* const h = a.H ? (T*)a.H + row * a.ldh : nullptr;
+
+    float v[P][8];
+    float sum = 0.0f;
+    auto form = [&](int64_t c, float (&o)[8]) {
+        load8(x + c, (int)(a.N - c), o);
+        if (r) {
+            float s[8];
+            load8(r + c, (int)(a.N - c), s);
+#pragma unroll
+            for (int i = 0; i < 8; i++) o[i] = rounded<T>(o[i] + s[i]);      // h as it is stored is what is normed
+        }
+    };
+    auto finish = [&](int64_t c, const float (&o)[8], float rstd) {
+        const int left = (int)(a.N - c);
+        float gm[8], y[8];
+        load8((const T*)a.gamma + c, left, gm);
+#pragma unroll
+        for (int i = 0; i < 8; i++) y[i] = o[i] * rstd * gm[i];
+        if (a.Y) store8((T*)a.Y + row * a.ldy + c, left, y);
+        if (a.Q) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = max(m, magnitude(y[i]));
+            const BlockScale s = block_scale(max16(m));
+            store_e4m3(a.Q + row * a.ldq + c, left, to_e4m3(y, s.inverse));
+            if ((lane & 15) == 0) a.scale[c / 128 * a.ld_scale + row] = s.scale;
+        }
+    };
+    if (live) {
+        const int passes = LOOP ? (a.N + 512 * W - 1) / (512 * W) : P;
+        for (int p0 = 0; p0 < passes; p0 += P)
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                const int64_t c = 8 * ((int64_t)lane + 64 * W * (p0 + p));
+                if (c < a.N) {
+                    form(c, v[p]);
+                    if (h) store8(h + c, (int)(a.N - c), v[p]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; i++) v[p][i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum += v[p][i] * v[p][i];
+            }
+    }
+    const float rstd = 1.0f / sqrtf(sum_row<W>(sum, lds) / (float)a.N + a.eps);
+    if (!live) return;
+    if (a.rstd && lane == 0) a.rstd[row] = rstd;
+    if (!a.Y && !a.Q) return;
+    if constexpr (LOOP) {
+        // whole blocks of 16 lanes take part in a block's scale: a chunk behind the row's end is zeros
+        for (int64_t c = 8 * (int64_t)lane; c < ((int64_t)a.N + 127) / 128 * 128; c += 512 * W) {
+            float o[8] = {};
+            if (c < a.N) { if (h) load8((const T*)h + c, (int)(a.N - c), o); else form(c, o); }
+            finish(c, o, rstd);
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + 64 * W * p);
+            if (c < (a.N + 127) / 128 * 128) finish(c, v[p], rstd);
+        }
+    }
+}
+
+template <typename T, int W, int P, int R, bool LOOP = false>
+int launch_norm(const NormArgs& a, hipStream_t stream)
+{
+    const unsigned grid = (unsigned)(((int64_t)a.M + R - 1) / R);
+    hipLaunchKernelGGL((rms_norm_kernel<T, W, P, R, LOOP>), dim3(grid), dim3(64 * W * R), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+}
+
+template <typename T>
+int norm_of_type(const NormArgs& a, hipStream_t stream)
+{
+    if (a.N <= 512) return launch_norm<T, 1, 1, 4>(a, stream);
+    if (a.N <= 1024) return launch_norm<T, 1, 2, 4>(a, stream);
+    if (a.N <= 2048) return launch_norm<T, 1, 4, 4>(a, stream);
+    if (a.N <= 4096) return launch_norm<T, 4, 2, 1>(a, stream);
+    if (a.N <= 8192) return launch_norm<T, 4, 4, 1>(a, stream);
+    if (a.N <= 16384) return launch_norm<T, 8, 4, 1>(a, stream);
+    return launch_norm<T, 16, 1, 1, true>(a, stream);
+}
+
+// ---- its gradients ------------------------------------------------------------------------------------------------------------
+// dX row by row; the columns' sums of dy xhat stay in registers over all rows of a workgroup, which writes them as one row of the workspace;
+// a second kernel adds those.  Every sum has a fixed order.
+template <typename T, int W, int P, int R>
+__global__ __launch_bounds__(64 * W * R) void rms_norm_grad_kernel(const NormGradArgs a)
+{
+    extern __shared__ float dyn[];                        // W * R floats, then (R > 1) a row of sums
+    const int lane = threadIdx.x % (64 * W), sub = threadIdx.x / (64 * W);
+    float dg[P][8] = {};
+    const int64_t step = (int64_t)gridDim.x * R;
+    for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.M; row0 += step) {      // the same number of trips for the whole workgroup
+        const int64_t row = row0 + sub;
+        const bool live = row < a.M;
+        float dy[P][8], hv[P][8], gm[8];
+        const float rstd = live ? a.rstd[row] : 0.0f;
+        float dot = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + 64 * W * p);
+            const int left = live ? a.N - c : 0;              // not above 0: nothing is read
+            load8((const T*)a.dY + row * a.lddy + c, left, dy[p]);
+            load8((const T*)a.H + row * a.ldh + c, left, hv[p]);
+            load8((const T*)a.gamma + c, left, gm);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float xhat = hv[p][i] * rstd;
+                hv[p][i] = xhat;
+                dg[p][i] += dy[p][i] * xhat;
+                dy[p][i] *= gm[i];
+                dot += dy[p][i] * xhat;
+            }
+        }
+        const float mean = sum_row<W>(dot, dyn) / (float)a.N;
+        if (live) {
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                const int c = 8 * (lane + 64 * W * p);
+                if (c >= a.N) continue;
+                float o[8], up[8] = {};
+                if (a.dH) load8((const T*)a.dH + row * a.lddh + c, a.N - c, up);
+#pragma unroll
+                for (int i = 0; i < 8; i++) o[i] = rstd * (dy[p][i] - hv[p][i] * mean) + up[i];
+                store8((T*)a.dX + row * a.lddx + c, a.N - c, o);
+            }
+        }
+    }
+    if (!a.dgamma) return;
+    // sums of the workgroup's row slots, in their order
+    float* const rows = dyn + W * R;
+    for (int s = R - 1; s > 0; s--)
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            __syncthreads();
+            if (sub == s)
+#pragma unroll
+                for (int i = 0; i < 8; i++) rows[i * 64 * W + lane] = dg[p][i];
+            __syncthreads();
+            if (sub == s - 1)
+#pragma unroll
+                for (int i = 0; i < 8; i++) dg[p][i] += rows[i * 64 * W + lane];
+        }
+    if (sub == 0) {
+        float* const out = a.ws + (int64_t)blockIdx.x * a.N;
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + 64 * W * p);
+#pragma unroll
+            for (int i = 0; i < 8; i++) if (c + i < a.N) out[c + i] = dg[p][i];
+        }
+    }
+}
+
+// Rows longer than the registers hold: dX in two passes over a row ...
+template <typename T>
+__global__ __launch_bounds__(1024) void rms_norm_grad_long_kernel(const NormGradArgs a)
+{
+    __shared__ float lds[16];
+    const int64_t row = blockIdx.x;
+    const T *const dyr = (const T*)a.dY + row * a.lddy, *const hr = (const T*)a.H + row * a.ldh, *const gr = (const T*)a.gamma;
+    const float rstd = a.rstd[row];
+    float dy[8], hv[8], gm[8], dot = 0.0f;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.N; c += 8192) {
+        load8(dyr + c, (int)(a.N - c), dy); load8(hr + c, (int)(a.N - c), hv); load8(gr + c, (int)(a.N - c), gm);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dot += dy[i] * gm[i] * (hv[i] * rstd);
+    }
+    const float mean = sum_row<16>(dot, lds) / (float)a.N;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.N; c += 8192) {
+        float up[8] = {}, o[8];
+        load8(dyr + c, (int)(a.N - c), dy); load8(hr + c, (int)(a.N - c), hv); load8(gr + c, (int)(a.N - c), gm);
+        if (a.dH) load8((const T*)a.dH + row * a.lddh + c, (int)(a.N - c), up);
+#pragma unroll
+        for (int i = 0; i < 8; i++) o[i] = rstd * (dy[i] * gm[i] - hv[i] * rstd * mean) + up[i];
+        store8((T*)a.dX + row * a.lddx + c, (int)(a.N - c), o);
+    }
+}
+// ... and the columns' sums before it (dX may be dY): a workgroup takes 2048 columns and every gridDim.y-th row
+template <typename T>
+__global__ __launch_bounds__(256) void rms_norm_dgamma_long_kernel(const NormGradArgs a)
+{
+    const int64_t c = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+    if (c >= a.N) return;
+    float dg[8] = {}, dy[8], hv[8];
+    for (int64_t row = blockIdx.y; row < a.M; row += gridDim.y) {
+        load8((const T*)a.dY + row * a.lddy + c, (int)(a.N - c), dy);
+        load8((const T*)a.H + row * a.ldh + c, (int)(a.N - c), hv);
+        const float rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < 8; i++) dg[i] += dy[i] * (hv[i] * rstd);
+    }
+    for (int i = 0; i < 8; i++) if (c + i < a.N) a.ws[(int64_t)blockIdx.y * a.N + c + i] = dg[i];
+}
+
+// dgamma[j] = sum of `parts` rows of the workspace: 64 columns a workgroup, wavefront w takes rows w, w + 16, ...
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ ws, int parts, int N, float* __restrict__ out)
+{
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < N) {
+#pragma unroll 4
+        for (int r = wave; r < parts; r += 16) s += ws[(int64_t)r * N + c];
+    }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < N) {
+#pragma unroll
+        for (int w = 1; w < 16; w++) s += lds[w][lane];
+        out[c] = s;
+    }
+}
+
+// rows a workgroup of the gradient takes at a time (in wavefronts a row times rows: 16 in all)
+inline int grad_rows(int N) { return N <= 1024 ? 16 : N <= 4096 ? 4 : N <= 8192 ? 2 : 1; }
+
+template <typename T, int W, int P>
+int launch_norm_grad(const NormGradArgs& a, int parts, hipStream_t stream)
+{
+    constexpr int R = 16 / W;
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, P, R>), dim3((unsigned)parts), dim3(1024), (W * R + 512 * W) * sizeof(float), stream, a);
+    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+}
+template <typename T>
+int norm_grad_of_type(const NormGradArgs& a, hipStream_t stream)
+{
+    const int parts = ops_norm_grad_parts(a.M, a.N);
+    int rc = GEMM_F16_OK;
+    if (a.M > 0) {
+        if (a.N <= 512) rc = launch_norm_grad<T, 1, 1>(a, parts, stream);
+        else if (a.N <= 1024) rc = launch_norm_grad<T, 1, 2>(a, parts, stream);
+        else if (a.N <= 2048) rc = launch_norm_grad<T, 4, 1>(a, parts, stream);
+        else if (a.N <= 4096) rc = launch_norm_grad<T, 4, 2>(a, parts, stream);
+        else if (a.N <= 8192) rc = launch_norm_grad<T, 8, 2>(a, parts, stream);
+        else if (a.N <= 16384) rc = launch_norm_grad<T, 16, 2>(a, parts, stream);
+        else {
+            if (a.dgamma) hipLaunchKernelGGL(rms_norm_dgamma_long_kernel<T>, dim3((unsigned)(((int64_t)a.N + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL(rms_norm_grad_long_kernel<T>, dim3((unsigned)a.M), dim3(1024), 0, stream, a);
+            rc = hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+        }
+        if (rc != GEMM_F16_OK) return rc;
+    }
+    if (!a.dgamma) return rc;
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)(((int64_t)a.N + 63) / 64)), dim3(1024), 0, stream, a.ws, parts, a.N, a.dgamma);
+    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+}
+
+// ---- quantisation in rows: 16 rows a workgroup, 16 lanes a block of 128; the 16 scales of a block column are stored together --------
+enum { ROW_BLOCKS = 4 };                                 // block columns a workgroup takes
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantArgs a)
+{
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (row >= a.M) return;
+    const T* const x = (const T*)a.X + row * a.ldx;
+#pragma unroll
+    for (int b = 0; b < ROW_BLOCKS; b++) {
+        const int64_t kb = (int64_t)blockIdx.y * ROW_BLOCKS + b, c = 128 * kb + 8 * (threadIdx.x & 15);
+        if (128 * kb >= a.N) break;
+        float y[8] = {};
+        if (c < a.N) {
+            load8(x + c, (int)(a.N - c), y);
+            if constexpr (ACT == GEMM_OPS_ACT_RELU) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) y[i] = y[i] < 0.0f ? 0.0f : y[i];
+            } else if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) {
+                float u[8];
+                load8(x + a.N + c, (int)(a.N - c), u);
+#pragma unroll
+                for (int i = 0; i < 8; i++) y[i] = y[i] / (1.0f + __expf(-y[i])) * u[i];
+            }
+        }
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, magnitude(y[i]));
+        const BlockScale s = block_scale(max16(m));
+        if (c < a.N) store_e4m3(a.Q + row * a.ldq + c, (int)(a.N - c), to_e4m3(y, s.inverse));
+        if ((threadIdx.x & 15) == 0) a.scale[kb * a.ld_scale + row] = s.scale;
+    }
+}
+
+// ---- quantisation in blocks: a workgroup takes 128 x 128, 16 rows at a time, and keeps them in registers -----------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_blocks_kernel(const QuantArgs a)
+{
+    __shared__ uint32_t most[4];
+    const int blocks_n = (int)(((int64_t)a.N + 127) / 128);
+    const int64_t bm = blockIdx.x / blocks_n, bn = blockIdx.x % blocks_n;
+    const int64_t c = 128 * bn + 8 * (threadIdx.x & 15);
+    float y[8][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int p = 0; p < 8; p++) {
+        const int64_t row = 128 * bm + 16 * p + threadIdx.x / 16;
+        if (row < a.M && c < a.N) {
+            load8((const T*)a.X + row * a.ldx + c, (int)(a.N - c), y[p]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[p][i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) m = max(m, magnitude(y[p][i]));
+    }
+    m = max16(m);
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+    __syncthreads();
+    const BlockScale s = block_scale(max(max(most[0], most[1]), max(most[2], most[3])));
+    if (threadIdx.x == 0) a.scale[bm * a.ld_scale + bn] = s.scale;
+#pragma unroll
+    for (int p = 0; p < 8; p++) {
+        const int64_t row = 128 * bm + 16 * p + threadIdx.x / 16;
+        if (row < a.M && c < a.N) store_e4m3(a.Q + row * a.ldq + c, (int)(a.N - c), to_e4m3(y[p], s.inverse));
+    }
+}
+
+template <typename T>
+int quant_rows_of_type(const QuantArgs& a, hipStream_t stream)
+{
+    const int64_t nb = ((int64_t)a.N + 127) / 128, gy = (nb + ROW_BLOCKS - 1) / ROW_BLOCKS;
+    // y takes 65535 workgroups: 33 million columns
+    if (gy > 65535) return GEMM_F16_ERR_SIZE;
+    const dim3 grid((unsigned)(((int64_t)a.M + 15) / 16), (unsigned)gy);
+    switch (a.act) {
+    case GEMM_OPS_ACT_NONE: hipLaunchKernelGGL((quantize_rows_kernel<T, GEMM_OPS_ACT_NONE>), grid, dim3(256), 0, stream, a); break;
+    case GEMM_OPS_ACT_RELU: hipLaunchKernelGGL((quantize_rows_kernel<T, GEMM_OPS_ACT_RELU>), grid, dim3(256), 0, stream, a); break;
+    default: hipLaunchKernelGGL((quantize_rows_kernel<T, GEMM_OPS_ACT_SWIGLU>), grid, dim3(256), 0, stream, a); break;
+    }
+    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+}
+template <typename T>
+int quant_blocks_of_type(const QuantArgs& a, hipStream_t stream)
+{
+    const int64_t tiles = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
+    if (tiles > INT32_MAX) return GEMM_F16_ERR_SIZE;
+    hipLaunchKernelGGL(quantize_blocks_kernel<T>, dim3((unsigned)tiles), dim3(256), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+}
+
+}  // namespace
+
+int ops_norm_grad_parts(int64_t M, int64_t N)
+{
+    const int64_t rows = grad_rows((int)(N < INT32_MAX ? N : INT32_MAX)), g = (M + rows - 1) / rows;
+    return (int)(g < 256 ? g : 256);
+}
+int ops_launch_norm(int type, const NormArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? norm_of_type<half_t>(a, stream) : norm_of_type<bf16_t>(a, stream); }
+int ops_launch_norm_grad(int type, const NormGradArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? norm_grad_of_type<half_t>(a, stream) : norm_grad_of_type<bf16_t>(a, stream); }
+int ops_launch_quant_rows(int type, const QuantArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? quant_rows_of_type<half_t>(a, stream) : quant_rows_of_type<bf16_t>(a, stream); }
+int ops_launch_quant_blocks(int type, const QuantArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? quant_blocks_of_type<half_t>(a, stream) : quant_blocks_of_type<bf16_t>(a, stream); }
