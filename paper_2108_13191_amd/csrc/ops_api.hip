@@ -11,6 +11,24 @@ int64_t blocks128(int64_t n) { return (n + 127) / 128; }
 bool is_16bit(int64_t type) { return type == GEMM_TYPE_F16 || type == GEMM_TYPE_BF16; }
 int type_size(int64_t type) { return type == GEMM_TYPE_F32 ? 4 : 2; }
 
+// What the tiled kernels take: 16-byte aligned operands, whose offsets within a tile fit 32 bits
+bool tiles_take(const OpsGemm& g)
+{
+    const int64_t chunk = g.elem == ELEM_E4M3 ? 16 : 8;
+    return !unaligned(g.A, 16) && !unaligned(g.B, 16) && g.lda % chunk == 0 && g.ldb % chunk == 0 && g.b_stride % chunk == 0 &&
+           g.lda <= (1 << 22) && g.ldb <= (1 << 22) && g.M <= INT32_MAX - 512 && g.N <= INT32_MAX - 512 && g.K <= INT32_MAX - 512;
+}
+
+int launch(const OpsGemm& g)
+{
+    if (!tiles_take(g)) return ops_launch_generic(g);
+    const int64_t tn = (g.N + 255) / 256, tm = g.k_ragged ? (int64_t)g.E * ((g.M + 255) / 256) : (g.M + 255) / 256;
+    const int64_t rows = g.k_ragged ? g.M : g.M / g.E;
+    int block = rows >= 192 && tm * tn >= 192 ? 256 : 128;
+    if (g.elem == ELEM_E4M3 && (block == 128 || g.c_type == ELEM_F32)) block = rows >= 192 && tm * tn >= 96 ? 257 : 128;
+    return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, block) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, block) : ops_launch_tiles_bf16(g, block);
+}
+
 // The e4m3 products.  E < 0: one product, nothing grouped.
 int run_e4m3(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
              const void* A, int64_t lda, const float* sa, int64_t ld_as, const void* B, int64_t ldb, int64_t b_stride,
@@ -32,15 +50,10 @@ int run_e4m3(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
     g.elem = ELEM_E4M3; g.c_type = (int)c_type; g.a_kc = g.b_kc = true;
     g.num_xcd = chip().xcds;
     g.stream = (hipStream_t)stream;
-    return ops_launch_generic(g);
+    return launch(g);
 }
 
-// The 16-bit products grouped by expert, with the checks they share done on what the caller calls its matrices.
-int run_grouped(const OpsGemm& g)
-{
-    return ops_launch_generic(g);
-}
-
+// What the 16-bit products grouped by expert share: checks and parameters
 int check_grouped(int64_t T, int64_t N, int64_t K, int64_t E, int64_t type, int64_t out_type)
 {
     if (bad_size(T) || bad_size(N) || bad_size(K) || E < 0 || E > 65535) return GEMM_F16_ERR_SIZE;
@@ -150,7 +163,7 @@ int gemm_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offs
     OpsGemm g = grouped_params(T, N, K, E, offsets, type, c_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)C; g.ldc = ldc;
     g.a_kc = true; g.b_kc = false;
-    return run_grouped(g);
+    return launch(g);
 }
 
 int gemm_grouped_grad_a(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, const void* dC, int64_t lddc,
@@ -166,7 +179,7 @@ int gemm_grouped_grad_a(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
     OpsGemm g = grouped_params(T, K, N, E, offsets, type, a_type, stream);
     g.A = (const char*)dC; g.lda = lddc; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)dA; g.ldc = ldda;
     g.a_kc = true; g.b_kc = true;
-    return run_grouped(g);
+    return launch(g);
 }
 
 int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, const void* A, int64_t lda,
@@ -182,7 +195,7 @@ int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
     OpsGemm g = grouped_params(K, N, T, E, offsets, type, b_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)dC; g.ldb = lddc; g.C = (char*)dB; g.ldc = lddb; g.c_stride = db_stride;
     g.a_kc = false; g.b_kc = false; g.k_ragged = true;
-    return run_grouped(g);
+    return launch(g);
 }
 
 }  // extern "C"

@@ -33,6 +33,11 @@ struct OpsGemm {
 // ops_generic.hip: any alignment, any size
 int ops_launch_generic(const OpsGemm& g);
 
+// ops_tile_*.hip: 16-byte aligned operands with pitches up to 2^22 elements; block: 256 or 128, the tile's rows and columns
+int ops_launch_tiles_e4m3(const OpsGemm& g, int block);
+int ops_launch_tiles_f16(const OpsGemm& g, int block);
+int ops_launch_tiles_bf16(const OpsGemm& g, int block);
+
 // ops_norm.hip
 struct NormArgs {
     int M, N;
