@@ -25,7 +25,7 @@ FASTCALL = os.path.join(HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFI
 FASTCALL_CC = ("gcc", "cc", "amdclang", "clang")         # the first one that is there (hipcc would link the HIP runtime into it)
 LADDER_LIB = os.path.join(HERE, "libgemm_f16_ladder.so")
 SOURCES = ["gemm_api.hip", "gemm_generic.hip", "gemm_unaligned.hip", "gemm_unaligned_pp.hip", "gemm_kslice.hip", "gemm_tiled.hip", "gemm_pingpong.hip", "gemm_pp128.hip", "gemm_w4a.hip", "gemm_w4a128.hip", "gemm_splitk_f16.hip",
-           "ops_api.hip", "ops_generic.hip", "ops_norm.hip", "ops_tile_e4m3.hip", "ops_tile_f16.hip", "ops_tile_bf16.hip"]
+           "ops_api.hip", "ops_generic.hip", "ops_norm.hip", "ops_tile_e4m3.hip", "ops_tile_f16.hip", "ops_tile_bf16.hip", "ops_skinny_e4m3.hip"]
 PLAIN_SOURCES = {s for s in SOURCES if s.startswith("ops_")}           # the same in both libraries
 LADDER_SOURCES = ["ladder/gemm_w4.hip", "ladder/gemm_overlap.hip", "ladder/gemm_interleaved.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

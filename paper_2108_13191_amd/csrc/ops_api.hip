@@ -19,14 +19,49 @@ bool tiles_take(const OpsGemm& g)
            g.lda <= (1 << 22) && g.ldb <= (1 << 22) && g.M <= INT32_MAX - 512 && g.N <= INT32_MAX - 512 && g.K <= INT32_MAX - 512;
 }
 
+// Tiles of bm x bn results that a launch is expected to have (how the rows are dealt is known on the device only): in groups with fewer
+// rows than a tile one each, in larger ones half a tile more than their rows fill.
+double expected_tiles(const OpsGemm& g, int bm, int bn)
+{
+    const double tn = (g.N + bn - 1) / bn;
+    if (g.k_ragged) return (double)g.E * ((g.M + bm - 1) / bm) * tn;
+    if (!g.offsets) return ((g.M + bm - 1) / bm) * tn;
+    const double groups = g.E < g.M ? g.E : g.M, rows = g.M / groups;
+    return (g.M / (double)bm + groups * (rows < bm ? 1.0 - 0.5 * rows / bm : 0.5)) * tn;
+}
+
+// The choice of kernel; us measured for the one taken | the other, groups as a random router deals them.
 int launch(const OpsGemm& g)
 {
     if (!tiles_take(g)) return ops_launch_generic(g);
-    const int64_t tn = (g.N + 255) / 256, tm = g.k_ragged ? (int64_t)g.E * ((g.M + 255) / 256) : (g.M + 255) / 256;
-    const int64_t rows = g.k_ragged ? g.M : g.M / g.E;
-    int block = rows >= 192 && tm * tn >= 192 ? 256 : 128;
-    if (g.elem == ELEM_E4M3 && (block == 128 || g.c_type == ELEM_F32)) block = rows >= 192 && tm * tn >= 96 ? 257 : 128;
-    return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, block) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, block) : ops_launch_tiles_bf16(g, block);
+    const int cus = chip().cus;
+    const double rows = (double)g.M / g.E;                                  // of a group
+    if (g.k_ragged) {
+        // gradient of B, 256 x 256 | 128 x 128: (16384 rows, 2048 x 1024, 32 experts) 1024 tiles 132 | 151, (16384, 4096 x 2048, 8) 1024 tiles
+        // 254 | 321, (16384, 2304 x 768, 8) 216 tiles 97 | 79, (2048, 1024 x 1024, 8) 128 tiles 23 | 15
+        const OpsTile t = expected_tiles(g, 256, 256) >= 2.0 * cus ? TILE_256 : TILE_128;
+        return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, t) : ops_launch_tiles_bf16(g, t);
+    }
+    // three quarters of the compute units with a tile of 256 x 256, and groups that fill three quarters of one
+    const bool large = rows >= 192.0 && expected_tiles(g, 256, 256) >= 0.75 * cus;
+    if (g.elem == ELEM_E4M3) {
+        // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
+        // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
+        if ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0)) {
+            const int fm = rows <= 16.0 ? 1 : 2;
+            // the widest tiles that give every compute unit one: (16,8192,8192) 32 columns 13.6, 16 columns 17.1; (16,2048,8192) 13.1, 9.6;
+            // (64,8192,8192) 64 columns 25.8, 32 columns 32; (64,4096,4096) 14.8, 10.4
+            const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
+            return ops_launch_skinny_e4m3(g, fm, nb);
+        }
+        // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 440 us
+        if (large && g.c_type != ELEM_F32) return ops_launch_tiles_e4m3(g, TILE_256);
+        // 256 x 128 | 128 x 128: 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100, 2048^3 (128 tiles) 32 | 22, (512,8192,8192) (128 tiles) 106 | 70
+        return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 256, 128) >= 0.75 * cus ? TILE_256x128 : TILE_128);
+    }
+    // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
+    const OpsTile t = large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128;
+    return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, t) : ops_launch_tiles_bf16(g, t);
 }
 
 // The e4m3 products.  E < 0: one product, nothing grouped.

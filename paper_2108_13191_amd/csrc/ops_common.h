@@ -33,10 +33,14 @@ struct OpsGemm {
 // ops_generic.hip: any alignment, any size
 int ops_launch_generic(const OpsGemm& g);
 
-// ops_tile_*.hip: 16-byte aligned operands with pitches up to 2^22 elements; block: 256 or 128, the tile's rows and columns
-int ops_launch_tiles_e4m3(const OpsGemm& g, int block);
-int ops_launch_tiles_f16(const OpsGemm& g, int block);
-int ops_launch_tiles_bf16(const OpsGemm& g, int block);
+// ops_tile_*.hip: 16-byte aligned operands with pitches up to 2^22 elements (each takes the tiles that the choice in ops_api.hip has for it)
+enum OpsTile { TILE_256, TILE_256x128, TILE_128x256, TILE_128 };
+int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile);
+int ops_launch_tiles_f16(const OpsGemm& g, OpsTile tile);
+int ops_launch_tiles_bf16(const OpsGemm& g, OpsTile tile);
+
+// ops_skinny_e4m3.hip: few rows; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
+int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb);
 
 // ops_norm.hip
 struct NormArgs {

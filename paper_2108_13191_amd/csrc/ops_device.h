@@ -67,36 +67,44 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int e, int li
     hi = min(max(offsets[e + 1], lo), limit);
 }
 
-// Tiles of `bm` rows over all groups in order: the group, first row and end of tile t, by one wavefront whose lanes look at 64
-// groups at a time.  tiles_before(…) at the end of the groups is the number of tiles.
-struct GroupTile { int e, row0, end, first_tile, tiles; };      // tiles `first_tile` .. + tiles - 1 are group e's
-__device__ __forceinline__ int group_tile_scan(const int32_t* offsets, int E, int limit, int bm, int want, GroupTile& out)
+// 64 groups at a time, a lane of a wavefront each: their rows lo .. hi, the tiles of BM rows that they need, and those of all
+// lanes up to and with this one.
+struct GroupScan {
+    int lo, hi, n, incl;
+    __device__ int total() const { return __builtin_amdgcn_readlane(incl, 63); }
+    __device__ int group_of(int tile) const { return __builtin_ctzll(__ballot(incl > tile) | (1ull << 63)); }    // whose tile it is
+    __device__ int tiles_of(int at) const { return max(1, __builtin_amdgcn_readlane(n, at)); }
+    __device__ int before(int at) const { return __builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(n, at); }
+    __device__ int lo_of(int at) const { return __builtin_amdgcn_readlane(lo, at); }
+    __device__ int hi_of(int at) const { return __builtin_amdgcn_readlane(hi, at); }
+};
+template <int BM>
+__device__ __forceinline__ GroupScan scan_groups(const int32_t* offsets, int e0, int E, int limit)
 {
     const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-        int lo = 0, hi = 0;
-        if (e0 + lane < E) group_rows(offsets, e0 + lane, limit, lo, hi);
-        const int n = (int)(((int64_t)(hi - lo) + bm - 1) / bm);
-        int incl = n;
+    GroupScan s = {0, 0, 0, 0};
+    if (e0 + lane < E) group_rows(offsets, e0 + lane, limit, s.lo, s.hi);
+    s.incl = s.n = (int)(((uint32_t)(s.hi - s.lo) + BM - 1) / BM);
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int v = __shfl_up(incl, d);
-            if (lane >= d) incl += v;
-        }
-        const int total = __builtin_amdgcn_readlane(incl, 63);
-        if (want >= base && want - base < total) {
-            const uint64_t above = __ballot(incl > want - base);
-            const int l = __builtin_ctzll(above);
-            out.e = e0 + l;
-            out.tiles = __builtin_amdgcn_readlane(n, l);
-            out.first_tile = base + __builtin_amdgcn_readlane(incl, l) - out.tiles;
-            out.row0 = __builtin_amdgcn_readlane(lo, l) + (want - out.first_tile) * bm;
-            out.end = __builtin_amdgcn_readlane(hi, l);
-        }
-        base += total;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(s.incl, d);
+        if (lane >= d) s.incl += v;
     }
-    return base;
+    return s;
+}
+// The group of the `rank`-th most rows (of equal ones the first first); beyond 64 groups within each 64.
+__device__ __forceinline__ int group_by_size(const int32_t* offsets, int E, int limit, int rank)
+{
+    const int lane = threadIdx.x & 63, e0 = rank & ~63;
+    int lo = 0, hi = 0, before = 0;
+    const bool there = e0 + lane < E;
+    if (there) group_rows(offsets, e0 + lane, limit, lo, hi);
+    const int rows = there ? hi - lo : -1;
+    for (int i = 0; i < min(64, E - e0); i++) {
+        const int other = __builtin_amdgcn_readlane(rows, i);
+        before += other > rows || (other == rows && i < lane);
+    }
+    return e0 + __builtin_ctzll(__ballot(there && before == (rank & 63)));
 }
 // what a launch needs at most: every group may end in a short tile
 inline int64_t max_group_tiles(int64_t rows, int64_t E, int64_t bm) { return rows / bm + (E < rows ? E : rows); }

@@ -63,9 +63,17 @@ __global__ __launch_bounds__(256) void ops_generic_kernel(const OpsGemm g)
         group_rows(g.offsets, e, g.K, k_first, k_end);
         row0 = (int64_t)tile_m * GT; row_end = g.M;
     } else if (g.offsets) {
-        GroupTile t;
-        if (tile_m >= group_tile_scan(g.offsets, g.E, g.M, GT, tile_m, t)) return;
-        e = t.e; row0 = t.row0; row_end = t.end;
+        // the tile_m-th tile of all groups in order
+        int want = tile_m, e0 = 0;
+        GroupScan s = scan_groups<GT>(g.offsets, 0, g.E, g.M);
+        while (want >= s.total()) {
+            want -= s.total();
+            e0 += 64;
+            if (e0 >= g.E) return;
+            s = scan_groups<GT>(g.offsets, e0, g.E, g.M);
+        }
+        const int at = s.group_of(want);
+        e = e0 + at; row0 = s.lo_of(at) + (int64_t)(want - s.before(at)) * GT; row_end = s.hi_of(at);
     } else {
         row0 = (int64_t)tile_m * GT; row_end = g.M;
     }

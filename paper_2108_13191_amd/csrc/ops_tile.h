@@ -15,7 +15,8 @@
 //      phase 4k+2   reads A rows 2nd half
 //      phase 4k+3   multiplies; copies A 2nd half, B (k+2)      (Y: A 2nd half)
 // Each copy overwrites what every reader read in an earlier phase, so two stages are enough: 128 KB of LDS for 256 x 256 and room
-// for scales.  X waits for k+1 at the end of its last multiplying phase of k (the copies issued in this k step may be on their way),
+// for scales (S stages, copies S k steps ahead, for smaller tiles).  X waits for k+1 at the end of its last multiplying phase of k (the copies for
+// later k steps may be on their way),
 // Y, whose B rows X reads a phase earlier than Y itself, at the end of both.
 //
 // e4m3: each MFMA starts from zero and its 4 results are added to the accumulators times a_scale * b_scale, in f32.  With the B
@@ -80,8 +81,8 @@ template <int ELEM> __device__ __forceinline__ floatx4 mfma_step(const Frag& a, 
     }
 }
 
-// Where a workgroup's tile lies.
-struct TileAt { int e, row0, row_end, k0, k_end, n0; };
+// Where a workgroup's tile lies (uniform); valid: whether there is one for this workgroup.
+struct TileAt { int e, row0, row_end, k0, k_end, n0; bool valid; };
 
 // The l-th of tm x tn tiles, `group` rows of tiles at a time
 __device__ __forceinline__ void in_order(int l, int tm, int tn, int group, int& m, int& n)
@@ -93,34 +94,43 @@ __device__ __forceinline__ void in_order(int l, int tm, int tn, int group, int& 
 }
 
 template <int BM, int BN>
-__device__ __forceinline__ bool find_tile(const OpsGemm& g, TileAt& t)
+__device__ __forceinline__ TileAt find_tile(const OpsGemm& g)
 {
     const int tn = (g.N + BN - 1) / BN, pid = blockIdx.x;
-    int m, n;
+    int e = 0, row0 = 0, row_end = g.M, k0 = 0, k_end = g.K, m = 0, n = 0;
+    bool valid = true;
     if (g.k_ragged) {
-        const int tm = (g.M + BM - 1) / BM, l = xcd_slice(g.E * tm * tn, g.num_xcd, pid);
-        t.e = l / (tm * tn);
-        in_order(l - t.e * tm * tn, tm, tn, 8, m, n);
-        group_rows(g.offsets, t.e, g.K, t.k0, t.k_end);
-        t.row0 = m * BM; t.row_end = g.M;
+        // experts one after another, the one with the most rows first, each dealt to all XCDs: (16384 rows, 4096 x 2048, 8 uneven experts)
+        // 425 us with an eighth of all tiles, one expert's, on each XCD
+        const int tm = (g.M + BM - 1) / BM, per = tm * tn;
+        e = group_by_size(g.offsets, g.E, g.K, pid / per);
+        in_order(xcd_slice(per, g.num_xcd, pid % per), tm, tn, 8, m, n);
+        group_rows(g.offsets, e, g.K, k0, k_end);
     } else if (g.offsets) {
-        GroupTile q = {};
-        const int total = group_tile_scan(g.offsets, g.E, g.M, BM, -1, q) * tn;
-        if (pid >= total) return false;
-        const int l = xcd_slice(total, g.num_xcd, pid);
-        group_tile_scan(g.offsets, g.E, g.M, BM, l / tn, q);
-        if (q.tiles <= 0) return false;                           // offsets that overlap beyond what an int counts
-        const int at = l / tn - q.first_tile;                     // row0 is that of tile l / tn
-        in_order(l - q.first_tile * tn, q.tiles, tn, 8, m, n);
-        t.e = q.e; t.row0 = q.row0 + (m - at) * BM; t.row_end = q.end;
-        t.k0 = 0; t.k_end = g.K;
+        GroupScan s = scan_groups<BM>(g.offsets, 0, g.E, g.M);
+        int total = s.total();
+        for (int e0 = 64; e0 < g.E; e0 += 64) total += scan_groups<BM>(g.offsets, e0, g.E, g.M).total();
+        valid = pid < total * tn;
+        const int l = valid ? xcd_slice(total * tn, g.num_xcd, pid) : 0;
+        int want = l / tn, e0 = 0;                                // the want-th tile of rows is one of the group's
+        while (valid && want >= s.total()) {
+            want -= s.total();
+            e0 += 64;
+            valid = e0 < g.E;                                     // (false only for offsets that overlap beyond what an int counts)
+            if (valid) s = scan_groups<BM>(g.offsets, e0, g.E, g.M);
+        }
+        const int at = valid ? s.group_of(want) : 0;
+        e = e0 + at;
+        const int tiles = valid ? s.tiles_of(at) : 1;
+        in_order(l - (l / tn - (want - s.before(at))) * tn, tiles, tn, 8, m, n);
+        row0 = s.lo_of(at);
+        row_end = s.hi_of(at);
     } else {
         const int tm = (g.M + BM - 1) / BM;
         in_order(xcd_slice(tm * tn, g.num_xcd, pid), tm, tn, 8, m, n);
-        t.e = 0; t.row0 = m * BM; t.row_end = g.M; t.k0 = 0; t.k_end = g.K;
     }
-    t.n0 = n * BN;
-    return true;
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    return {uniform(e), uniform(row0 + m * BM), uniform(row_end), uniform(k0), uniform(k_end), uniform(n * BN), valid};
 }
 
 // Where chunk `chunk` of k row `krow` lies in its row of CPR chunks.  Rows of 256 and 512 bytes all begin at bank 0, so the 4 k rows of a
@@ -133,15 +143,14 @@ template <int CPR> __device__ __forceinline__ int mc_chunk(int chunk, int krow)
 }
 
 constexpr int STEP = 128;                                  // bytes of a k row a step; 64 k rows a step in the other layout
-template <int BM, int BN, bool SCALED> constexpr int stage_bytes() { return (BM + BN) * STEP; }
-template <int BM, int BN, bool SCALED> constexpr int lds_bytes()
+template <int BM, int BN, int S, bool SCALED> constexpr int lds_bytes()
 {
-    const int stages = 2 * stage_bytes<BM, BN, SCALED>() + (SCALED ? 2 * BM * 4 : 0), out = 8 * 32 * (BN + 16);
+    const int stages = S * ((BM + BN) * STEP + (SCALED ? BM * 4 : 0)), out = 8 * 32 * (BN + 16);
     return stages > out ? stages : out;
 }
 
 // EXACT: e4m3 values are widened to f16 and multiplied by f16 MFMAs
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, bool EXACT, typename CT>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, typename CT>
 __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
 {
     constexpr bool SCALED = ELEM == ELEM_E4M3;
@@ -151,19 +160,18 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
     constexpr int A_STAGE = BM * STEP, B_STAGE = BN * STEP, A_HALF = A_STAGE / 2, B_HALF = B_STAGE / 2;
     constexpr int TA = HM / 32, TB = BN / 64;              // copies of 1 KB of a wavefront and k step
     constexpr int NC = TA + TB + (SCALED ? 1 : 0);
-    constexpr uint32_t A0 = 0, B0 = 2 * A_STAGE, S0 = B0 + 2 * B_STAGE;
+    constexpr uint32_t A0 = 0, B0 = S * A_STAGE, S0 = B0 + S * B_STAGE;
+    static_assert(S * NC <= 63, "copies in flight are counted in 6 bits");
     static_assert(TA >= 2 && (AKC || TA == 4 || TA == 2), "copies of a group's rows come in two halves");
 
-    __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<BM, BN, SCALED>()];
+    __shared__ __attribute__((aligned(1024))) char smem[lds_bytes<BM, BN, S, SCALED>()];
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wave >> 2, wn = wave & 3;
 
-    TileAt t;
-    if (!find_tile<BM, BN>(g, t)) return;
-    t.e = __builtin_amdgcn_readfirstlane(t.e); t.row0 = __builtin_amdgcn_readfirstlane(t.row0); t.row_end = __builtin_amdgcn_readfirstlane(t.row_end);
-    t.k0 = __builtin_amdgcn_readfirstlane(t.k0); t.k_end = __builtin_amdgcn_readfirstlane(t.k_end); t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+    const TileAt t = find_tile<BM, BN>(g);
+    if (!t.valid) return;
     const int K = t.k_end - t.k0, k_full = K / KE, KT = (K + KE - 1) / KE;
 
     // ---- copies ---------------------------------------------------------------------------------------------------
@@ -204,13 +212,13 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
     const char* const b_tile = BKC ? b_mat + ((int64_t)t.n0 * g.ldb + t.k0) * ES : b_mat + ((int64_t)t.k0 * g.ldb + t.n0) * ES;
     const int64_t a_step = AKC ? STEP : 64 * g.lda * ES, b_step = BKC ? STEP : 64 * g.ldb * ES;
     // scales of A: wavefronts wn and wn + 2 of a group bring in the same 64 rows (the same count of copies for all)
-    const uint32_t s_off = SCALED ? 4u * (uint32_t)min(grp * HM + (HM >= 128 ? 64 * (wn & 1) : 0) + lane, a_cols - 1) : 0u;
+    uint32_t s_off = SCALED ? 4u * (uint32_t)min(grp * HM + (HM >= 128 ? 64 * (wn & 1) : 0) + lane, a_cols - 1) : 0u;
     const float* const s_tile = SCALED ? g.sa + t.row0 : nullptr;
     typedef const __attribute__((address_space(4))) float* const_f32;
     const const_f32 sb = SCALED ? (const_f32)(uintptr_t)(g.sb + (int64_t)t.e * g.sb_stride + (int64_t)((t.n0 + wn * WN) / 128 < (g.N + 127) / 128 ? (t.n0 + wn * WN) / 128 : 0) * g.ld_sb) : nullptr;
 
-    auto a_dst = [&](int s, int i) -> uint32_t { return smem_base + A0 + (s & 1) * A_STAGE + grp * A_HALF + 1024 * (wn + 4 * i); };
-    auto b_dst = [&](int s, int i) -> uint32_t { return smem_base + B0 + (s & 1) * B_STAGE + grp * B_HALF + 1024 * (wn + 4 * i); };
+    auto a_dst = [&](int st, int i) -> uint32_t { return smem_base + A0 + st * A_STAGE + grp * A_HALF + 1024 * (wn + 4 * i); };
+    auto b_dst = [&](int st, int i) -> uint32_t { return smem_base + B0 + st * B_STAGE + grp * B_HALF + 1024 * (wn + 4 * i); };
     // a chunk of the last, short k step goes through registers with zeros behind the end of the sum
     auto tail_chunk = [&](const char* src, int left_bytes) -> uintx4 {       // left_bytes: of the chunk within the sum
         uintx4 v = {0u, 0u, 0u, 0u};
@@ -225,28 +233,29 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         return v;
     };
     auto put = [&](uint32_t dst, uintx4 v) { *(__attribute__((address_space(3))) uintx4*)(uintptr_t)(dst + 16 * lane) = v; };
-    auto copy_a = [&](int s, int i, auto whole) {
-        if constexpr (decltype(whole)::value) { async_copy16(a_tile + s * a_step, a_off[i], a_dst(s, i)); }
+    // k step s into stage st
+    auto copy_a = [&](int s, int st, int i, auto whole) {
+        if constexpr (decltype(whole)::value) { async_copy16(a_tile + s * a_step, a_off[i], a_dst(st, i)); }
         else if constexpr (AKC) {
             const int row = grp * HM + 8 * (wn + 4 * i) + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-            put(a_dst(s, i), tail_chunk(a_tile + s * a_step + a_off[i], (K - s * KE) * ES - 16 * chunk));
+            put(a_dst(st, i), tail_chunk(a_tile + s * a_step + a_off[i], (K - s * KE) * ES - 16 * chunk));
         } else {
             const int krow = (64 * (wn + 4 * i) + lane) / A_CPR;
-            put(a_dst(s, i), tail_chunk(a_tile + s * a_step + a_off[i], krow < K - s * KE ? 16 : 0));
+            put(a_dst(st, i), tail_chunk(a_tile + s * a_step + a_off[i], krow < K - s * KE ? 16 : 0));
         }
     };
-    auto copy_b = [&](int s, int i, auto whole) {
-        if constexpr (decltype(whole)::value) { async_copy16(b_tile + s * b_step, b_off[i], b_dst(s, i)); }
+    auto copy_b = [&](int s, int st, int i, auto whole) {
+        if constexpr (decltype(whole)::value) { async_copy16(b_tile + s * b_step, b_off[i], b_dst(st, i)); }
         else if constexpr (BKC) {
             const int row = grp * (BN / 2) + 8 * (wn + 4 * i) + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
-            put(b_dst(s, i), tail_chunk(b_tile + s * b_step + b_off[i], (K - s * KE) * ES - 16 * chunk));
+            put(b_dst(st, i), tail_chunk(b_tile + s * b_step + b_off[i], (K - s * KE) * ES - 16 * chunk));
         } else {
             const int krow = (64 * (wn + 4 * i) + lane) / B_CPR + 32 * grp;
-            put(b_dst(s, i), tail_chunk(b_tile + s * b_step + b_off[i], krow < K - s * KE ? 16 : 0));
+            put(b_dst(st, i), tail_chunk(b_tile + s * b_step + b_off[i], krow < K - s * KE ? 16 : 0));
         }
     };
-    auto copy_s = [&](int s) {
-        if constexpr (SCALED) copy_dword(s_tile + s * g.ld_sa, s_off, smem_base + S0 + (s & 1) * (BM * 4) + grp * (HM * 4) + (HM >= 128 ? 256 * (wn & 1) : 0));
+    auto copy_s = [&](int s, int st) {
+        if constexpr (SCALED) copy_dword(s_tile + s * g.ld_sa, s_off, smem_base + S0 + st * (BM * 4) + grp * (HM * 4) + (HM >= 128 ? 256 * (wn & 1) : 0));
     };
     typedef std::true_type Whole;
     typedef std::false_type Tail;
@@ -260,21 +269,21 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
     if (KT > 0) {
         auto issue = [&](int s) {
             if (s >= KT) return;
-            copy_s(s);
+            copy_s(s, s);
             if (s < k_full) {
 #pragma unroll
-                for (int i = 0; i < TA; i++) copy_a(s, i, Whole{});
+                for (int i = 0; i < TA; i++) copy_a(s, s, i, Whole{});
 #pragma unroll
-                for (int i = 0; i < TB; i++) copy_b(s, i, Whole{});
+                for (int i = 0; i < TB; i++) copy_b(s, s, i, Whole{});
             } else {
 #pragma unroll
-                for (int i = 0; i < TA; i++) copy_a(s, i, Tail{});
+                for (int i = 0; i < TA; i++) copy_a(s, s, i, Tail{});
 #pragma unroll
-                for (int i = 0; i < TB; i++) copy_b(s, i, Tail{});
+                for (int i = 0; i < TB; i++) copy_b(s, s, i, Tail{});
             }
         };
-        issue(0);
-        issue(1);
+#pragma unroll
+        for (int s = 0; s < S; s++) issue(s);
 
         // ---- fragment addresses -----------------------------------------------------------------------------------
         const int l16 = lane & 15, q = lane >> 4;
@@ -295,7 +304,7 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
 #pragma unroll
             for (int n = 0; n < FN; n++) { const int col = wn * WN + 16 * n + 4 * (l16 & 3); b_rd[n] = smem_base + B0 + krow * (BN * 2) + 16 * mc_chunk<B_CPR>(col >> 3, krow) + 2 * (col & 7); }
         }
-        const uint32_t s_rd = smem_base + S0 + (grp * HM + l16) * 4;
+        uint32_t s_rd = smem_base + S0 + (grp * HM + l16) * 4;
 
         Frag fa[FH], fb[FN];
         Wide wa[EXACT ? FH : 1], wb[EXACT ? FN : 1];
@@ -311,8 +320,8 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
             return f;
         };
         auto read16 = [&](uint32_t at) -> uintx4 { return *(__attribute__((address_space(3))) const uintx4*)(uintptr_t)at; };
-        auto read_phase = [&](int k, int h) {
-            const uint32_t as = (k & 1) * A_STAGE, bs = (k & 1) * B_STAGE;
+        auto read_phase = [&](int k, int st, int h) {
+            const uint32_t as = st * A_STAGE, bs = st * B_STAGE;
             if (h == 0) {
                 if constexpr (BKC) {
                     uint32_t b0 = b_rd[0] + bs, b1 = b_rd[1] + bs;
@@ -337,7 +346,7 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
             if constexpr (SCALED) {
 #pragma unroll
                 for (int m = 0; m < FH; m++)
-                    scale[m] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(s_rd + (k & 1) * (BM * 4) + (h * FH + m) * 64);
+                    scale[m] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(s_rd + st * (BM * 4) + (h * FH + m) * 64);
             }
             if constexpr (EXACT) {
                 if (h == 0) {
@@ -348,9 +357,10 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
                 for (int m = 0; m < FH; m++) wa[m] = widened(fa[m]);
             }
         };
-        // COPY: 0 none, 1 of a whole k step, 2 of the short one
+        // COPY: 1 of a whole k step, 2 of the short one, both into the stage that this k step has been read from; 0 and below: none, this is
+        // the last k step but -COPY
         // GRP: the group, as a constant (both have their own code, without branches in a phase)
-        auto multiply_phase = [&](int k, auto half, auto copy, auto group) {
+        auto multiply_phase = [&](int k, int st, auto half, auto copy, auto group) {
             constexpr int COPY = decltype(copy)::value, h = decltype(half)::value, GRP = decltype(group)::value;
             constexpr int NM = FH * FN;
             if constexpr (SCALED) {
@@ -380,7 +390,7 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
                 } else {
                     acc[h * FH + m][n] = mfma_step<ELEM>(fb[n], fa[m], acc[h * FH + m][n]);
                 }
-                if constexpr (COPY != 0) {
+                if constexpr (COPY > 0) {
                     typedef typename std::conditional<COPY == 1, Whole, Tail>::type W;
                     constexpr int SLOTS = 8;                                  // places of copies among the MFMAs
                     constexpr int EVERY = NM >= SLOTS ? NM / SLOTS : 1, PER = NM >= SLOTS ? 1 : SLOTS / NM;
@@ -391,9 +401,9 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
                         for (int j = 0; j < PER; j++) {
                             const int c = slot * PER + j;                     // 0 .. 7
                             const int na = AKC ? TA / 2 : (h == 0 ? 0 : TA), a_first = AKC ? h * (TA / 2) : 0;
-                            if (c < na) copy_a(k + 2, a_first + c, W{});
-                            else if (c < na + TB && GRP == 1 - h) copy_b(k + 2, c - na, W{});
-                            if (SCALED && h == 1 && c == 7) copy_s(k + 2);
+                            if (c < na) copy_a(k + S, st, a_first + c, W{});
+                            else if (c < na + TB && GRP == 1 - h) copy_b(k + S, st, c - na, W{});
+                            if (SCALED && h == 1 && c == 7) copy_s(k + S, st);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -405,33 +415,53 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
             }
             if constexpr (h == 1 || GRP == 1) {
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (COPY == 1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC) : "memory");
-                else                     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                // copies for later k steps than the next may be on their way
+                if constexpr (COPY == 1)      asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
+                else if constexpr (COPY == 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                else                          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(COPY <= -1 ? NC * (-COPY - 1) : 0) : "memory");
             }
         };
-        auto half_step = [&](int k, auto half, auto copy, auto group) {
+        auto half_step = [&](int k, int st, auto half, auto copy, auto group) {
             constexpr int h = decltype(half)::value, GRP = decltype(group)::value;
-            read_phase(k, h);
+            read_phase(k, st, h);
             __builtin_amdgcn_s_waitcnt(0xC07F);                              // lgkmcnt(0)
             asm volatile("" ::: "memory");
             phase_barrier();
-            multiply_phase(k, half, copy, group);
+            multiply_phase(k, st, half, copy, group);
             // Y began one barrier later and leaves out the last one
-            if (decltype(copy)::value != 0 || GRP == 0 || h == 0 || k + 1 < KT) phase_barrier();
+            if constexpr (decltype(copy)::value != 0 || GRP == 0 || h == 0) phase_barrier();
         };
         auto run_loop = [&](auto group) {
-            auto k_step = [&](int k, auto copy) {
-                half_step(k, std::integral_constant<int, 0>{}, copy, group);
-                half_step(k, std::integral_constant<int, 1>{}, copy, group);
+            int k = 0, st = 0;                                               // the k step and its stage
+            auto k_step = [&](auto copy) {
+                half_step(k, st, std::integral_constant<int, 0>{}, copy, group);
+                half_step(k, st, std::integral_constant<int, 1>{}, copy, group);
+                k++;
+                st = st + 1 == S ? 0 : st + 1;
             };
-            int k = 0;
-            for (; k + 2 < k_full; k++) k_step(k, std::integral_constant<int, 1>{});
-            for (; k + 2 < KT; k++) k_step(k, std::integral_constant<int, 2>{});
-            for (; k < KT; k++) k_step(k, std::integral_constant<int, 0>{});
+            // what the loop uses is in registers before it begins: a spilled offset reloaded behind the loop's head would be
+            // waited for in every k step, and every copy in flight with it
+            auto pin = [](uint32_t& x) { asm volatile("" : "+v"(x)); };
+#pragma unroll
+            for (int i = 0; i < TA; i++) pin(a_off[i]);
+#pragma unroll
+            for (int i = 0; i < TB; i++) pin(b_off[i]);
+#pragma unroll
+            for (uint32_t& x : a_rd) pin(x);
+#pragma unroll
+            for (uint32_t& x : b_rd) pin(x);
+            if constexpr (SCALED) { pin(s_off); pin(s_rd); }
+            while (k + S < k_full) k_step(std::integral_constant<int, 1>{});
+            if (k + S < KT) k_step(std::integral_constant<int, 2>{});
+            auto last = [&](auto left) { if (KT - k == 1 - decltype(left)::value) k_step(left); };     // left = 0: the last one
+            if constexpr (S >= 4) last(std::integral_constant<int, -3>{});
+            if constexpr (S >= 3) last(std::integral_constant<int, -2>{});
+            last(std::integral_constant<int, -1>{});
+            last(std::integral_constant<int, 0>{});
         };
-        // k step 0 has landed, those of k step 1 may be on their way
-        if (1 < k_full) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC) : "memory");
-        else            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // k step 0 has landed, those behind it may be on their way
+        if (S <= k_full) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
+        else             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         phase_barrier();
         if (grp == 0) {
             run_loop(std::integral_constant<int, 0>{});
@@ -485,14 +515,14 @@ inline int64_t tile_grid(const OpsGemm& g)
     return rows > INT32_MAX / tn ? -1 : rows * tn;
 }
 
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, bool EXACT = false>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false>
 int launch_tiles(const OpsGemm& g)
 {
     const int64_t grid = tile_grid<BM, BN>(g);
     if (grid < 0) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, EXACT, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
-    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, EXACT, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
-    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, EXACT, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
+    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 

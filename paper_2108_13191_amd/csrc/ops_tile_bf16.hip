@@ -1,12 +1,19 @@
 // The tiled kernel on bf16 operands: forward (A in k rows, B not), gradient of A (both), gradient of B (neither).
 #include "ops_tile.h"
 
-int ops_launch_tiles_bf16(const OpsGemm& g, int block)
+namespace {
+template <bool AKC, bool BKC>
+int launch_tile(const OpsGemm& g, OpsTile tile)
 {
     using namespace ops_tile;
-    if (g.a_kc) {
-        if (g.b_kc) return block == 256 ? launch_tiles<ELEM_BF16, true, true, 256, 256>(g) : launch_tiles<ELEM_BF16, true, true, 128, 128>(g);
-        return block == 256 ? launch_tiles<ELEM_BF16, true, false, 256, 256>(g) : launch_tiles<ELEM_BF16, true, false, 128, 128>(g);
-    }
-    return block == 256 ? launch_tiles<ELEM_BF16, false, false, 256, 256>(g) : launch_tiles<ELEM_BF16, false, false, 128, 128>(g);
+    if (tile == TILE_256) return launch_tiles<ELEM_BF16, AKC, BKC, 256, 256, 2>(g);
+    if constexpr (AKC && !BKC) { if (tile == TILE_128x256) return launch_tiles<ELEM_BF16, true, false, 128, 256, 3>(g); }
+    return launch_tiles<ELEM_BF16, AKC, BKC, 128, 128, 2>(g);
+}
+}  // namespace
+
+int ops_launch_tiles_bf16(const OpsGemm& g, OpsTile tile)
+{
+    if (g.a_kc) return g.b_kc ? launch_tile<true, true>(g, tile) : launch_tile<true, false>(g, tile);
+    return launch_tile<false, false>(g, tile);
 }

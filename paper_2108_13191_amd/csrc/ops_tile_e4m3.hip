@@ -5,9 +5,9 @@
 // values widened to f16 are exact and their sums f32, at half the matrix rate.
 #include "ops_tile.h"
 
-int ops_launch_tiles_e4m3(const OpsGemm& g, int block)
+int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile)
 {
     using namespace ops_tile;
-    if (block == 256) return launch_tiles<ELEM_E4M3, true, true, 256, 256>(g);
-    return block == 257 ? launch_tiles<ELEM_E4M3, true, true, 256, 128, true>(g) : launch_tiles<ELEM_E4M3, true, true, 128, 128, true>(g);
+    if (tile == TILE_256) return launch_tiles<ELEM_E4M3, true, true, 256, 256, 2>(g);
+    return tile == TILE_256x128 ? launch_tiles<ELEM_E4M3, true, true, 256, 128, 2, true>(g) : launch_tiles<ELEM_E4M3, true, true, 128, 128, 2, true>(g);
 }

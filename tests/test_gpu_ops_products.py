@@ -99,6 +99,7 @@ def test_e4m3_grouped(counts, N, K):
 # 2^-13 of the largest one's exponent of a group cut off.  A product of a group of 8 is then off by at most 2^-13 of the group's largest,
 # a sum by 8 * 2^-13 of its magnitudes at the very most; over many results errors of random sign stay below 2^-15 of their norm.
 LARGE = [(3400, 3700, 300), (4096, 3585, 640), (3333, 4500, 129)]
+MIDDLE = [(1200, 1300, 300), (1025, 1601, 520), (900, 2000, 128)]         # between those and the ones for few rows: 128 x 128 tiles
 
 
 def large_e4m3(M, N, K, c, counts=None, integers=False):
@@ -159,7 +160,18 @@ def test_e4m3_large_product_of_integers(M, N, K, c):
     assert np.array_equal(got, torch.from_numpy(want).float().to({"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[c]).double().numpy())
 
 
-@pytest.mark.parametrize("counts", [[1000, 0, 700, 1300, 33], [257, 256, 1, 2900], [3000]], ids=str)
+@pytest.mark.parametrize("M,N,K", MIDDLE)
+@pytest.mark.parametrize("c", ["f16", "bf16", "f32"])
+def test_e4m3_middle_product(M, N, K, c):
+    """Exact products and f32 sums whatever the result's type."""
+    got, want, mag = large_e4m3(M, N, K, c)
+    inside = np.abs(want) < (65504.0 if c == "f16" else np.inf)
+    assert_within(got[inside], want[inside], result_bound(want, mag, c)[inside], f"e4m3 {(M, N, K)}")
+    got, want, mag = large_e4m3(M, N, K, c, integers=True)
+    assert np.array_equal(got, torch.from_numpy(want).float().to({"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[c]).double().numpy())
+
+
+@pytest.mark.parametrize("counts", [[1000, 0, 700, 1300, 33], [257, 256, 1, 2900], [3000], [100, 90, 0, 64, 129, 128] * 2, [30, 0, 41, 25] * 5], ids=str)
 @pytest.mark.parametrize("c,extra", [("bf16", 0), ("f32", 11)])
 def test_e4m3_large_grouped(counts, c, extra):
     got, want, mag = large_e4m3(sum(counts) + extra, 4100, 390, c, counts, integers=True)
