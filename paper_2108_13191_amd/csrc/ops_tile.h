@@ -267,20 +267,21 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         for (int n = 0; n < FN; n++) acc[m][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
     if (KT > 0) {
+        // k step s into stage s, in the order that the loop issues copies in: Y waits for its B rows, which X reads first, while its
+        // second half of A may still be on its way
+        auto issue_in_order = [&](int s, auto whole) {
+#pragma unroll
+            for (int i = 0; i < (AKC ? TA / 2 : 0); i++) copy_a(s, s, i, whole);
+#pragma unroll
+            for (int i = 0; i < TB; i++) copy_b(s, s, i, whole);
+#pragma unroll
+            for (int i = AKC ? TA / 2 : 0; i < TA; i++) copy_a(s, s, i, whole);
+            copy_s(s, s);
+        };
         auto issue = [&](int s) {
             if (s >= KT) return;
-            copy_s(s, s);
-            if (s < k_full) {
-#pragma unroll
-                for (int i = 0; i < TA; i++) copy_a(s, s, i, Whole{});
-#pragma unroll
-                for (int i = 0; i < TB; i++) copy_b(s, s, i, Whole{});
-            } else {
-#pragma unroll
-                for (int i = 0; i < TA; i++) copy_a(s, s, i, Tail{});
-#pragma unroll
-                for (int i = 0; i < TB; i++) copy_b(s, s, i, Tail{});
-            }
+            if (s < k_full) issue_in_order(s, Whole{});
+            else            issue_in_order(s, Tail{});
         };
 #pragma unroll
         for (int s = 0; s < S; s++) issue(s);

@@ -331,6 +331,47 @@ def test_grouped_gradients_are_those_of_the_forward_product():
         assert (forward(a, up) - forward(a, down)) / 2 == gb[e, k, n]
 
 
+@pytest.mark.parametrize("counts,N,K,type", [([257, 256, 1, 2900], 392, 4200, "bf16"), ([3000, 1000], 3000, 200, "f16"), ([90] * 40, 1000, 640, "f16")], ids=str)
+def test_grouped_repeats_to_the_bit(counts, N, K, type):
+    """Forty launches of each product in a row, on integers (every order of sums exact): a copy into LDS that is read before it has
+    arrived would show in some of them."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    T, E, dt = sum(counts), len(counts), {"f16": torch.float16, "bf16": torch.bfloat16}[type]
+    A, D, B = (torch.randint(-2, 3, s, device="cuda", generator=g).to(dt) for s in ((T, K), (T, N), (E, K, N)))
+    out = [[torch.zeros(s, device="cuda") for s in ((T, N), (T, K), (E, K, N))] for _ in range(2)]
+    off = offsets_of(counts).tolist()
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        a, d, b = A[r].float(), D[r].float(), B[e].float()
+        out[1][0][r], out[1][1][r], out[1][2][e] = a @ b, d @ b.t().contiguous(), a.t().contiguous() @ d
+    dev, s = torch.tensor(off, dtype=torch.int32, device="cuda"), stream()
+    C, dA, dB = out[0]
+    for i in range(40):
+        for t in out[0]:
+            t.zero_()
+        binding.check(binding.gemm_grouped(T, N, K, E, dev, TYPE[type], A, K, B, N, K * N, C, N, TYPE["f32"], s))
+        binding.check(binding.gemm_grouped_grad_a(T, N, K, E, dev, TYPE[type], D, N, B, N, K * N, dA, K, TYPE["f32"], s))
+        binding.check(binding.gemm_grouped_grad_b(T, N, K, E, dev, TYPE[type], A, K, D, N, dB, N, K * N, TYPE["f32"], s))
+        for name, got, want in zip(("C", "dA", "dB"), out[0], out[1]):
+            assert torch.equal(got, want), f"{name} in launch {i}"
+
+
+@pytest.mark.parametrize("M,N,K,c", [(4096, 3585, 640, "bf16"), (4096, 3585, 640, "f32"), (1200, 1300, 2000, "f32"), (24, 8192, 4096, "f32")])
+def test_e4m3_repeats_to_the_bit(M, N, K, c):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    a, b = (torch.randint(-4, 5, s, device="cuda", generator=g).float().to(torch.float8_e4m3fn) for s in ((M, K), (N, K)))
+    ld = up16(K)
+    A, B = torch.zeros(M, ld, dtype=torch.float8_e4m3fn, device="cuda"), torch.zeros(N, ld, dtype=torch.float8_e4m3fn, device="cuda")
+    A[:, :K], B[:, :K] = a, b
+    sa, sb = torch.ones(ceil128(K), M, device="cuda"), torch.ones(ceil128(N), ceil128(K), device="cuda")
+    want = (a.float() @ b.float().t().contiguous()).to({"bf16": torch.bfloat16, "f32": torch.float32}[c])
+    C = torch.zeros_like(want)
+    for i in range(40):
+        C.zero_()
+        binding.check(binding.gemm_e4m3_block(M, N, K, A, ld, sa, M, B, ld, sb, sb.stride(0), C, N, TYPE[c], stream()))
+        assert torch.equal(C, want), f"launch {i}"
+
+
 def test_offsets_out_of_range_and_decreasing_stay_inside():
     """Offsets below 0, above T and decreasing: what is in range is computed, nothing else is touched."""
     T, N, K = 50, 40, 64
