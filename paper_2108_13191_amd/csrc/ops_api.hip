@@ -11,12 +11,15 @@ int64_t blocks128(int64_t n) { return (n + 127) / 128; }
 bool is_16bit(int64_t type) { return type == GEMM_TYPE_F16 || type == GEMM_TYPE_BF16; }
 int type_size(int64_t type) { return type == GEMM_TYPE_F32 ? 4 : 2; }
 
-// What the tiled kernels take: 16-byte aligned operands, whose offsets within a tile fit 32 bits
+// What the tiled kernels take: operands whose offsets within a tile fit 32 bits, and but for one form of the 16-bit ones 16-byte aligned ones
 bool tiles_take(const OpsGemm& g)
 {
+    return g.lda <= (1 << 22) && g.ldb <= (1 << 22) && g.M <= INT32_MAX - 512 && g.N <= INT32_MAX - 512 && g.K <= INT32_MAX - 512;
+}
+bool is_aligned(const OpsGemm& g)
+{
     const int64_t chunk = g.elem == ELEM_E4M3 ? 16 : 8;
-    return !unaligned(g.A, 16) && !unaligned(g.B, 16) && g.lda % chunk == 0 && g.ldb % chunk == 0 && g.b_stride % chunk == 0 &&
-           g.lda <= (1 << 22) && g.ldb <= (1 << 22) && g.M <= INT32_MAX - 512 && g.N <= INT32_MAX - 512 && g.K <= INT32_MAX - 512;
+    return !unaligned(g.A, 16) && !unaligned(g.B, 16) && g.lda % chunk == 0 && g.ldb % chunk == 0 && g.b_stride % chunk == 0;
 }
 
 // Tiles of bm x bn results that a launch is expected to have (how the rows are dealt is known on the device only): in groups with fewer
@@ -34,6 +37,11 @@ double expected_tiles(const OpsGemm& g, int bm, int bn)
 int launch(const OpsGemm& g)
 {
     if (!tiles_take(g)) return ops_launch_generic(g);
+    if (!is_aligned(g)) {
+        // a form that loads 8 elements at any alignment needs rows that have them
+        if (g.elem == ELEM_E4M3 || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8) return ops_launch_generic(g);
+        return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, TILE_128_ANY) : ops_launch_tiles_bf16(g, TILE_128_ANY);
+    }
     const int cus = chip().cus;
     const double rows = (double)g.M / g.E;                                  // of a group
     if (g.k_ragged) {

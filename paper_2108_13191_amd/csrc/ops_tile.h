@@ -150,8 +150,12 @@ template <int BM, int BN, int S, bool SCALED> constexpr int lds_bytes()
 }
 
 // EXACT: e4m3 values are widened to f16 and multiplied by f16 MFMAs
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, typename CT>
-__global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
+// ANY: operands of any alignment, in 16 bits, with rows of 8 elements or more: copies go through registers, a 16-byte load at element alignment and
+// a k step later, where the copy into LDS would be asked for, a write to LDS.  A chunk that would leave its row is loaded as the row's
+// last 8 elements and shifted, so that no load lies in a branch: behind one the compiler waits for every load in flight.
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, bool ANY, typename CT>
+// (128 x 128 tiles: registers for two workgroups a compute unit; widened e4m3 ones spill then, (1024,4096,1023) 22.5 us against 17.3)
+__global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void ops_tile_kernel(const OpsGemm g)
 {
     constexpr bool SCALED = ELEM == ELEM_E4M3;
     constexpr int ES = Elem<ELEM>::size, KE = STEP / ES;   // elements of a k step
@@ -183,6 +187,7 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         return (uint32_t)min(row, limit - 1) * (uint32_t)(ld * ES) + 16u * chunk;
     };
     uint32_t a_off[TA], b_off[TB];
+    int a_shift[TA], b_shift[TB];                          // ANY: elements that a chunk begins before its place
     constexpr int A_CPR = HM / 8, B_CPR = BN / 8;                            // chunks of a k row (other layout)
     const int a_cols = t.row_end - t.row0, b_cols = g.N - t.n0;
 #pragma unroll
@@ -192,7 +197,8 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         } else {
             const int c = 64 * (wn + 4 * i) + lane, krow = c / A_CPR;
             int col = grp * HM + 8 * mc_chunk<A_CPR>(c % A_CPR, krow);
-            if (col >= a_cols) col = 0;
+            if constexpr (ANY) { a_shift[i] = max(0, col + 8 - a_cols); col -= a_shift[i]; }
+            else if (col >= a_cols) col = 0;
             a_off[i] = ((uint32_t)krow * (uint32_t)g.lda + (uint32_t)col) * ES;
         }
     }
@@ -203,7 +209,8 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         } else {
             const int c = 64 * (wn + 4 * i) + lane, krow = c / B_CPR + 32 * grp;
             int col = 8 * mc_chunk<B_CPR>(c % B_CPR, krow);
-            if (col >= b_cols) col = 0;
+            if constexpr (ANY) { b_shift[i] = max(0, col + 8 - b_cols); col -= b_shift[i]; }
+            else if (col >= b_cols) col = 0;
             b_off[i] = ((uint32_t)krow * (uint32_t)g.ldb + (uint32_t)col) * ES;
         }
     }
@@ -233,9 +240,45 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         return v;
     };
     auto put = [&](uint32_t dst, uintx4 v) { *(__attribute__((address_space(3))) uintx4*)(uintptr_t)(dst + 16 * lane) = v; };
+    // ANY: chunk i of k step s; in the short last step its k rows behind the sum are any, its chunks of a k row end with the sum
+    typedef uintx4 uintx4_any __attribute__((aligned(2)));
+    auto fetch = [&](const char* tile, uint32_t off, int64_t step, int64_t ld, int k_at, int s, bool kc, auto whole) -> uintx4 {      // k_at: of the chunk in its k step
+        int64_t back = 0;
+        if constexpr (!decltype(whole)::value)
+            back = kc ? ES * (int64_t)max(0, s * KE + k_at + 8 - K) : (int64_t)max(0, s * KE + k_at + 1 - K) * ld * ES;
+        return *(const uintx4_any*)(tile + s * step + (int64_t)(int32_t)off - back);      // (a chunk may begin before its tile)
+    };
+    auto shifted = [](uintx4 v, int n) -> uintx4 {                           // by n elements towards the first, zeros behind
+        const uint32_t h = (n & 1) ? 16u : 0u;
+        uintx4 w;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t lo = v[i], hi = i < 3 ? v[i < 3 ? i + 1 : 3] : 0u;
+            w[i] = (uint32_t)((((uint64_t)hi << 32) | lo) >> h);
+        }
+        if (n & 2) w = uintx4{w[1], w[2], w[3], 0u};
+        if (n & 4) w = uintx4{w[2], w[3], 0u, 0u};
+        if (n >= 8) w = uintx4{0u, 0u, 0u, 0u};
+        return w;
+    };
+    const bool edge_a = !AKC && t.row0 + BM > t.row_end, edge_b = !BKC && t.n0 + BN > g.N;
+    auto a_k = [&](int i) { if constexpr (AKC) return 8 * ((lane & 7) ^ (((grp * HM + 8 * (wn + 4 * i) + (lane >> 3)) >> 1) & 7)); else return (64 * (wn + 4 * i) + lane) / A_CPR; };
+    auto b_k = [&](int i) { if constexpr (BKC) return 8 * ((lane & 7) ^ (((grp * (BN / 2) + 8 * (wn + 4 * i) + (lane >> 3)) >> 1) & 7)); else return (64 * (wn + 4 * i) + lane) / B_CPR + 32 * grp; };
+    uintx4 held_a[ANY ? TA : 1], held_b[ANY ? TB : 1];                       // the chunks of the k step to be written next
+    auto fetch_a = [&](int s, int i, auto whole) { held_a[i] = fetch(a_tile, a_off[i], a_step, g.lda, a_k(i), s, AKC, whole); };
+    auto fetch_b = [&](int s, int i, auto whole) { held_b[i] = fetch(b_tile, b_off[i], b_step, g.ldb, b_k(i), s, BKC, whole); };
+    auto finished = [&](uintx4 v, int shift, bool edge, int k_at, int s, bool kc, auto whole) -> uintx4 {
+        if (edge) v = shifted(v, shift);
+        if (!decltype(whole)::value && s >= k_full) {                        // the short step
+            if (kc) v = shifted(v, max(0, s * KE + k_at + 8 - K));
+            else if (s * KE + k_at >= K) v = uintx4{0u, 0u, 0u, 0u};
+        }
+        return v;
+    };
     // k step s into stage st
     auto copy_a = [&](int s, int st, int i, auto whole) {
-        if constexpr (decltype(whole)::value) { async_copy16(a_tile + s * a_step, a_off[i], a_dst(st, i)); }
+        if constexpr (ANY) { put(a_dst(st, i), finished(held_a[i], AKC ? 0 : a_shift[i], edge_a, a_k(i), s, AKC, whole)); if (whole || s + 1 < KT) fetch_a(s + 1, i, whole); }
+        else if constexpr (decltype(whole)::value) { async_copy16(a_tile + s * a_step, a_off[i], a_dst(st, i)); }
         else if constexpr (AKC) {
             const int row = grp * HM + 8 * (wn + 4 * i) + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
             put(a_dst(st, i), tail_chunk(a_tile + s * a_step + a_off[i], (K - s * KE) * ES - 16 * chunk));
@@ -245,7 +288,8 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         }
     };
     auto copy_b = [&](int s, int st, int i, auto whole) {
-        if constexpr (decltype(whole)::value) { async_copy16(b_tile + s * b_step, b_off[i], b_dst(st, i)); }
+        if constexpr (ANY) { put(b_dst(st, i), finished(held_b[i], BKC ? 0 : b_shift[i], edge_b, b_k(i), s, BKC, whole)); if (whole || s + 1 < KT) fetch_b(s + 1, i, whole); }
+        else if constexpr (decltype(whole)::value) { async_copy16(b_tile + s * b_step, b_off[i], b_dst(st, i)); }
         else if constexpr (BKC) {
             const int row = grp * (BN / 2) + 8 * (wn + 4 * i) + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
             put(b_dst(st, i), tail_chunk(b_tile + s * b_step + b_off[i], (K - s * KE) * ES - 16 * chunk));
@@ -280,9 +324,15 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
         };
         auto issue = [&](int s) {
             if (s >= KT) return;
-            if (s < k_full) issue_in_order(s, Whole{});
-            else            issue_in_order(s, Tail{});
+            if (!ANY && s < k_full) issue_in_order(s, Whole{});
+            else                    issue_in_order(s, Tail{});
         };
+        if constexpr (ANY) {
+#pragma unroll
+            for (int i = 0; i < TA; i++) fetch_a(0, i, Tail{});
+#pragma unroll
+            for (int i = 0; i < TB; i++) fetch_b(0, i, Tail{});
+        }
 #pragma unroll
         for (int s = 0; s < S; s++) issue(s);
 
@@ -417,7 +467,8 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
             if constexpr (h == 1 || GRP == 1) {
                 __builtin_amdgcn_sched_barrier(0);
                 // copies for later k steps than the next may be on their way
-                if constexpr (COPY == 1)      asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
+                if constexpr (ANY)           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                else if constexpr (COPY == 1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
                 else if constexpr (COPY == 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 else                          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(COPY <= -1 ? NC * (-COPY - 1) : 0) : "memory");
             }
@@ -452,8 +503,10 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
 #pragma unroll
             for (uint32_t& x : b_rd) pin(x);
             if constexpr (SCALED) { pin(s_off); pin(s_rd); }
-            while (k + S < k_full) k_step(std::integral_constant<int, 1>{});
-            if (k + S < KT) k_step(std::integral_constant<int, 2>{});
+            // (ANY: a k step also loads the one behind the one that it writes)
+            while (k + S + (ANY ? 1 : 0) < k_full) k_step(std::integral_constant<int, 1>{});
+            if constexpr (ANY) { while (k + S < KT) k_step(std::integral_constant<int, 2>{}); }
+            else if (k + S < KT) k_step(std::integral_constant<int, 2>{});
             auto last = [&](auto left) { if (KT - k == 1 - decltype(left)::value) k_step(left); };     // left = 0: the last one
             if constexpr (S >= 4) last(std::integral_constant<int, -3>{});
             if constexpr (S >= 3) last(std::integral_constant<int, -2>{});
@@ -461,8 +514,9 @@ __global__ __launch_bounds__(512) void ops_tile_kernel(const OpsGemm g)
             last(std::integral_constant<int, 0>{});
         };
         // k step 0 has landed, those behind it may be on their way
-        if (S <= k_full) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
-        else             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (ANY)              asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        else if (S <= k_full) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NC * (S - 1)) : "memory");
+        else                  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         phase_barrier();
         if (grp == 0) {
             run_loop(std::integral_constant<int, 0>{});
@@ -516,14 +570,14 @@ inline int64_t tile_grid(const OpsGemm& g)
     return rows > INT32_MAX / tn ? -1 : rows * tn;
 }
 
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false, bool ANY = false>
 int launch_tiles(const OpsGemm& g)
 {
     const int64_t grid = tile_grid<BM, BN>(g);
     if (grid < 0) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
-    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
-    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
+    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 
