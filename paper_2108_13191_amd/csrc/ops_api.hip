@@ -1,6 +1,7 @@
 // The C ABI of include/gemm_ops.h: checks of arguments and the choice of kernel.
 #include "ops_common.h"
 #include "../../include/gemm_ops.h"
+#include <math.h>
 
 namespace {
 
@@ -62,8 +63,14 @@ int launch(const OpsGemm& g)
             const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
             return ops_launch_skinny_e4m3(g, fm, nb);
         }
-        // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 440 us
-        if (large && g.c_type != ELEM_F32) return ops_launch_tiles_e4m3(g, TILE_256);
+        // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 437 us, (1593,7232,4552) 65 against 134 widened.
+        // Below 2^22 results the widened form costs little or nothing more.  256 x 256 | 128 x 128: groups of 1024 rows
+        // (4096,2048) 166 | 189, (8192,8192,1024) 87 | 104; rounds of workgroups that are a quarter empty (4730,6880,272) 45 | 32, (7266,4800,1232) 75 | 70; groups
+        // of 128 rows (2048,2048) 173 | 158 (widened 251)
+        if (g.c_type != ELEM_F32 && (int64_t)g.M * g.N >= (1 << 22)) {
+            const double rounds = expected_tiles(g, 256, 256) / cus;
+            return ops_launch_tiles_e4m3(g, large && rounds >= 0.75 * ceil(rounds) ? TILE_256 : TILE_128_FAST);
+        }
         // 256 x 128 | 128 x 128: 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100, 2048^3 (128 tiles) 32 | 22, (512,8192,8192) (128 tiles) 106 | 70
         return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 256, 128) >= 0.75 * cus ? TILE_256x128 : TILE_128);
     }

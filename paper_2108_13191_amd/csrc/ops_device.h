@@ -92,19 +92,18 @@ __device__ __forceinline__ GroupScan scan_groups(const int32_t* offsets, int e0,
     }
     return s;
 }
-// The group of the `rank`-th most rows (of equal ones the first first); beyond 64 groups within each 64.
+// The group of the `rank`-th most rows (of equal ones the first first), of up to 64 groups.
 __device__ __forceinline__ int group_by_size(const int32_t* offsets, int E, int limit, int rank)
 {
-    const int lane = threadIdx.x & 63, e0 = rank & ~63;
-    int lo = 0, hi = 0, before = 0;
-    const bool there = e0 + lane < E;
-    if (there) group_rows(offsets, e0 + lane, limit, lo, hi);
-    const int rows = there ? hi - lo : -1;
-    for (int i = 0; i < min(64, E - e0); i++) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = -1, before = 0;
+    if (lane < E) group_rows(offsets, lane, limit, lo, hi);
+    const int rows = hi - lo;                              // -1 where there is no group
+    for (int i = 0; i < E; i++) {
         const int other = __builtin_amdgcn_readlane(rows, i);
         before += other > rows || (other == rows && i < lane);
     }
-    return e0 + __builtin_ctzll(__ballot(there && before == (rank & 63)));
+    return __builtin_ctzll(__ballot(lane < E && before == rank));
 }
 // what a launch needs at most: every group may end in a short tile
 inline int64_t max_group_tiles(int64_t rows, int64_t E, int64_t bm) { return rows / bm + (E < rows ? E : rows); }

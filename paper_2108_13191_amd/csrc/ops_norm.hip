@@ -188,7 +188,7 @@ int norm_of_type(const NormArgs& a, hipStream_t stream)
 template <typename T, int W, int P, int R>
 __global__ __launch_bounds__(64 * W * R) void rms_norm_grad_kernel(const NormGradArgs a)
 {
-    extern __shared__ float dyn[];                        // 2 * W * R floats, then (R > 1) a row of sums
+    extern __shared__ float dyn[];                        // 2 * W * R floats (32), then R * 512 * W of sums (32 KB)
     const int lane = threadIdx.x % (64 * W), sub = threadIdx.x / (64 * W), wave = threadIdx.x >> 6;
     float dg[P][8] = {};
     Raw8<T> gamma[P];
@@ -246,27 +246,21 @@ __global__ __launch_bounds__(64 * W * R) void rms_norm_grad_kernel(const NormGra
         }
     }
     if (!a.dgamma) return;
-    // sums of the workgroup's row slots, in their order
-    float* const rows = dyn + 2 * W * R;
-    for (int s = R - 1; s > 0; s--)
+    // sums of the workgroup's row slots, in their order, 512 W columns at a time
+    float* const sums = dyn + 2 * W * R;
+    float* const out = gridDim.x == 1 ? a.dgamma : a.ws + (int64_t)blockIdx.x * a.N;       // one workgroup's sums are the result
 #pragma unroll
-        for (int p = 0; p < P; p++) {
-            __syncthreads();
-            if (sub == s)
+    for (int p = 0; p < P; p++) {
+        __syncthreads();
 #pragma unroll
-                for (int i = 0; i < 8; i++) rows[i * 64 * W + lane] = dg[p][i];
-            __syncthreads();
-            if (sub == s - 1)
+        for (int i = 0; i < 8; i += 4) *(floatx4*)&sums[sub * 512 * W + 8 * lane + i] = floatx4{dg[p][i], dg[p][i + 1], dg[p][i + 2], dg[p][i + 3]};
+        __syncthreads();
+        for (int j = threadIdx.x; j < 512 * W; j += 64 * W * R) {
+            const int c = 512 * W * p + j;
+            float s = sums[j];
 #pragma unroll
-                for (int i = 0; i < 8; i++) dg[p][i] += rows[i * 64 * W + lane];
-        }
-    if (sub == 0) {
-        float* const out = a.ws + (int64_t)blockIdx.x * a.N;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-#pragma unroll
-            for (int i = 0; i < 8; i++) if (c + i < a.N) out[c + i] = dg[p][i];
+            for (int r = 1; r < R; r++) s += sums[r * 512 * W + j];
+            if (c < a.N) out[c] = s;
         }
     }
 }
@@ -338,7 +332,7 @@ inline int grad_rows(int N) { return N <= 1024 ? 16 : N <= 2048 ? 8 : N <= 4096 
 template <typename T, int W, int P, int R>
 int launch_norm_grad(const NormGradArgs& a, int parts, hipStream_t stream)
 {
-    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, P, R>), dim3((unsigned)parts), dim3(64 * W * R), (2 * W * R + 512 * W) * sizeof(float), stream, a);
+    hipLaunchKernelGGL((rms_norm_grad_kernel<T, W, P, R>), dim3((unsigned)parts), dim3(64 * W * R), (2 * W * R + R * 512 * W) * sizeof(float), stream, a);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 template <typename T>
@@ -360,7 +354,7 @@ int norm_grad_of_type(const NormGradArgs& a, hipStream_t stream)
         }
         if (rc != GEMM_F16_OK) return rc;
     }
-    if (!a.dgamma) return rc;
+    if (!a.dgamma || (parts == 1 && a.N <= 16384)) return rc;
     hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)(((int64_t)a.N + 63) / 64)), dim3(1024), 0, stream, a.ws, parts, a.N, a.dgamma);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }

@@ -12,7 +12,7 @@ namespace {
 
 using namespace ops_tile;
 
-constexpr int WAVES = 8;
+constexpr int WAVES = 8;      // (16 for the fewest workgroups: no faster)
 
 // OCC: wavefronts a SIMD that the registers leave room for
 template <int FM, int NB, int OCC, typename CT>

@@ -95,10 +95,10 @@ def test_e4m3_grouped(counts, N, K):
     run_e4m3(sum(counts) + 9, N, K, "f32", counts, seed=K)            # nine rows without an expert
 
 
-# Large products, whose tiles fill the chip: 16-bit results come from the e4m3 matrix instructions, which add products with the bits below
+# Large products, of 2^22 results and more: 16-bit results come from the e4m3 matrix instructions, which add products with the bits below
 # 2^-13 of the largest one's exponent of a group cut off.  A product of a group of 8 is then off by at most 2^-13 of the group's largest,
 # a sum by 8 * 2^-13 of its magnitudes at the very most; over many results errors of random sign stay below 2^-15 of their norm.
-LARGE = [(3400, 3700, 300), (4096, 3585, 640), (3333, 4500, 129)]
+LARGE = [(3400, 3700, 300), (4096, 3585, 640), (3333, 4500, 129), (4730, 4400, 272), (2048, 2050, 200)]
 MIDDLE = [(1200, 1300, 300), (1025, 1601, 520), (900, 2000, 128)]         # between those and the ones for few rows: 128 x 128 tiles
 
 
@@ -171,7 +171,8 @@ def test_e4m3_middle_product(M, N, K, c):
     assert np.array_equal(got, torch.from_numpy(want).float().to({"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[c]).double().numpy())
 
 
-@pytest.mark.parametrize("counts", [[1000, 0, 700, 1300, 33], [257, 256, 1, 2900], [3000], [100, 90, 0, 64, 129, 128] * 2, [30, 0, 41, 25] * 5], ids=str)
+@pytest.mark.parametrize("counts", [[1000, 0, 700, 1300, 33], [257, 256, 1, 2900], [3000], [100, 90, 0, 64, 129, 128] * 2, [30, 0, 41, 25] * 5,
+                                    [100, 90, 0, 64, 129, 128] * 8], ids=str)
 @pytest.mark.parametrize("c,extra", [("bf16", 0), ("f32", 11)])
 def test_e4m3_large_grouped(counts, c, extra):
     got, want, mag = large_e4m3(sum(counts) + extra, 4100, 390, c, counts, integers=True)
