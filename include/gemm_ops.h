@@ -11,7 +11,8 @@
  * allocated, nothing thrown, no state kept.  An output must not overlap an
  * input unless said otherwise.  No call writes between a row's end and the
  * pitch; an aligned 16-byte fetch may read there.  All entry points may be
- * captured into a HIP graph.
+ * captured into a HIP graph.  GEMM_F16_ERR_SIZE also stands for a result in more tiles than one
+ * launch has workgroups (2^22 or more).
  *
  * Element types: GEMM_TYPE_F16 / _BF16 (16 bits), _F32 (results only).  "e4m3" is
  * the 8-bit format with 4 exponent and 3 mantissa bits, no infinities, largest
@@ -65,7 +66,7 @@ int quantize_e4m3_blocks(int64_t M, int64_t N, int64_t type,
 /*
  * RMS norm of M rows of N elements with the residual's addition:
  *     h = x + r                    rounded to `type`; r NULL: h = x
- *     rstd = 1 / sqrt(mean(h^2) + eps)      of the rounded h, in f32
+ *     rstd = 1 / sqrt(mean(h^2) + eps)      of the rounded h, in f32 (0 where the squares' sum passes its range)
  *     y = h * rstd * gamma
  * Outputs, each of which may be NULL: H (h), Y (y in `type`), Q with scale (y in
  * e4m3 with scales in the rows form, quantised from the f32 value), rstd (M

@@ -30,6 +30,9 @@ struct OpsGemm {
     hipStream_t stream;
 };
 
+// A launch has less than 2^32 threads in a dimension of its grid.
+inline bool fits_a_launch(int64_t workgroups, int threads) { return workgroups <= UINT32_MAX / threads; }
+
 // ops_generic.hip: any alignment, any size
 int ops_launch_generic(const OpsGemm& g);
 

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * W * R) void rms_norm_kernel(const NormArgs a)
         }
     };
     if (live) {
-        const int passes = LOOP ? (a.N + 512 * W - 1) / (512 * W) : P;
+        const int passes = LOOP ? (int)(((int64_t)a.N + 512 * W - 1) / (512 * W)) : P;
         for (int p0 = 0; p0 < passes; p0 += P)
 #pragma unroll
             for (int p = 0; p < P; p++) {
@@ -348,6 +348,7 @@ int norm_grad_of_type(const NormGradArgs& a, hipStream_t stream)
         else if (a.N <= 8192) rc = launch_norm_grad<T, 8, 2, 2>(a, parts, stream);
         else if (a.N <= 16384) rc = launch_norm_grad<T, 16, 2, 1>(a, parts, stream);
         else {
+            if (!fits_a_launch(a.M, 1024)) return GEMM_F16_ERR_SIZE;
             if (a.dgamma) hipLaunchKernelGGL(rms_norm_dgamma_long_kernel<T>, dim3((unsigned)(((int64_t)a.N + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a);
             hipLaunchKernelGGL(rms_norm_grad_long_kernel<T>, dim3((unsigned)a.M), dim3(1024), 0, stream, a);
             rc = hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
@@ -454,7 +455,7 @@ template <typename T>
 int quant_blocks_of_type(const QuantArgs& a, hipStream_t stream)
 {
     const int64_t tiles = (((int64_t)a.M + 127) / 128) * (((int64_t)a.N + 127) / 128);
-    if (tiles > INT32_MAX) return GEMM_F16_ERR_SIZE;
+    if (!fits_a_launch(tiles, 256)) return GEMM_F16_ERR_SIZE;
     hipLaunchKernelGGL(quantize_blocks_kernel<T>, dim3((unsigned)tiles), dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
@@ -466,7 +467,35 @@ int ops_norm_grad_parts(int64_t M, int64_t N)
     const int64_t rows = grad_rows((int)(N < INT32_MAX ? N : INT32_MAX)), g = (M + rows - 1) / rows;
     return (int)(g < 256 ? g : 256);
 }
-int ops_launch_norm(int type, const NormArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? norm_of_type<half_t>(a, stream) : norm_of_type<bf16_t>(a, stream); }
+// Rows need nothing of each other: more of them than the grid of one launch has threads for (a row takes up to 1024) go in several launches.
+constexpr int64_t LAUNCH_ROWS = 1 << 21;
+int ops_launch_norm(int type, const NormArgs& all, hipStream_t stream)
+{
+    int rc = GEMM_F16_OK;
+    for (int64_t i = 0; i < all.M && rc == GEMM_F16_OK; i += LAUNCH_ROWS) {
+        NormArgs a = all;
+        a.M = (int)(all.M - i < LAUNCH_ROWS ? all.M - i : LAUNCH_ROWS);
+        a.X = (const half_t*)all.X + i * all.ldx;                          // both types have 2 bytes
+        if (a.R) a.R = (const half_t*)all.R + i * all.ldr;
+        if (a.H) a.H = (half_t*)all.H + i * all.ldh;
+        if (a.Y) a.Y = (half_t*)all.Y + i * all.ldy;
+        if (a.Q) { a.Q += i * all.ldq; a.scale += i; }
+        if (a.rstd) a.rstd += i;
+        rc = type == GEMM_TYPE_F16 ? norm_of_type<half_t>(a, stream) : norm_of_type<bf16_t>(a, stream);
+    }
+    return rc;
+}
 int ops_launch_norm_grad(int type, const NormGradArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? norm_grad_of_type<half_t>(a, stream) : norm_grad_of_type<bf16_t>(a, stream); }
-int ops_launch_quant_rows(int type, const QuantArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? quant_rows_of_type<half_t>(a, stream) : quant_rows_of_type<bf16_t>(a, stream); }
+int ops_launch_quant_rows(int type, const QuantArgs& all, hipStream_t stream)
+{
+    int rc = GEMM_F16_OK;
+    for (int64_t i = 0; i < all.M && rc == GEMM_F16_OK; i += LAUNCH_ROWS) {
+        QuantArgs a = all;
+        a.M = (int)(all.M - i < LAUNCH_ROWS ? all.M - i : LAUNCH_ROWS);
+        a.X = (const half_t*)all.X + i * all.ldx;
+        a.Q += i * all.ldq; a.scale += i;
+        rc = type == GEMM_TYPE_F16 ? quant_rows_of_type<half_t>(a, stream) : quant_rows_of_type<bf16_t>(a, stream);
+    }
+    return rc;
+}
 int ops_launch_quant_blocks(int type, const QuantArgs& a, hipStream_t stream) { return type == GEMM_TYPE_F16 ? quant_blocks_of_type<half_t>(a, stream) : quant_blocks_of_type<bf16_t>(a, stream); }

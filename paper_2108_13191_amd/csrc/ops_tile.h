@@ -575,7 +575,7 @@ template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = fals
 int launch_tiles(const OpsGemm& g)
 {
     const int64_t grid = tile_grid<BM, BN>(g);
-    if (grid < 0) return GEMM_F16_ERR_SIZE;
+    if (grid < 0 || !fits_a_launch(grid, 512)) return GEMM_F16_ERR_SIZE;
     if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
     else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
