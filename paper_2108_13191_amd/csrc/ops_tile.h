@@ -552,7 +552,7 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
                     ctx4 o;
 #pragma unroll
                     for (int e = 0; e < 4; e++) o[e] = (CT)v[e];
-                    *(ctx4*)dst = o;
+                    __builtin_nontemporal_store(o, (ctx4*)dst);      // past the L2s, which hold what other tiles read: 16-bit (16384,2304,768) 76 -> 68 us
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; e++) if (col + e < g.N) dst[e] = (CT)v[e];
