@@ -71,6 +71,9 @@ int launch(const OpsGemm& g)
             const double rounds = expected_tiles(g, 256, 256) / cus;
             return ops_launch_tiles_e4m3(g, large && rounds >= 0.75 * ceil(rounds) ? TILE_256 : TILE_128_FAST);
         }
+        // groups that leave quarters of 128 rows empty, with | without a branch around those: 24 rows each of 16 experts (4096,2048) 39 | 46, 32 rows
+        // 41 | 46, 30 rows of 64 (1408,2048) 58 | 65, 48 rows 56 | 56, 100 rows 67 | 62
+        if (g.offsets && rows <= 40.0) return ops_launch_tiles_e4m3(g, TILE_128_SHORT);
         // 256 x 128 | 128 x 128: 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100, 2048^3 (128 tiles) 32 | 22, (512,8192,8192) (128 tiles) 106 | 70
         return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 256, 128) >= 0.75 * cus ? TILE_256x128 : TILE_128);
     }

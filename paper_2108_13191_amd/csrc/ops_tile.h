@@ -154,7 +154,7 @@ template <int BM, int BN, int S, bool SCALED> constexpr int lds_bytes()
 // ANY: operands of any alignment, in 16 bits, with rows of 8 elements or more: copies go through registers, a 16-byte load at element alignment and
 // a k step later, where the copy into LDS would be asked for, a write to LDS.  A chunk that would leave its row is loaded as the row's
 // last 8 elements and shifted, so that no load lies in a branch: behind one the compiler waits for every load in flight.
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, bool ANY, typename CT>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, bool ANY, bool SHORT, typename CT>
 // (128 x 128 tiles: registers for two workgroups a compute unit; widened e4m3 ones spill then, (1024,4096,1023) 22.5 us against 17.3)
 __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void ops_tile_kernel(const OpsGemm g)
 {
@@ -358,6 +358,9 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
         }
         uint32_t s_rd = smem_base + S0 + (grp * HM + l16) * 4;
 
+        // SHORT: quarters of the tile without rows are neither read nor multiplied, by a branch in each phase (the copies stay, as the waits count them)
+        const int live = SHORT ? min(max((t.row_end - t.row0 - grp * HM + HM / 2 - 1) / (HM / 2), 0), 2) : 2;
+
         Frag fa[FH], fb[FN];
         Wide wa[EXACT ? FH : 1], wb[EXACT ? FN : 1];
         float scale[FH];
@@ -415,11 +418,36 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
         auto multiply_phase = [&](int k, int st, auto half, auto copy, auto group) {
             constexpr int COPY = decltype(copy)::value, h = decltype(half)::value, GRP = decltype(group)::value;
             constexpr int NM = FH * FN;
+            // copies of this phase behind MFMA i: A's half in k rows (all of A in the second phase otherwise), B in X's second and Y's first phase
+            auto copies = [&](int i) {
+                if constexpr (COPY > 0) {
+                    typedef typename std::conditional<COPY == 1, Whole, Tail>::type W;
+                    constexpr int SLOTS = 8;                                  // places of copies among the MFMAs
+                    constexpr int EVERY = NM >= SLOTS ? NM / SLOTS : 1, PER = NM >= SLOTS ? 1 : SLOTS / NM;
+                    if (i % EVERY == 0) {
+                        const int slot = i / EVERY;
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int j = 0; j < PER; j++) {
+                            const int c = slot * PER + j;                     // 0 .. 7
+                            const int na = AKC ? TA / 2 : (h == 0 ? 0 : TA), a_first = AKC ? h * (TA / 2) : 0;
+                            if (c < na) copy_a(k + S, st, a_first + c, W{});
+                            else if (c < na + TB && GRP == 1 - h) copy_b(k + S, st, c - na, W{});
+                            if (SCALED && h == 1 && c == 7) copy_s(k + S, st);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            };
+            if (!(h < live)) {
+#pragma unroll
+                for (int i = 0; i < NM; i++) copies(i);
+                return;
+            }
             if constexpr (SCALED) {
 #pragma unroll
                 for (int m = 0; m < FH; m++) scale[m] *= sbk;
             }
-            // copies of this phase: A's half in k rows (all of A in the second phase otherwise), B in X's second and Y's first phase
             // e4m3: the results of MFMA i are added while MFMAs i + 1 and i + 2 run
             constexpr int BEHIND = 2;
             floatx4 part[BEHIND + 1];
@@ -442,29 +470,20 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
                 } else {
                     acc[h * FH + m][n] = mfma_step<ELEM>(fb[n], fa[m], acc[h * FH + m][n]);
                 }
-                if constexpr (COPY > 0) {
-                    typedef typename std::conditional<COPY == 1, Whole, Tail>::type W;
-                    constexpr int SLOTS = 8;                                  // places of copies among the MFMAs
-                    constexpr int EVERY = NM >= SLOTS ? NM / SLOTS : 1, PER = NM >= SLOTS ? 1 : SLOTS / NM;
-                    if (i % EVERY == 0) {
-                        const int slot = i / EVERY;
-                        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int j = 0; j < PER; j++) {
-                            const int c = slot * PER + j;                     // 0 .. 7
-                            const int na = AKC ? TA / 2 : (h == 0 ? 0 : TA), a_first = AKC ? h * (TA / 2) : 0;
-                            if (c < na) copy_a(k + S, st, a_first + c, W{});
-                            else if (c < na + TB && GRP == 1 - h) copy_b(k + S, st, c - na, W{});
-                            if (SCALED && h == 1 && c == 7) copy_s(k + S, st);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
+                copies(i);
             }
             if constexpr (SCALED) {
 #pragma unroll
                 for (int i = NM - BEHIND; i < NM; i++) add(i);
             }
+        };
+        auto half_step = [&](int k, int st, auto half, auto copy, auto group) {
+            constexpr int h = decltype(half)::value, GRP = decltype(group)::value, COPY = decltype(copy)::value;
+            if (h < live) read_phase(k, st, h);
+            __builtin_amdgcn_s_waitcnt(0xC07F);                              // lgkmcnt(0)
+            asm volatile("" ::: "memory");
+            phase_barrier();
+            multiply_phase(k, st, half, copy, group);
             if constexpr (h == 1 || GRP == 1) {
                 __builtin_amdgcn_sched_barrier(0);
                 // copies for later k steps than the next may be on their way
@@ -473,16 +492,8 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
                 else if constexpr (COPY == 2) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 else                          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(COPY <= -1 ? NC * (-COPY - 1) : 0) : "memory");
             }
-        };
-        auto half_step = [&](int k, int st, auto half, auto copy, auto group) {
-            constexpr int h = decltype(half)::value, GRP = decltype(group)::value;
-            read_phase(k, st, h);
-            __builtin_amdgcn_s_waitcnt(0xC07F);                              // lgkmcnt(0)
-            asm volatile("" ::: "memory");
-            phase_barrier();
-            multiply_phase(k, st, half, copy, group);
             // Y began one barrier later and leaves out the last one
-            if constexpr (decltype(copy)::value != 0 || GRP == 0 || h == 0) phase_barrier();
+            if constexpr (COPY != 0 || GRP == 0 || h == 0) phase_barrier();
         };
         auto run_loop = [&](auto group) {
             int k = 0, st = 0;                                               // the k step and its stage
@@ -571,14 +582,14 @@ inline int64_t tile_grid(const OpsGemm& g)
     return rows > INT32_MAX / tn ? -1 : rows * tn;
 }
 
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false, bool ANY = false>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false, bool ANY = false, bool SHORT = false>
 int launch_tiles(const OpsGemm& g)
 {
     const int64_t grid = tile_grid<BM, BN>(g);
     if (grid < 0 || !fits_a_launch(grid, 512)) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
-    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
-    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
+    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 

@@ -10,5 +10,6 @@ int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile)
     using namespace ops_tile;
     if (tile == TILE_256) return launch_tiles<ELEM_E4M3, true, true, 256, 256, 2>(g);
     if (tile == TILE_128_FAST) return launch_tiles<ELEM_E4M3, true, true, 128, 128, 2>(g);
+    if (tile == TILE_128_SHORT) return launch_tiles<ELEM_E4M3, true, true, 128, 128, 2, true, false, true>(g);
     return tile == TILE_256x128 ? launch_tiles<ELEM_E4M3, true, true, 256, 128, 2, true>(g) : launch_tiles<ELEM_E4M3, true, true, 128, 128, 2, true>(g);
 }
