@@ -46,13 +46,17 @@ int launch(const OpsGemm& g)
     const int cus = chip().cus;
     const double rows = (double)g.M / g.E;                                  // of a group
     if (g.k_ragged) {
-        // gradient of B, 256 x 256 | 128 x 128: (16384 rows, 2048 x 1024, 32 experts) 1024 tiles 132 | 151, (16384, 4096 x 2048, 8) 1024 tiles
-        // 254 | 321, (16384, 2304 x 768, 8) 216 tiles 97 | 79, (2048, 1024 x 1024, 8) 128 tiles 23 | 15
-        const OpsTile t = expected_tiles(g, 256, 256) >= 2.0 * cus ? TILE_256 : TILE_128;
+        // gradient of B, 256 x 256 | 128 x 128, from two rounds of the former on: both gradients of (16384 rows, 2048 x 1024, 32 experts) 1024 tiles 214 | 231,
+        // (16384, 4096 x 2048, 8) 1024 tiles 505 | 563; below one: B's alone, (16384, 2304 x 768, 8) 216 tiles 89 | 77, (2048 x 1024, 4) 128 tiles 139 | 91.
+        // Between, with many rows a group, (16384, 4096 x 2048, 3) 384 tiles 231 | 277, (2048 x 2048, 5) 320 tiles 146 | 151, with few (4000, 1408 x 2048, 8) 46 | 40; and
+        // one round of a single group's, whose operands 128 x 128 tiles read too often: (16384, 4096 x 4096, 1) 380 | 602, (1000, ..) 40 | 43
+        const double tiles = expected_tiles(g, 256, 256);
+        const OpsTile t = tiles >= 2.0 * cus || (tiles >= 1.25 * cus && (double)g.K / g.E >= 1024.0) || tiles >= (double)g.E * cus ? TILE_256 : TILE_128;
         return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, t) : ops_launch_tiles_bf16(g, t);
     }
-    // three quarters of the compute units with a tile of 256 x 256, and groups that fill three quarters of one
-    const bool large = rows >= 192.0 && expected_tiles(g, 256, 256) >= 0.75 * cus;
+    // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
+    // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
+    const bool large = rows >= 192.0 && expected_tiles(g, 128, 128) >= 2.0 * cus;
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
         // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
@@ -66,16 +70,17 @@ int launch(const OpsGemm& g)
         // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 437 us, (1593,7232,4552) 65 against 134 widened.
         // Below 2^22 results the widened form costs little or nothing more.  256 x 256 | 128 x 128: groups of 1024 rows
         // (4096,2048) 166 | 189, (8192,8192,1024) 87 | 104; rounds of workgroups that are a quarter empty (4730,6880,272) 45 | 32, (7266,4800,1232) 75 | 70; groups
-        // of 128 rows (2048,2048) 173 | 158 (widened 251)
+        // of 128 rows (2048,2048) 173 | 158 (widened 251); one round that is half full (4000,2304,6000) 71 | 88
         if (g.c_type != ELEM_F32 && (int64_t)g.M * g.N >= (1 << 22)) {
             const double rounds = expected_tiles(g, 256, 256) / cus;
-            return ops_launch_tiles_e4m3(g, large && rounds >= 0.75 * ceil(rounds) ? TILE_256 : TILE_128_FAST);
+            return ops_launch_tiles_e4m3(g, large && rounds >= (rounds > 1.0 ? 0.75 : 0.5) * ceil(rounds) ? TILE_256 : TILE_128_FAST);
         }
         // groups that leave quarters of 128 rows empty, with | without a branch around those: 24 rows each of 16 experts (4096,2048) 39 | 46, 32 rows
         // 41 | 46, 30 rows of 64 (1408,2048) 58 | 65, 48 rows 56 | 56, 100 rows 67 | 62
         if (g.offsets && rows <= 40.0) return ops_launch_tiles_e4m3(g, TILE_128_SHORT);
-        // 256 x 128 | 128 x 128: 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100, 2048^3 (128 tiles) 32 | 22, (512,8192,8192) (128 tiles) 106 | 70
-        return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 256, 128) >= 0.75 * cus ? TILE_256x128 : TILE_128);
+        // 256 x 128 | 128 x 128, whose registers leave room for one a compute unit: more than a round of the latter, 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100,
+        // (2304,2048,2048) (288 of 128 x 128) 31 | 39; a round 2048^3 32 | 22, (512,8192,8192) 106 | 70
+        return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 128, 128) > cus ? TILE_256x128 : TILE_128);
     }
     // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
     const OpsTile t = large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128;
