@@ -4,6 +4,10 @@
 // All of it is bound by memory: every element is read once and written once, in 16-byte accesses (8 elements of 16 bits a lane), and what a row's
 // sum needs again stays in registers.  A block of 128 is 16 neighbouring lanes, so its largest magnitude takes four
 // rotations within a row of lanes.  Accesses are at element alignment: rows of any pitch take the same path.
+//
+// Measured (a copy of 1 GiB: 5.15 TB/s): norm of (16384,4096) bf16 with residual and e4m3 output 86.4 us, 5.5 TB/s; 16 rows of 8192 4.5 us, of which a launch
+// and its first load and barrier are all but little; gradients of (8191,4000) 60 us, 4.4 TB/s; SwiGLU (4096,8192) to e4m3 35.9 us, 4.7 TB/s; blocks of
+// (8192,8192) 42 us, 4.8 TB/s.
 #include "ops_device.h"
 #include "../../include/gemm_ops.h"
 
@@ -169,7 +173,7 @@ int launch_norm(const NormArgs& a, hipStream_t stream)
 template <typename T>
 int norm_of_type(const NormArgs& a, hipStream_t stream)
 {
-    // few rows: as many wavefronts a row as it has chunks of 512 columns, (16,8192) f16 4.1 us against 5.9 with 4
+    // few rows: as many wavefronts a row as it has chunks of 512 columns, (16,8192) f16 4.5 us against 5.9 with 4
     if (a.M <= 2 * chip().cus && a.N > 2048 && a.N <= 8192) return launch_norm<T, 16, 1, 1>(a, stream);
     if (a.N <= 512) return launch_norm<T, 1, 1, 4>(a, stream);
     if (a.N <= 1024) return launch_norm<T, 1, 2, 4>(a, stream);
@@ -183,8 +187,8 @@ int norm_of_type(const NormArgs& a, hipStream_t stream)
 // ---- its gradients ------------------------------------------------------------------------------------------------------------
 // dX row by row; the columns' sums of dy xhat stay in registers over all rows of a workgroup, which writes them as one row of the workspace;
 // a second kernel adds those.  Every sum has a fixed order.
-// 16 wavefronts a workgroup with two chunks a lane: (8191,4000) bf16 with dH 62 us, 4.2 TB/s (rows of 8192 bytes 4.9); one chunk a lane and the next row's loads
-// ahead 68, four chunks a lane in 8 wavefronts 64.
+// 16 wavefronts a workgroup with two chunks a lane: (8191,4000) bf16 with dH 60 us, 4.4 TB/s (rows of 8192 bytes 4.9); one chunk a lane and the next row's loads
+// ahead 68, four chunks a lane in 8 wavefronts 64 (against 62 then).
 template <typename T, int W, int P, int R>
 __global__ __launch_bounds__(64 * W * R) void rms_norm_grad_kernel(const NormGradArgs a)
 {

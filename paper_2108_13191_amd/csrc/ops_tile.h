@@ -22,6 +22,12 @@
 // e4m3: each MFMA starts from zero and its 4 results are added to the accumulators times a_scale * b_scale, in f32.  With the B
 // fragment first a lane holds 4 columns of one row, so the factor is one register for a block of 16 x 16; the columns of a
 // wavefront lie in one block of 128, whose scale is a scalar.  The scales of the tile's rows come into LDS with the operands.
+//
+// Measured.  256 x 256 x 8192^2 in e4m3: 437 us, 2.5 PFLOP/s, MFMAs busy 63 % at 1.87 GHz: the chip's power (zero operands: 354 us).  Shorter sums are bound by
+// what a tile does around its loop -- its group, the first copies, its stores, which all compute units do at once -- and by the last round of tiles: f16
+// (16384,2304,768) of 8 experts 68 us, 24 us a round of which 11 are MFMAs; gradients (16384 rows, 2048 x 1024, 32 experts) 95 and 117 us.  Tried for those: a
+// workgroup a compute unit that goes from tile to tile and requests the next one's operands before its stores, half of the workgroups
+// later than the others: no faster.
 #pragma once
 #include <type_traits>
 #include "ops_device.h"
