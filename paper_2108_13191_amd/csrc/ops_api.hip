@@ -78,9 +78,13 @@ int launch(const OpsGemm& g)
         // groups that leave quarters of 128 rows empty, with | without a branch around those: 24 rows each of 16 experts (4096,2048) 39 | 46, 32 rows
         // 41 | 46, 30 rows of 64 (1408,2048) 58 | 65, 48 rows 56 | 56, 100 rows 67 | 62
         if (g.offsets && rows <= 40.0) return ops_launch_tiles_e4m3(g, TILE_128_SHORT);
-        // 256 x 128 | 128 x 128, whose registers leave room for one a compute unit: more than a round of the latter, 4000^3 f32 128 | 154, (4096,8192,1024) 85 | 100,
-        // (2304,2048,2048) (288 of 128 x 128) 31 | 39; a round 2048^3 32 | 22, (512,8192,8192) 106 | 70
-        return ops_launch_tiles_e4m3(g, rows >= 192.0 && expected_tiles(g, 128, 128) > cus ? TILE_256x128 : TILE_128);
+        // Up to a round of 128 x 128 ones, one a compute unit: those in registers for one | two, 2048^3 22 | 23, (512,8192,8192) 70 | 75.
+        if (expected_tiles(g, 128, 128) <= cus) return ops_launch_tiles_e4m3(g, TILE_128);
+        // 256 x 128 | 128 x 128, two a compute unit: a round of the former (2048,3000,2048) 35 | 36; full rounds and long sums 4000^3 129 | 134; else (3000,3000,2048)
+        // 66 | 53, (4096,8192,1024) 90 | 79, (8192,8192,256) 88 | 67, (13785,15296,400) 397 | 328, 16384 rows of 32 experts (2048,512) 66 | 56
+        const double rounds = expected_tiles(g, 256, 128) / cus;
+        const bool tall = rows >= 192.0 && (rounds <= 1.0 || (g.K > 2048 && rounds >= 0.9 * ceil(rounds)));
+        return ops_launch_tiles_e4m3(g, tall ? TILE_256x128 : TILE_128_PAIR);
     }
     // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
     const OpsTile t = large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128;

@@ -156,15 +156,23 @@ template <int BM, int BN, int S, bool SCALED> constexpr int lds_bytes()
     return stages > out ? stages : out;
 }
 
-// EXACT: e4m3 values are widened to f16 and multiplied by f16 MFMAs
-// ANY: operands of any alignment, in 16 bits, with rows of 8 elements or more: copies go through registers, a 16-byte load at element alignment and
-// a k step later, where the copy into LDS would be asked for, a write to LDS.  A chunk that would leave its row is loaded as the row's
-// last 8 elements and shifted, so that no load lies in a branch: behind one the compiler waits for every load in flight.
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT, bool ANY, bool SHORT, typename CT>
-// (128 x 128 tiles: registers for two workgroups a compute unit; widened e4m3 ones spill then, (1024,4096,1023) 22.5 us against 17.3)
-__global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void ops_tile_kernel(const OpsGemm g)
+// Forms of the kernel
+enum Form {
+    PLAIN,
+    WIDENED,            // e4m3 values are widened to f16 and multiplied by f16 MFMAs
+    WIDENED_PAIR,       // in registers for two workgroups a compute unit, of 128 x 128
+    WIDENED_SHORT,      // quarters of the tile without rows are left out
+    // operands of any alignment, in 16 bits, with rows of 8 elements or more: copies go through registers, a 16-byte load at element alignment and
+    // a k step later, where the copy into LDS would be asked for, a write to LDS.  A chunk that would leave its row is loaded as the row's
+    // last 8 elements and shifted, so that no load lies in a branch: behind one the compiler waits for every load in flight.
+    ANY_ALIGNMENT
+};
+
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, Form FORM, typename CT>
+// (128 x 128 tiles: registers for two workgroups a compute unit, also where some are spilled: 16-bit (16384,2047,1023) of any alignment 131 us against 175)
+__global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && FORM != WIDENED_SHORT ? 4 : 2) void ops_tile_kernel(const OpsGemm g)
 {
-    constexpr bool SCALED = ELEM == ELEM_E4M3;
+    constexpr bool SCALED = ELEM == ELEM_E4M3, EXACT = FORM == WIDENED || FORM == WIDENED_PAIR || FORM == WIDENED_SHORT, ANY = FORM == ANY_ALIGNMENT, SHORT = FORM == WIDENED_SHORT;
     constexpr int ES = Elem<ELEM>::size, KE = STEP / ES;   // elements of a k step
     constexpr int HM = BM / 2, WN = BN / 4;                // rows of a group, columns of a wavefront
     constexpr int FM = HM / 16, FN = WN / 16, FH = FM / 2; // blocks of 16 x 16; rows of blocks of a half
@@ -394,6 +402,11 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
                     for (int n = 0; n < FN; n++) { uint32_t b0 = b_rd[n] + bs; asm volatile("" : "+v"(b0)); fb[n] = read_tr(b0, BN * 2); }
                 }
                 if constexpr (SCALED) sbk = sb[k];
+                if constexpr (FORM == WIDENED_PAIR) {                        // before A is read: fewer registers at a time
+#pragma unroll
+                    for (int n = 0; n < FN; n++) wb[n] = widened(fb[n]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if constexpr (AKC) {
                 uint32_t a0 = a_rd[0] + as, a1 = a_rd[1] + as;
@@ -410,7 +423,7 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && !EXACT ? 4 : 2) void
                     scale[m] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(s_rd + st * (BM * 4) + (h * FH + m) * 64);
             }
             if constexpr (EXACT) {
-                if (h == 0) {
+                if (h == 0 && FORM != WIDENED_PAIR) {
 #pragma unroll
                     for (int n = 0; n < FN; n++) wb[n] = widened(fb[n]);
                 }
@@ -588,14 +601,14 @@ inline int64_t tile_grid(const OpsGemm& g)
     return rows > INT32_MAX / tn ? -1 : rows * tn;
 }
 
-template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, bool EXACT = false, bool ANY = false, bool SHORT = false>
+template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, Form FORM = PLAIN>
 int launch_tiles(const OpsGemm& g)
 {
     const int64_t grid = tile_grid<BM, BN>(g);
     if (grid < 0 || !fits_a_launch(grid, 512)) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
-    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
-    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, EXACT, ANY, SHORT, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, FORM, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
+    else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, FORM, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }
+    else if constexpr (ELEM != ELEM_F16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, FORM, bf16_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 

@@ -8,7 +8,7 @@ int launch_tile(const OpsGemm& g, OpsTile tile)
     using namespace ops_tile;
     if (tile == TILE_256) return launch_tiles<ELEM_F16, AKC, BKC, 256, 256, 2>(g);
     if constexpr (AKC && !BKC) { if (tile == TILE_128x256) return launch_tiles<ELEM_F16, true, false, 128, 256, 3>(g); }
-    if (tile == TILE_128_ANY) return launch_tiles<ELEM_F16, AKC, BKC, 128, 128, 2, false, true>(g);
+    if (tile == TILE_128_ANY) return launch_tiles<ELEM_F16, AKC, BKC, 128, 128, 2, ANY_ALIGNMENT>(g);
     return launch_tiles<ELEM_F16, AKC, BKC, 128, 128, 2>(g);
 }
 }  // namespace
