@@ -37,6 +37,7 @@ inline bool fits_a_launch(int64_t workgroups, int threads) { return workgroups <
 int ops_launch_generic(const OpsGemm& g);
 
 // ops_tile_*.hip: 16-byte aligned operands (TILE_128_ANY: any) with pitches up to 2^22 elements (each takes the tiles that the choice in ops_api.hip has for it)
+// e4m3: TILE_256 and TILE_128_FAST on the e4m3 instructions, the others widened to f16 (_PAIR: two workgroups a compute unit, _SHORT: short groups of rows)
 enum OpsTile { TILE_256, TILE_256x128, TILE_128x256, TILE_128, TILE_128_ANY, TILE_128_FAST, TILE_128_PAIR, TILE_128_SHORT };
 int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_f16(const OpsGemm& g, OpsTile tile);
