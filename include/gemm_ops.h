@@ -42,7 +42,7 @@ enum { GEMM_OPS_ACT_NONE = 0, GEMM_OPS_ACT_RELU = 1, GEMM_OPS_ACT_SWIGLU = 2 };
 
 /*
  * Quantise to e4m3.  For each block: scale = max(largest |x|, 2^-96) / 448 in
- * f32, element = x * (448 / largest) rounded to nearest even.  A block that holds a NaN
+ * f32, element = x / scale rounded to nearest even.  A block that holds a NaN
  * or an infinity gets the scale NaN and elements NaN, so that it shows in any
  * product; nothing else is touched by it.  A block of zeros is zeros with the scale 2^-96 / 448.
  *

@@ -39,24 +39,32 @@ __device__ __forceinline__ float sum64(float x)
     return x;
 }
 
-// The scale of a block from the largest magnitude in it (bits), and what its values are multiplied by: NaN where the block
-// holds a NaN or an infinity.
+// The scale of a block from the largest magnitude in it (bits), and its reciprocal: NaN where the block holds a NaN or an infinity.
 constexpr float E4M3_MAX = 448.0f, SCALE_FLOOR = 0x1p-96f;
-struct BlockScale { float scale, inverse; };
+struct BlockScale {
+    float scale, inverse;
+    // y / scale: the product with the reciprocal, corrected by what it leaves of y (exact in one fma).  16-bit values and their scales make ties of e4m3
+    // often: the product alone rounds 1 of 1000 elements of a normal bf16 matrix the other way, 1 of 10000 in f16.  (Zeros keep their sign.)
+    __device__ __forceinline__ float quotient(float y) const
+    {
+        const float t = y * inverse;
+        return __builtin_fmaf(-__builtin_fmaf(t, scale, -y), inverse, t);
+    }
+};
 __device__ __forceinline__ BlockScale block_scale(uint32_t bits)
 {
     if (bits >= 0x7f800000u) { const float nan = __builtin_nanf(""); return {nan, nan}; }
-    const float m = fmaxf(__builtin_bit_cast(float, bits), SCALE_FLOOR);
-    return {m / E4M3_MAX, E4M3_MAX / m};
+    const float scale = fmaxf(__builtin_bit_cast(float, bits), SCALE_FLOOR) / E4M3_MAX;
+    return {scale, 1.0f / scale};
 }
-// 8 values to e4m3, to nearest even (none is above 448 but for the last bit of the product, which rounds back)
-__device__ __forceinline__ uintx2 to_e4m3(const float (&y)[8], float inverse)
+// 8 values to e4m3, to nearest even (none is above 448 but for the last bits of the quotient, which round back)
+__device__ __forceinline__ uintx2 to_e4m3(const float (&y)[8], const BlockScale& s)
 {
     int lo = 0, hi = 0;
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * inverse, y[1] * inverse, lo, false);
-    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * inverse, y[3] * inverse, lo, true);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * inverse, y[5] * inverse, hi, false);
-    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * inverse, y[7] * inverse, hi, true);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(s.quotient(y[0]), s.quotient(y[1]), lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(s.quotient(y[2]), s.quotient(y[3]), lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(s.quotient(y[4]), s.quotient(y[5]), hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(s.quotient(y[6]), s.quotient(y[7]), hi, true);
     return uintx2{(uint32_t)lo, (uint32_t)hi};
 }
 

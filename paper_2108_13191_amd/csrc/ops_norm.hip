@@ -6,8 +6,8 @@
 // rotations within a row of lanes.  Accesses are at element alignment: rows of any pitch take the same path.
 //
 // Measured (a copy of 1 GiB: 5.15 TB/s): norm of (16384,4096) bf16 with residual and e4m3 output 86.4 us, 5.5 TB/s; 16 rows of 8192 4.5 us, of which a launch
-// and its first load and barrier are all but little; gradients of (8191,4000) 60 us, 4.4 TB/s; SwiGLU (4096,8192) to e4m3 35.9 us, 4.7 TB/s; blocks of
-// (8192,8192) 42 us, 4.8 TB/s.
+// and its first load and barrier are all but little; gradients of (8191,4000) 60 us, 4.4 TB/s; SwiGLU (4096,8192) to e4m3 36.1 us, 4.7 TB/s; blocks of
+// (8192,8192) 43 us, 4.7 TB/s.
 #include "ops_device.h"
 #include "../../include/gemm_ops.h"
 
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * W * R) void rms_norm_kernel(const NormArgs a)
 #pragma unroll
             for (int i = 0; i < 8; i++) m = max(m, magnitude(y[i]));
             const BlockScale s = block_scale(max16(m));
-            store_e4m3(a.Q + row * a.ldq + c, left, to_e4m3(y, s.inverse));
+            store_e4m3(a.Q + row * a.ldq + c, left, to_e4m3(y, s));
             if ((lane & 15) == 0) a.scale[c / 128 * a.ld_scale + row] = s.scale;
         }
     };
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantArgs a)
             m = max(m, magnitude(y[i]));
         }
         const BlockScale s = block_scale(max16(m));
-        if (left_at(p) > 0) store_e4m3(a.Q + row * a.ldq + first + 512 * p, left_at(p), to_e4m3(y, s.inverse));
+        if (left_at(p) > 0) store_e4m3(a.Q + row * a.ldq + first + 512 * p, left_at(p), to_e4m3(y, s));
         if ((lane & 15) == 0) scales[4 * p + lane / 16][wave] = s.scale;
     }
     __syncthreads();
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(256) void quantize_blocks_kernel(const QuantArgs a)
 #pragma unroll
     for (int p = 0; p < 8; p++) {
         const int64_t row = 128 * bm + 16 * p + threadIdx.x / 16;
-        if (row < a.M && c < a.N) store_e4m3(a.Q + row * a.ldq + c, (int)(a.N - c), to_e4m3(y[p], s.inverse));
+        if (row < a.M && c < a.N) store_e4m3(a.Q + row * a.ldq + c, (int)(a.N - c), to_e4m3(y[p], s));
     }
 }
 

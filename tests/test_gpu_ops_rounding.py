@@ -1,0 +1,59 @@
+"""What the quantisers round, to the bit: an element is the e4m3 value nearest to its f32 value divided by the scale that is stored beside it, ties
+to even."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_2108_13191_amd import binding                                    # noqa: E402
+from ops_util import DT, TYPE, ceil128, stream                              # noqa: E402
+
+
+def bits(t):
+    return t.contiguous().view(torch.uint8)
+
+
+def quotients(y, scale):
+    """e4m3(y / scale) on the host: both roundings to nearest even."""
+    return (y / scale).to(DT["e4m3"])
+
+
+@pytest.mark.parametrize("M,N", [(64, 4096), (300, 1000), (129, 8200)])
+@pytest.mark.parametrize("type", ["f16", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+def test_rows_hold_the_nearest_quotients(M, N, type, act):
+    x = (torch.randn(M, N, generator=torch.Generator().manual_seed(M)) * 3.0).to(DT[type])
+    q, s = torch.empty(M, N, dtype=DT["e4m3"], device="cuda"), torch.empty(ceil128(N), M, device="cuda")
+    code = binding.ACT_RELU if act == "relu" else binding.ACT_NONE
+    binding.check(binding.quantize_e4m3_rows(M, N, TYPE[type], code, x.cuda(), N, q, N, s, M, stream()))
+    y = x.float().clamp_min(0.0) if act == "relu" else x.float()
+    most = torch.nn.functional.pad(y, (0, -N % 128)).view(M, -1, 128).abs().amax(2).clamp_min(2.0 ** -96)
+    assert torch.equal(s.cpu().t(), most / 448.0)
+    want = quotients(y, s.cpu().t().repeat_interleave(128, 1)[:, :N])
+    assert torch.equal(bits(q.cpu()), bits(want))
+
+
+@pytest.mark.parametrize("M,N", [(256, 2048), (300, 1000)])
+@pytest.mark.parametrize("type", ["f16", "bf16"])
+def test_blocks_hold_the_nearest_quotients(M, N, type):
+    x = (torch.randn(M, N, generator=torch.Generator().manual_seed(N)) * 0.02).to(DT[type])
+    q, s = torch.empty(M, N, dtype=DT["e4m3"], device="cuda"), torch.empty(ceil128(M), ceil128(N), device="cuda")
+    binding.check(binding.quantize_e4m3_blocks(M, N, TYPE[type], x.cuda(), N, q, N, s, ceil128(N), stream()))
+    want = quotients(x.float(), s.cpu().repeat_interleave(128, 0)[:M].repeat_interleave(128, 1)[:, :N])
+    assert torch.equal(bits(q.cpu()), bits(want))
+
+
+@pytest.mark.parametrize("N", [2048, 4096, 8192, 16384, 32768])
+def test_the_norm_holds_the_nearest_quotients(N):
+    """Rows of +-1 and +-7, 11 to 5, have the mean square 16: rstd is 1/4 and y exact in f32, whatever the order of the sum."""
+    M, gen = 24, torch.Generator().manual_seed(N)
+    row = torch.tensor([1.0] * 11 + [7.0] * 5).repeat(N // 16)
+    x = torch.stack([row[torch.randperm(N, generator=gen)] for _ in range(M)]) * (torch.randint(0, 2, (M, N), generator=gen) * 2 - 1)
+    gamma = (1.0 + 0.1 * torch.randn(N, generator=gen)).bfloat16()
+    q, s = torch.empty(M, N, dtype=DT["e4m3"], device="cuda"), torch.empty(N // 128, M, device="cuda")
+    binding.check(binding.rms_norm(M, N, TYPE["bf16"], x.bfloat16().cuda(), N, None, 0, gamma.cuda(), 0.0, None, 0, None, 0, q, N, s, M, None, stream()))
+    want = quotients(x * 0.25 * gamma.float(), s.cpu().t().repeat_interleave(128, 1))
+    assert torch.equal(bits(q.cpu()), bits(want))
