@@ -6,7 +6,7 @@
 // rotations within a row of lanes.  Accesses are at element alignment: rows of any pitch take the same path.
 //
 // Measured (a copy of 1 GiB: 5.15 TB/s): norm of (16384,4096) bf16 with residual and e4m3 output 86.4 us, 5.5 TB/s; 16 rows of 8192 4.5 us, of which a launch
-// and its first load and barrier are all but little; gradients of (8191,4000) 60 us, 4.4 TB/s; SwiGLU (4096,8192) to e4m3 36.1 us, 4.7 TB/s; blocks of
+// and its first load and barrier are all but little; gradients of (8191,4000) 60 us, 4.4 TB/s; SwiGLU (4096,8192) to e4m3 37.2 us, 4.5 TB/s; blocks of
 // (8192,8192) 43 us, 4.7 TB/s.
 #include "ops_device.h"
 #include "../../include/gemm_ops.h"
@@ -367,6 +367,17 @@ int norm_grad_of_type(const NormGradArgs& a, hipStream_t stream)
 // ---- quantisation in rows: a wavefront takes 2048 columns of a row, 512 at a time, 16 lanes a block of 128; a workgroup's four rows'
 // scales are stored together ---------------------------------------------------------------------------------------------------
 constexpr int ROW_PASSES = 4;
+// g / (1 + exp(-g)).  exp(-g) = 2^a 2^r: a = -g / ln 2 as f32 rounds it, r what that leaves (exact product by an fma, and the constant's own next bits),
+// 2^r = 1 + r ln 2 to f32's last bit, as r is below 1e-5 where 2^a is finite.  Without r the error would grow with g, to 4e-6 at 60.  The exponential and reciprocal
+// instructions are good to one unit in the last place each; a denormal reciprocal, of gates below -87.3, is 0.  Beyond +-1024, where the
+// result is 0 or g itself, the exponent is that of +-1024, so that neither a nor r overflows.
+__device__ __forceinline__ float silu(float g)
+{
+    constexpr float LOG2E = 1.4426950408889634f, LOG2E_REST = (float)(1.4426950408889634 - (double)LOG2E), LN2 = 0.6931471805599453f;
+    const float x = __builtin_amdgcn_fmed3f(-g, -1024.0f, 1024.0f), a = x * LOG2E;
+    const float r = __builtin_fmaf(x, LOG2E_REST, __builtin_fmaf(x, LOG2E, -a));
+    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a) * __builtin_fmaf(r, LN2, 1.0f));
+}
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantArgs a)
 {
@@ -390,8 +401,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantArgs a)
         for (int i = 0; i < 8; i++) {
             y[i] = (float)v[p][i];
             if constexpr (ACT == GEMM_OPS_ACT_RELU) y[i] = y[i] < 0.0f ? 0.0f : y[i];
-            // g / (1 + exp(-g)) with the reciprocal instruction (1 ulp)
-            else if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) y[i] = y[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-y[i])) * (float)u[p][i];
+            else if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) y[i] = silu(y[i]) * (float)u[p][i];
             m = max(m, magnitude(y[i]));
         }
         const BlockScale s = block_scale(max16(m));

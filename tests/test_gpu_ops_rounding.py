@@ -1,5 +1,6 @@
 """What the quantisers round, to the bit: an element is the e4m3 value nearest to its f32 value divided by the scale that is stored beside it, ties
-to even."""
+to even; and SwiGLU in f32 to a few units in the last place whatever the gate."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +58,29 @@ def test_the_norm_holds_the_nearest_quotients(N):
     binding.check(binding.rms_norm(M, N, TYPE["bf16"], x.bfloat16().cuda(), N, None, 0, gamma.cuda(), 0.0, None, 0, None, 0, q, N, s, M, None, stream()))
     want = quotients(x * 0.25 * gamma.float(), s.cpu().t().repeat_interleave(128, 1))
     assert torch.equal(bits(q.cpu()), bits(want))
+
+
+@pytest.mark.parametrize("type", ["f16", "bf16"])
+def test_swiglu_is_as_exact_for_every_gate(type):
+    """A block of one gate value and one u: its scale is the magnitude of the result over 448.  f32 has 6e-8 of relative error in each of exp, its
+    argument's correction, 1 + exp, the reciprocal (two units), three products and the scale's division: below 1e-6 together."""
+    g = torch.linspace(-86.0, 86.0, 4001).to(DT[type])
+    M = g.numel()
+    x = torch.cat([g[:, None].expand(M, 128), torch.full((M, 128), 3.0, dtype=DT[type])], 1).contiguous().cuda()
+    q, s = torch.empty(M, 128, dtype=DT["e4m3"], device="cuda"), torch.empty(1, M, device="cuda")
+    binding.check(binding.quantize_e4m3_rows(M, 128, TYPE[type], binding.ACT_SWIGLU, x, 256, q, 128, s, M, stream()))
+    y = g.double().numpy()
+    want = np.maximum(np.abs(y / (1.0 + np.exp(-y)) * 3.0), 2.0 ** -96) / 448.0
+    assert (np.abs(s.cpu().double().numpy()[0] - want) <= 1e-6 * want).all()
+
+
+def test_swiglu_of_the_largest_gates_and_infinities():
+    """exp beyond f32's range: 0 below, the gate itself above; an infinite gate shows in its block."""
+    g = torch.tensor([-3e38, -1e4, -200.0, 200.0, 1e4, 3e38, float("-inf"), float("inf"), float("nan")]).bfloat16()
+    M = g.numel()
+    x = torch.cat([g[:, None].expand(M, 128), torch.ones(M, 128, dtype=torch.bfloat16)], 1).contiguous().cuda()
+    q, s = torch.empty(M, 128, dtype=DT["e4m3"], device="cuda"), torch.empty(1, M, device="cuda")
+    binding.check(binding.quantize_e4m3_rows(M, 128, TYPE["bf16"], binding.ACT_SWIGLU, x, 256, q, 128, s, M, stream()))
+    q, s = q.float().cpu(), s.cpu()[0]
+    assert (q[:3] == 0).all() and (q[3:6] == 448).all() and q[6:].isnan().all() and s[6:].isnan().all()
+    assert torch.equal(s[:3], torch.full((3,), 2.0 ** -96) / 448.0) and torch.equal(s[3:6], g[3:6].float() / 448.0)
