@@ -27,8 +27,16 @@ def _blocks(n):
     return (n + 127) // 128
 
 
-def _stream():
+def _stream(t):
+    """The current stream, for kernels that take `t` and others beside it: memory of the current GPU."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors of the current GPU expected, got one on {t.device}")
     return torch.cuda.current_stream().cuda_stream
+
+
+def _pitch(t):
+    """Elements from one row to the next (of a single row torch keeps any number)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def quantize_weights(w):
@@ -37,7 +45,7 @@ def quantize_weights(w):
     q = torch.empty(w.shape, dtype=E4M3, device=w.device)
     scale = torch.empty(*w.shape[:-2], _blocks(N), _blocks(K), dtype=torch.float32, device=w.device)
     for m, qm, sm in zip(w.reshape(-1, N, K), q.reshape(-1, N, K), scale.reshape(-1, _blocks(N), _blocks(K))):
-        check(binding.quantize_e4m3_blocks(N, K, TYPES[w.dtype], m, m.stride(0), qm, K, sm, _blocks(K), _stream()))
+        check(binding.quantize_e4m3_blocks(N, K, TYPES[w.dtype], m, m.stride(0), qm, K, sm, _blocks(K), _stream(m)))
     return SimpleNamespace(q=q, scale=scale)
 
 
@@ -83,13 +91,21 @@ class ExpertLayer:
         """Sum over each token's rows, in a fixed order, f32."""
         return (rows[route.place].float().view(-1, self.top_k, rows.shape[1]) * route.weight[..., None]).sum(1)
 
+    def _rows(self, name, t, tokens):
+        """A caller's matrix as the kernels take it, which see an address, a pitch and the layer's type.  Rows of any pitch are taken
+        as they lie; a copy is made where a row's elements are apart or rows overlap (an expanded gradient)."""
+        if tuple(t.shape) != (tokens, self.hidden) or t.dtype != self.dtype or t.device != self.gamma.device:
+            raise ValueError(f"{name}: {tokens} x {self.hidden} of {self.dtype} on {self.gamma.device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+        return t if t.stride(1) == 1 and _pitch(t) >= self.hidden else t.contiguous()
+
     def _norm(self, x, r, quantized):
-        T, H = x.shape
-        n = SimpleNamespace(h=torch.empty_like(x), y=torch.empty_like(x), rstd=torch.empty(T, dtype=torch.float32, device=x.device), q=None, scale=None)
+        T, H = x.shape[0], self.hidden
+        x, r = self._rows("x", x, T), self._rows("r", r, T)
+        n = SimpleNamespace(h=torch.empty(T, H, dtype=x.dtype, device=x.device), y=torch.empty(T, H, dtype=x.dtype, device=x.device), rstd=torch.empty(T, dtype=torch.float32, device=x.device), q=None, scale=None)
         if quantized:
             n.q = torch.empty(T, H, dtype=E4M3, device=x.device)
             n.scale = torch.empty(_blocks(H), T, dtype=torch.float32, device=x.device)
-        check(binding.rms_norm(T, H, TYPES[x.dtype], x, x.stride(0), r, r.stride(0), self.gamma, self.eps, n.h, H, n.y, H, n.q, H, n.scale, T, n.rstd, _stream()))
+        check(binding.rms_norm(T, H, TYPES[x.dtype], x, _pitch(x), r, _pitch(r), self.gamma, self.eps, n.h, H, n.y, H, n.q, H, n.scale, T, n.rstd, _stream(x)))
         return n
 
     def _product8(self, q, scale, w, offsets=None):
@@ -97,16 +113,16 @@ class ExpertLayer:
         E, N = w.q.shape[:2]
         c = torch.empty(rows, N, dtype=self.dtype, device=q.device)
         if offsets is None:
-            check(binding.gemm_e4m3_block(rows, N, K, q, K, scale, rows, w.q, K, w.scale, _blocks(K), c, N, TYPES[c.dtype], _stream()))
+            check(binding.gemm_e4m3_block(rows, N, K, q, K, scale, rows, w.q, K, w.scale, _blocks(K), c, N, TYPES[c.dtype], _stream(c)))
         else:
-            check(binding.gemm_e4m3_block_grouped(rows, N, K, E, offsets, q, K, scale, rows, w.q, K, N * K, w.scale, _blocks(K), w.scale.stride(0), c, N, TYPES[c.dtype], _stream()))
+            check(binding.gemm_e4m3_block_grouped(rows, N, K, E, offsets, q, K, scale, rows, w.q, K, N * K, w.scale, _blocks(K), w.scale.stride(0), c, N, TYPES[c.dtype], _stream(c)))
         return c
 
     def _swiglu8(self, u):
         rows, N = u.shape[0], u.shape[1] // 2
         q = torch.empty(rows, N, dtype=E4M3, device=u.device)
         scale = torch.empty(_blocks(N), rows, dtype=torch.float32, device=u.device)
-        check(binding.quantize_e4m3_rows(rows, N, TYPES[u.dtype], binding.ACT_SWIGLU, u, 2 * N, q, N, scale, rows, _stream()))
+        check(binding.quantize_e4m3_rows(rows, N, TYPES[u.dtype], binding.ACT_SWIGLU, u, 2 * N, q, N, scale, rows, _stream(u)))
         return q, scale
 
     def serve(self, x, r):
@@ -122,15 +138,15 @@ class ExpertLayer:
     def _product(self, a, w, offsets):
         (rows, K), (E, _, N) = a.shape, w.shape
         c = torch.empty(rows, N, dtype=a.dtype, device=a.device)
-        check(binding.gemm_grouped(rows, N, K, E, offsets, TYPES[a.dtype], a, K, w, N, K * N, c, N, TYPES[c.dtype], _stream()))
+        check(binding.gemm_grouped(rows, N, K, E, offsets, TYPES[a.dtype], a, K, w, N, K * N, c, N, TYPES[c.dtype], _stream(c)))
         return c
 
     def _product_backward(self, a, w, dc, offsets):
         """Gradients of a (its type) and of w (f32, as an optimizer adds them up)."""
         (rows, K), (E, _, N) = a.shape, w.shape
         da, dw = torch.empty_like(a), torch.empty(w.shape, dtype=torch.float32, device=w.device)
-        check(binding.gemm_grouped_grad_a(rows, N, K, E, offsets, TYPES[a.dtype], dc, N, w, N, K * N, da, K, TYPES[a.dtype], _stream()))
-        check(binding.gemm_grouped_grad_b(rows, N, K, E, offsets, TYPES[a.dtype], a, K, dc, N, dw, N, K * N, TYPES[dw.dtype], _stream()))
+        check(binding.gemm_grouped_grad_a(rows, N, K, E, offsets, TYPES[a.dtype], dc, _pitch(dc), w, N, K * N, da, K, TYPES[a.dtype], _stream(a)))
+        check(binding.gemm_grouped_grad_b(rows, N, K, E, offsets, TYPES[a.dtype], a, K, dc, _pitch(dc), dw, N, K * N, TYPES[dw.dtype], _stream(a)))
         return da, dw
 
     def train_forward(self, x, r):
@@ -154,7 +170,8 @@ class ExpertLayer:
             du = torch.cat([d * v * sig * (1.0 + g * (1.0 - sig)), d * g * sig], dim=-1).to(u.dtype)
             da, dup = self._product_backward(a, up, du, offsets)
             return da, dup, ddown
-        route = s.route
+        route, tokens = s.route, s.h.shape[0]
+        dout, dh = self._rows("dout", dout, tokens), self._rows("dh", dh, tokens)
         dweight = (s.d[route.place].view(-1, self.top_k, self.hidden).float() * dout[:, None].float()).sum(-1)
         weight = torch.empty(route.place.numel(), dtype=torch.float32, device=dout.device)
         weight[route.place] = route.weight.flatten()
@@ -165,7 +182,7 @@ class ExpertLayer:
         dx, dgamma = torch.empty_like(dy), torch.empty(H, dtype=torch.float32, device=dy.device)
         size = binding.rms_norm_grad_workspace_bytes(T, H)
         workspace = torch.empty(size, dtype=torch.uint8, device=dy.device)
-        check(binding.rms_norm_grad(T, H, TYPES[dy.dtype], dy, H, s.h, H, self.gamma, s.rstd, dh, dh.stride(0), dx, H, dgamma, workspace, size, _stream()))
+        check(binding.rms_norm_grad(T, H, TYPES[dy.dtype], dy, H, s.h, H, self.gamma, s.rstd, dh, _pitch(dh), dx, H, dgamma, workspace, size, _stream(dy)))
         return SimpleNamespace(x=dx, gamma=dgamma, up=dup, down=ddown, shared_up=dshared_up, shared_down=dshared_down, weight=dweight)
 
 

@@ -1,0 +1,95 @@
+"""What paper_2108_13191_amd/expert_layer.py hands to the kernels, on the host, where each operand is read by its address, pitch and type: callers' matrices
+of other layouts give what contiguous copies of them give, and other types, shapes and places are refused."""
+import pytest
+import torch
+
+import ops_emulation
+from paper_2108_13191_amd import binding, expert_layer
+
+T, H, F, E, TOP = 13, 264, 136, 4, 2
+
+
+@pytest.fixture
+def layer(monkeypatch):
+    for f in ops_emulation.ENTRY_POINTS:
+        monkeypatch.setattr(binding, f.__name__, f)
+    monkeypatch.setattr(expert_layer, "_stream", lambda *t: 0)
+    made = expert_layer.ExpertLayer(H, F, E, TOP, seed=1, device="cpu")
+    made.prepare()
+    return made
+
+
+def inputs(tokens=T):
+    gen = torch.Generator().manual_seed(2)
+    return [torch.randn(tokens, H, generator=gen).bfloat16() for _ in range(4)]
+
+
+def columns(t):
+    """The same values as columns of a wider matrix, whose other columns are NaN."""
+    wide = torch.full((t.shape[0], H + 40), float("nan"), dtype=t.dtype)
+    wide[:, 16:16 + H] = t
+    return wide[:, 16:16 + H]
+
+
+def last(t):
+    """... as the last columns of a matrix, behind which nothing follows."""
+    wide = torch.full((t.shape[0], 2 * H), float("nan"), dtype=t.dtype)
+    wide[:, H:] = t
+    return wide[:, H:]
+
+
+def transposed(t):
+    return t.t().contiguous().t()
+
+
+def every_other(t):
+    return torch.stack([t, torch.full_like(t, float("nan"))], 2)[:, :, 0]
+
+
+def same(a, b):
+    a, b = vars(a), vars(b)
+    assert a.keys() == b.keys()
+    return all(torch.equal(a[n], b[n]) if isinstance(a[n], torch.Tensor) else n == "route" and same(a[n], b[n]) for n in a if a[n] is not None)
+
+
+@pytest.mark.parametrize("lay", [columns, last, transposed, every_other])
+@pytest.mark.parametrize("tokens", [1, T])
+def test_matrices_of_any_layout(layer, lay, tokens):
+    x, r, dout, dh = inputs(tokens)
+    served, s = layer.serve(x, r), layer.train_forward(x, r)
+    grads = layer.backward(s, dout, dh)
+    x, r, dout, dh = map(lay, (x, r, dout, dh))
+    assert same(layer.serve(x, r), served)
+    s2 = layer.train_forward(x, r)
+    assert same(s2, s) and same(layer.backward(s2, dout, dh), grads)
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (1, H), (T, 1)])
+def test_expanded_gradients(layer, shape):
+    """As the gradient of a sum comes: one element or row in place of all of them."""
+    x, r, _, _ = inputs()
+    s = layer.train_forward(x, r)
+    d = torch.randn(shape, generator=torch.Generator().manual_seed(3)).bfloat16().expand(T, H)
+    assert same(layer.backward(s, d, d), layer.backward(s, d.contiguous(), d.contiguous()))
+
+
+def test_other_types_shapes_and_places_are_refused(layer):
+    x, r, dout, dh = inputs()
+    s = layer.train_forward(x, r)
+    for bad in (lambda t: t.float(), lambda t: t.half(), lambda t: t[:, :-8], lambda t: t[None], lambda t: t.to("meta")):
+        for call in (lambda b: layer.serve(b(x), r), lambda b: layer.serve(x, b(r)), lambda b: layer.train_forward(b(x), r), lambda b: layer.train_forward(x, b(r)),
+                     lambda b: layer.backward(s, b(dout), dh), lambda b: layer.backward(s, dout, b(dh))):
+            with pytest.raises(ValueError):
+                call(bad)
+    for call in (lambda: layer.serve(x, r[1:]), lambda: layer.backward(s, dout[1:], dh), lambda: layer.backward(s, dout, dh[1:])):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_host_memory_is_no_operand():
+    """Nothing is launched on tensors that no kernel could read."""
+    made = expert_layer.ExpertLayer(H, F, E, TOP, device="cpu")
+    x, r, _, _ = inputs()
+    for call in (lambda: made.train_forward(x, r), made.prepare):
+        with pytest.raises(ValueError):
+            call()
