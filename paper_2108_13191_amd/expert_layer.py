@@ -42,10 +42,11 @@ def _pitch(t):
 def quantize_weights(w):
     """w (E x N x K or N x K) -> e4m3 of the same shape, scales E x ceil(N / 128) x ceil(K / 128)."""
     N, K = w.shape[-2:]
+    w = w if w.stride(-1) == 1 and w.stride(-2) >= K else w.contiguous()
     q = torch.empty(w.shape, dtype=E4M3, device=w.device)
     scale = torch.empty(*w.shape[:-2], _blocks(N), _blocks(K), dtype=torch.float32, device=w.device)
     for m, qm, sm in zip(w.reshape(-1, N, K), q.reshape(-1, N, K), scale.reshape(-1, _blocks(N), _blocks(K))):
-        check(binding.quantize_e4m3_blocks(N, K, TYPES[w.dtype], m, m.stride(0), qm, K, sm, _blocks(K), _stream(m)))
+        check(binding.quantize_e4m3_blocks(N, K, TYPES[w.dtype], m, _pitch(m), qm, K, sm, _blocks(K), _stream(m)))
     return SimpleNamespace(q=q, scale=scale)
 
 
@@ -65,12 +66,12 @@ class ExpertLayer:
 
         def random(*shape, scale):
             return (torch.randn(*shape, generator=gen, device=device) * scale).to(dtype)
+        self._shapes = {"gamma": (hidden,), "up": (experts, hidden, 2 * ffn), "down": (experts, ffn, hidden), "shared_up": (1, hidden, 2 * ffn), "shared_down": (1, ffn, hidden)}
         self.gamma = (1.0 + 0.1 * torch.randn(hidden, generator=gen, device=device)).to(dtype)
         self.router = random(hidden, experts, scale=hidden ** -0.5)
-        self.up = random(experts, hidden, 2 * ffn, scale=hidden ** -0.5)
-        self.down = random(experts, ffn, hidden, scale=ffn ** -0.5)
-        self.shared_up = random(1, hidden, 2 * ffn, scale=hidden ** -0.5)
-        self.shared_down = random(1, ffn, hidden, scale=ffn ** -0.5)
+        for name in ("up", "down", "shared_up", "shared_down"):
+            shape = self._shapes[name]
+            setattr(self, name, random(*shape, scale=shape[1] ** -0.5))
 
     def prepare(self):
         """The weights in e4m3, a row for each output."""
@@ -98,7 +99,15 @@ class ExpertLayer:
             raise ValueError(f"{name}: {tokens} x {self.hidden} of {self.dtype} on {self.gamma.device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
         return t if t.stride(1) == 1 and _pitch(t) >= self.hidden else t.contiguous()
 
+    def _check_weights(self, *names):
+        """They may have been replaced: the kernels read them as the constructor lays them out."""
+        for name in names:
+            w = getattr(self, name)
+            if tuple(w.shape) != self._shapes[name] or w.dtype != self.dtype or w.device != self.gamma.device or not w.is_contiguous():
+                raise ValueError(f"{name}: {self._shapes[name]} of {self.dtype}, contiguous, on {self.gamma.device} expected")
+
     def _norm(self, x, r, quantized):
+        self._check_weights("gamma")
         T, H = x.shape[0], self.hidden
         x, r = self._rows("x", x, T), self._rows("r", r, T)
         n = SimpleNamespace(h=torch.empty(T, H, dtype=x.dtype, device=x.device), y=torch.empty(T, H, dtype=x.dtype, device=x.device), rstd=torch.empty(T, dtype=torch.float32, device=x.device), q=None, scale=None)
@@ -151,6 +160,7 @@ class ExpertLayer:
 
     def train_forward(self, x, r):
         """h, out and what `backward` needs."""
+        self._check_weights(*self._shapes)
         s = self._norm(x, r, quantized=False)
         s.route = self.route(s.y)
         s.all = torch.arange(2, dtype=torch.int32, device=x.device) * x.shape[0]      # the shared expert: one group
@@ -170,6 +180,7 @@ class ExpertLayer:
             du = torch.cat([d * v * sig * (1.0 + g * (1.0 - sig)), d * g * sig], dim=-1).to(u.dtype)
             da, dup = self._product_backward(a, up, du, offsets)
             return da, dup, ddown
+        self._check_weights(*self._shapes)
         route, tokens = s.route, s.h.shape[0]
         dout, dh = self._rows("dout", dout, tokens), self._rows("dh", dh, tokens)
         dweight = (s.d[route.place].view(-1, self.top_k, self.hidden).float() * dout[:, None].float()).sum(-1)

@@ -93,3 +93,26 @@ def test_host_memory_is_no_operand():
     for call in (lambda: made.train_forward(x, r), made.prepare):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("lay", [lambda w: w, lambda w: w.transpose(-1, -2).contiguous().transpose(-1, -2), lambda w: w.expand(3, *w.shape[-2:]),
+                                 lambda w: torch.cat([w, w], -1)[..., :w.shape[-1]]], ids=["contiguous", "transposed", "expanded", "columns"])
+def test_weights_of_any_layout_are_quantised(layer, lay):
+    w = lay(torch.randn(1, 136, 264, generator=torch.Generator().manual_seed(4)).bfloat16())
+    got, want = expert_layer.quantize_weights(w), expert_layer.quantize_weights(w.clone(memory_format=torch.contiguous_format))
+    assert torch.equal(got.q.view(torch.uint8), want.q.view(torch.uint8)) and torch.equal(got.scale, want.scale)
+    assert torch.equal(expert_layer.quantize_weights(w[0]).scale, want.scale[0])
+
+
+@pytest.mark.parametrize("name", ["up", "down", "shared_up", "shared_down", "gamma"])
+def test_weights_that_are_no_weights_are_refused(layer, name):
+    """A weight that was replaced by one of another type, shape or layout than products read."""
+    x, r, dout, dh = inputs()
+    s, good = layer.train_forward(x, r), getattr(layer, name)
+    for bad in (good.float(), good[..., :-8], torch.stack([good, good], -1)[..., 0]):
+        setattr(layer, name, bad)
+        for call in (lambda: layer.train_forward(x, r), lambda: layer.backward(s, dout, dh)):
+            with pytest.raises(ValueError):
+                call()
+    setattr(layer, name, good)
+    layer.backward(layer.train_forward(x, r), dout, dh)
