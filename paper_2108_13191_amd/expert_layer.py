@@ -4,7 +4,7 @@
     out[t] = swiglu(y[t] W_up) W_down  of a shared expert  +  sum over the top_k experts e of token t:  weight[t, e] * (the same with W_up[e], W_down[e])
 
 `serve` runs it in e4m3: the norm writes y quantised, the experts' products read it, SwiGLU writes its result quantised for the second
-products.  `train_forward` and `backward` run it in 16 bits.  What is left to torch: the router's small product and
+products.  `train_forward` and `train_backward` run it in 16 bits.  What is left to torch: the router's small product and
 selection, moving rows into the experts' order and back, and SwiGLU in 16 bits.  Memory comes from torch; nothing synchronises with the host.
 
     python -m paper_2108_13191_amd.expert_layer --tokens 4096 --hidden 4096 --ffn 2048 --experts 8 --top-k 2
@@ -66,7 +66,7 @@ class ExpertLayer:
 
         def random(*shape, scale):
             return (torch.randn(*shape, generator=gen, device=device) * scale).to(dtype)
-        self._shapes = {"gamma": (hidden,), "up": (experts, hidden, 2 * ffn), "down": (experts, ffn, hidden), "shared_up": (1, hidden, 2 * ffn), "shared_down": (1, ffn, hidden)}
+        self._shapes = {"gamma": (hidden,), "router": (hidden, experts), "up": (experts, hidden, 2 * ffn), "down": (experts, ffn, hidden), "shared_up": (1, hidden, 2 * ffn), "shared_down": (1, ffn, hidden)}
         self.gamma = (1.0 + 0.1 * torch.randn(hidden, generator=gen, device=device)).to(dtype)
         self.router = random(hidden, experts, scale=hidden ** -0.5)
         for name in ("up", "down", "shared_up", "shared_down"):
@@ -171,8 +171,16 @@ class ExpertLayer:
         s.out = (self._combine(s.d, s.route) + shared.float()).to(self.dtype)
         return s
 
+    def train_backward(self, s, dout, dh):
+        """From the gradients of out and h: of x (and of r), gamma, the router, the experts' and the shared weights; and of the routing weights."""
+        return self._backward(s, dout, dh, through_router=True)
+
     def backward(self, s, dout, dh):
-        """From the gradients of out and h: of x (and of r), gamma, the experts' and the shared weights, and the routing weights."""
+        """The same with the routing weights held, as a router of the caller's own needs it: x and gamma without what reaches them through the
+        weights, whose gradient is `weight`; none of the router."""
+        return self._backward(s, dout, dh, through_router=False)
+
+    def _backward(self, s, dout, dh, through_router):
         def expert(a, u, sw, up, down, dd, offsets):
             ds, ddown = self._product_backward(sw, down, dd, offsets)
             (g, v), d = u.float().chunk(2, dim=-1), ds.float()
@@ -188,13 +196,19 @@ class ExpertLayer:
         weight[route.place] = route.weight.flatten()
         da, dup, ddown = expert(s.a, s.u, s.s, self.up, self.down, (dout[route.source].float() * weight[:, None]).to(self.dtype), route.offsets)
         dy, dshared_up, dshared_down = expert(s.shared_a, s.shared_u, s.shared_s, self.shared_up, self.shared_down, dout, s.all)
-        dy = (dy.float() + da[route.place].view(-1, self.top_k, self.hidden).float().sum(1)).to(self.dtype)
+        dy, router = dy.float() + da[route.place].view(-1, self.top_k, self.hidden).float().sum(1), {}
+        if through_router:
+            # top-k of a softmax, divided by their sum: the softmax of the chosen logits alone.  dlogit = weight (dweight - sum(weight dweight)); others' are 0
+            dchosen = route.weight * (dweight - (route.weight * dweight).sum(-1, keepdim=True))
+            dlogits = torch.zeros(tokens, self.experts, device=dy.device).scatter_(1, route.expert, dchosen)
+            dy, router = dy + dlogits @ self.router.float().t(), {"router": s.y.float().t() @ dlogits}
+        dy = dy.to(self.dtype)
         T, H = dy.shape
         dx, dgamma = torch.empty_like(dy), torch.empty(H, dtype=torch.float32, device=dy.device)
         size = binding.rms_norm_grad_workspace_bytes(T, H)
         workspace = torch.empty(size, dtype=torch.uint8, device=dy.device)
         check(binding.rms_norm_grad(T, H, TYPES[dy.dtype], dy, H, s.h, H, self.gamma, s.rstd, dh, _pitch(dh), dx, H, dgamma, workspace, size, _stream(dy)))
-        return SimpleNamespace(x=dx, gamma=dgamma, up=dup, down=ddown, shared_up=dshared_up, shared_down=dshared_down, weight=dweight)
+        return SimpleNamespace(x=dx, gamma=dgamma, up=dup, down=ddown, shared_up=dshared_up, shared_down=dshared_down, weight=dweight, **router)
 
 
 def main(argv=None):
@@ -218,7 +232,7 @@ def main(argv=None):
         end.synchronize()
         return begin.elapsed_time(end) / a.steps
     products = 6.0 * a.tokens * (a.top_k + 1) * a.hidden * a.ffn
-    forward, both = time(lambda: layer.serve(x, r)), time(lambda: layer.backward(layer.train_forward(x, r), dout, dh))
+    forward, both = time(lambda: layer.serve(x, r)), time(lambda: layer.train_backward(layer.train_forward(x, r), dout, dh))
     print(f"{a.tokens} tokens, hidden {a.hidden}, ffn {a.ffn}, top {a.top_k} of {a.experts} experts and a shared one")
     print(f"serve, e4m3:               {forward:8.3f} ms, {products / forward * 1e-9:7.1f} TFLOP/s in the products")
     print(f"train, bf16, both ways:    {both:8.3f} ms, {3 * products / both * 1e-9:7.1f} TFLOP/s in the products")

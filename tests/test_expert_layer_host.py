@@ -116,3 +116,16 @@ def test_weights_that_are_no_weights_are_refused(layer, name):
                 call()
     setattr(layer, name, good)
     layer.backward(layer.train_forward(x, r), dout, dh)
+
+
+@pytest.mark.parametrize("lay", [columns, transposed])
+def test_the_whole_derivative_adds_what_the_router_carries(layer, lay):
+    x, r, dout, dh = inputs()
+    s = layer.train_forward(x, r)
+    held, whole = layer.backward(s, dout, dh), layer.train_backward(s, lay(dout), lay(dh))
+    for name in ("up", "down", "shared_up", "shared_down", "weight"):
+        assert torch.equal(getattr(held, name), getattr(whole, name)), name
+    assert not hasattr(held, "router") and whole.router.shape == layer.router.shape and whole.router.dtype == torch.float32
+    assert not torch.equal(held.x, whole.x) and not torch.equal(held.gamma, whole.gamma)
+    # a shift of a token's logits changes nothing: the gradient of a token's logits sums to 0
+    assert (whole.router.sum(1).abs() <= 1e-4 * whole.router.abs().sum(1)).all()
