@@ -129,3 +129,24 @@ def test_the_whole_derivative_adds_what_the_router_carries(layer, lay):
     assert not torch.equal(held.x, whole.x) and not torch.equal(held.gamma, whole.gamma)
     # a shift of a token's logits changes nothing: the gradient of a token's logits sums to 0
     assert (whole.router.sum(1).abs() <= 1e-4 * whole.router.abs().sum(1)).all()
+
+
+@pytest.mark.parametrize("hidden,ffn", [(264, 136), (256, 136), (264, 128), (256, 128), (8, 8)])
+def test_e4m3_rows_begin_at_multiples_of_16(layer, monkeypatch, hidden, ffn):
+    """Whatever the widths: the products' fast kernels need it of addresses, pitches and the experts' strides."""
+    calls = []
+
+    def watch(f):
+        def g(*args):
+            names = dict(zip(f.__code__.co_varnames, args))
+            calls.append(f.__name__)
+            for t in "AB":
+                assert names["ld" + t.lower()] % 16 == 0 and names[t].data_ptr() % 16 == 0 and names.get("b_stride", 0) % 16 == 0
+            return f(*args)
+        return g
+    for f in (ops_emulation.gemm_e4m3_block, ops_emulation.gemm_e4m3_block_grouped):
+        monkeypatch.setattr(binding, f.__name__, watch(f))
+    made = expert_layer.ExpertLayer(hidden, ffn, E, TOP, seed=1, device="cpu")
+    made.prepare()
+    made.serve(*(torch.randn(T, hidden).bfloat16() for _ in range(2)))
+    assert calls.count("gemm_e4m3_block") == 2 and calls.count("gemm_e4m3_block_grouped") == 2
