@@ -160,6 +160,14 @@ int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
                         const void* A, int64_t lda, const void* dC, int64_t lddc,
                         void* dB, int64_t lddb, int64_t db_stride, int64_t b_type, void* stream);
 
+/*
+ * The kernel that a product runs on, by name, for tests and traces: nothing is launched.  E < 0: gemm_e4m3_block.  lda, ldb: the
+ * pitches of the operands that are read (A or dC, B or dC); addresses and the experts' strides are taken as multiples of 16 bytes.  NULL: sizes that
+ * are refused or leave nothing to run.
+ */
+enum { GEMM_OPS_E4M3 = 0, GEMM_OPS_FORWARD = 1, GEMM_OPS_GRAD_A = 2, GEMM_OPS_GRAD_B = 3 };
+const char* gemm_ops_form(int64_t product, int64_t T, int64_t N, int64_t K, int64_t E, int64_t lda, int64_t ldb, int64_t c_type);
+
 #ifdef __cplusplus
 }
 #endif

@@ -116,6 +116,8 @@ def load() -> ctypes.CDLL:
             setattr(lib, name + "_address", ctypes.cast(f, vp).value)
         lib.rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
         lib.rms_norm_grad_workspace_bytes.restype = i64
+        lib.gemm_ops_form.argtypes = [i64] * 8
+        lib.gemm_ops_form.restype = ctypes.c_char_p
         # where the entry points are, for _fastcall
         for name in ("gemm_f16_f32acc", "gemm_f16_f16acc", "gemm_f16_f16acc_static_workspace", "gemm_f16_f32acc_bias_act",
                      "gemm_f16_f16acc_bias_act", "gemm_f16_f16acc_workspace"):
@@ -193,7 +195,7 @@ def gemm_f16_f16acc_bias_act(M, N, K, A, lda, B, ldb, C, ldc, bias, act, stream=
 
 
 # ---- include/gemm_ops.h: the operators around the products of a transformer layer.  Matrices and pitches in elements; every function
-# but the last returns the library's status code.
+# but the last two returns the library's status code.
 
 TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
 ACT_SWIGLU = 2
@@ -259,6 +261,15 @@ def gemm_grouped_grad_b(T, N, K, E, offsets, type, A, lda, dC, lddc, dB, lddb, d
 def rms_norm_grad_workspace_bytes(M, N) -> int:
     """Bytes of workspace that rms_norm_grad needs to form dgamma."""
     return load().rms_norm_grad_workspace_bytes(M, N)
+
+
+PRODUCT_E4M3, PRODUCT_FORWARD, PRODUCT_GRAD_A, PRODUCT_GRAD_B = 0, 1, 2, 3
+
+
+def product_form(product, T, N, K, E, lda, ldb, c_type):
+    """The name of the kernel that a product would run on (E < 0: gemm_e4m3_block), None where there is nothing to run."""
+    name = load().gemm_ops_form(product, T, N, K, E, lda, ldb, c_type)
+    return name.decode() if name else None
 
 
 def strerror(code: int) -> str:

@@ -34,15 +34,22 @@ double expected_tiles(const OpsGemm& g, int bm, int bn)
     return (g.M / (double)bm + groups * (rows < bm ? 1.0 - 0.5 * rows / bm : 0.5)) * tn;
 }
 
-// The choice of kernel; us measured for the one taken | the other, groups as a random router deals them.
-int launch(const OpsGemm& g)
+// What a product runs on: the kernel for any alignment, the tiled one, or the one for few rows on 16 fm x 16 nb results a workgroup.
+struct Form {
+    enum Kernel { ANY, TILES, FEW_ROWS } kernel;
+    OpsTile tile;
+    int fm, nb;
+};
+Form any_alignment() { return {Form::ANY, TILE_256, 0, 0}; }
+Form tiles(OpsTile t) { return {Form::TILES, t, 0, 0}; }
+Form few_rows(int fm, int nb) { return {Form::FEW_ROWS, TILE_256, fm, nb}; }
+
+// The choice of it; us measured for the one taken | the other, groups as a random router deals them.
+Form choose(const OpsGemm& g)
 {
-    if (!tiles_take(g)) return ops_launch_generic(g);
-    if (!is_aligned(g)) {
-        // a form that loads 8 elements at any alignment needs rows that have them
-        if (g.elem == ELEM_E4M3 || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8) return ops_launch_generic(g);
-        return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, TILE_128_ANY) : ops_launch_tiles_bf16(g, TILE_128_ANY);
-    }
+    if (!tiles_take(g)) return any_alignment();
+    // (a form that loads 8 elements at any alignment needs rows that have them)
+    if (!is_aligned(g)) return g.elem == ELEM_E4M3 || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8 ? any_alignment() : tiles(TILE_128_ANY);
     const int cus = chip().cus;
     const double rows = (double)g.M / g.E;                                  // of a group
     if (g.k_ragged) {
@@ -50,9 +57,8 @@ int launch(const OpsGemm& g)
         // (16384, 4096 x 2048, 8) 1024 tiles 505 | 563; below one: B's alone, (16384, 2304 x 768, 8) 216 tiles 89 | 77, (2048 x 1024, 4) 128 tiles 139 | 91.
         // Between, with many rows a group, (16384, 4096 x 2048, 3) 384 tiles 231 | 277, (2048 x 2048, 5) 320 tiles 146 | 151, with few (4000, 1408 x 2048, 8) 46 | 40; and
         // one round of a single group's, whose operands 128 x 128 tiles read too often: (16384, 4096 x 4096, 1) 380 | 602, (1000, ..) 40 | 43
-        const double tiles = expected_tiles(g, 256, 256);
-        const OpsTile t = tiles >= 2.0 * cus || (tiles >= 1.25 * cus && (double)g.K / g.E >= 1024.0) || tiles >= (double)g.E * cus ? TILE_256 : TILE_128;
-        return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, t) : ops_launch_tiles_bf16(g, t);
+        const double n = expected_tiles(g, 256, 256);
+        return tiles(n >= 2.0 * cus || (n >= 1.25 * cus && (double)g.K / g.E >= 1024.0) || n >= (double)g.E * cus ? TILE_256 : TILE_128);
     }
     // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
     // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
@@ -65,7 +71,7 @@ int launch(const OpsGemm& g)
             // the widest tiles that give every compute unit one: (16,8192,8192) 32 columns 13.6, 16 columns 17.1; (16,2048,8192) 13.1, 9.6;
             // (64,8192,8192) 64 columns 25.8, 32 columns 32; (64,4096,4096) 14.8, 10.4
             const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
-            return ops_launch_skinny_e4m3(g, fm, nb);
+            return few_rows(fm, nb);
         }
         // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 437 us, (1593,7232,4552) 65 against 134 widened.
         // Below 2^22 results the widened form costs little or nothing more.  256 x 256 | 128 x 128: groups of 1024 rows
@@ -73,22 +79,68 @@ int launch(const OpsGemm& g)
         // of 128 rows (2048,2048) 173 | 158 (widened 251); one round that is half full (4000,2304,6000) 71 | 88
         if (g.c_type != ELEM_F32 && (int64_t)g.M * g.N >= (1 << 22)) {
             const double rounds = expected_tiles(g, 256, 256) / cus;
-            return ops_launch_tiles_e4m3(g, large && rounds >= (rounds > 1.0 ? 0.75 : 0.5) * ceil(rounds) ? TILE_256 : TILE_128_FAST);
+            return tiles(large && rounds >= (rounds > 1.0 ? 0.75 : 0.5) * ceil(rounds) ? TILE_256 : TILE_128_FAST);
         }
         // groups that leave quarters of 128 rows empty, with | without a branch around those: 24 rows each of 16 experts (4096,2048) 39 | 46, 32 rows
         // 41 | 46, 30 rows of 64 (1408,2048) 58 | 65, 48 rows 56 | 56, 100 rows 67 | 62
-        if (g.offsets && rows <= 40.0) return ops_launch_tiles_e4m3(g, TILE_128_SHORT);
+        if (g.offsets && rows <= 40.0) return tiles(TILE_128_SHORT);
         // Up to a round of 128 x 128 ones, one a compute unit: those in registers for one | two, 2048^3 22 | 23, (512,8192,8192) 70 | 75.
-        if (expected_tiles(g, 128, 128) <= cus) return ops_launch_tiles_e4m3(g, TILE_128);
+        if (expected_tiles(g, 128, 128) <= cus) return tiles(TILE_128);
         // 256 x 128 | 128 x 128, two a compute unit: a round of the former (2048,3000,2048) 35 | 36; full rounds and long sums 4000^3 129 | 134; else (3000,3000,2048)
         // 66 | 53, (4096,8192,1024) 90 | 79, (8192,8192,256) 88 | 67, (13785,15296,400) 397 | 328, 16384 rows of 32 experts (2048,512) 66 | 56
         const double rounds = expected_tiles(g, 256, 128) / cus;
         const bool tall = rows >= 192.0 && (rounds <= 1.0 || (g.K > 2048 && rounds >= 0.9 * ceil(rounds)));
-        return ops_launch_tiles_e4m3(g, tall ? TILE_256x128 : TILE_128_PAIR);
+        return tiles(tall ? TILE_256x128 : TILE_128_PAIR);
     }
     // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
-    const OpsTile t = large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128;
-    return g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, t) : ops_launch_tiles_bf16(g, t);
+    return tiles(large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128);
+}
+
+int launch(const OpsGemm& g)
+{
+    const Form f = choose(g);
+    if (f.kernel == Form::ANY) return ops_launch_generic(g);
+    if (f.kernel == Form::FEW_ROWS) return ops_launch_skinny_e4m3(g, f.fm, f.nb);
+    return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, f.tile) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, f.tile) : ops_launch_tiles_bf16(g, f.tile);
+}
+
+const char* name_of(const OpsGemm& g, const Form& f)
+{
+    if (f.kernel == Form::ANY) return "any_alignment_64x64";
+    if (f.kernel == Form::FEW_ROWS)
+        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : "few_rows_16x32") : f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
+    const bool e4m3 = g.elem == ELEM_E4M3;
+    switch (f.tile) {
+    case TILE_256: return e4m3 ? "e4m3_256x256" : "256x256";
+    case TILE_128_FAST: return "e4m3_128x128";
+    case TILE_256x128: return "widened_256x128";
+    case TILE_128_PAIR: return "widened_128x128_two";
+    case TILE_128_SHORT: return "widened_128x128_short_groups";
+    case TILE_128x256: return "128x256";
+    case TILE_128_ANY: return "any_alignment_128x128";
+    case TILE_128: return e4m3 ? "widened_128x128" : "128x128";
+    }
+    return nullptr;
+}
+
+// The sizes of a call as the kernels have them: M x N x K, the sum over K.
+OpsGemm shaped(int64_t product, int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, int64_t c_type, void* stream)
+{
+    OpsGemm g = {};
+    // grad A: rows of dC by rows of B[e], the sum runs over the N that both have contiguous; grad B: columns of A by columns of dC over the group's rows
+    g.M = (int)(product == GEMM_OPS_GRAD_B ? K : T);
+    g.N = (int)(product == GEMM_OPS_GRAD_A ? K : N);
+    g.K = (int)(product == GEMM_OPS_GRAD_A ? N : product == GEMM_OPS_GRAD_B ? T : K);
+    g.E = E < 0 ? 1 : (int)E;
+    g.offsets = offsets;
+    g.elem = product == GEMM_OPS_E4M3 ? (int)ELEM_E4M3 : (int)type;
+    g.c_type = (int)c_type;
+    g.a_kc = product != GEMM_OPS_GRAD_B;
+    g.b_kc = product == GEMM_OPS_E4M3 || product == GEMM_OPS_GRAD_A;
+    g.k_ragged = product == GEMM_OPS_GRAD_B;
+    g.num_xcd = chip().xcds;
+    g.stream = (hipStream_t)stream;
+    return g;
 }
 
 // The e4m3 products.  E < 0: one product, nothing grouped.
@@ -103,35 +155,19 @@ int run_e4m3(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
     if (K > 0 && (bad_pitch(ld_as, M) || bad_pitch(ld_bs, blocks128(K)))) return GEMM_F16_ERR_PITCH;
     if (!C || (E > 0 && !offsets) || (K > 0 && (!A || !B || !sa || !sb))) return GEMM_F16_ERR_NULL;
     if (unaligned(C, type_size(c_type)) || unaligned(sa, 4) || unaligned(sb, 4) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
-    OpsGemm g = {};
-    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.E = E < 0 ? 1 : (int)E;
-    g.offsets = offsets;
+    OpsGemm g = shaped(GEMM_OPS_E4M3, M, N, K, E, offsets, 0, c_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride;
     g.C = (char*)C; g.ldc = ldc;
     g.sa = sa; g.ld_sa = ld_as; g.sb = sb; g.ld_sb = ld_bs; g.sb_stride = bs_stride;
-    g.elem = ELEM_E4M3; g.c_type = (int)c_type; g.a_kc = g.b_kc = true;
-    g.num_xcd = chip().xcds;
-    g.stream = (hipStream_t)stream;
     return launch(g);
 }
 
-// What the 16-bit products grouped by expert share: checks and parameters
+// What the 16-bit products grouped by expert share
 int check_grouped(int64_t T, int64_t N, int64_t K, int64_t E, int64_t type, int64_t out_type)
 {
     if (bad_size(T) || bad_size(N) || bad_size(K) || E < 0 || E > 65535) return GEMM_F16_ERR_SIZE;
     if (!is_16bit(type) || (out_type != type && out_type != GEMM_TYPE_F32)) return GEMM_F16_ERR_CONFIG;
     return GEMM_F16_OK;
-}
-
-OpsGemm grouped_params(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t type, int64_t c_type, void* stream)
-{
-    OpsGemm g = {};
-    g.M = (int)M; g.N = (int)N; g.K = (int)K; g.E = (int)E;
-    g.offsets = offsets;
-    g.elem = (int)type; g.c_type = (int)c_type;
-    g.num_xcd = chip().xcds;
-    g.stream = (hipStream_t)stream;
-    return g;
 }
 
 }  // namespace
@@ -222,9 +258,8 @@ int gemm_grouped(int64_t T, int64_t N, int64_t K, int64_t E, const int32_t* offs
     if (bad_pitch(lda, K) || bad_pitch(ldb, N) || bad_pitch(ldc, N) || b_stride < 0) return GEMM_F16_ERR_PITCH;
     if (!C || !offsets || (K > 0 && (!A || !B))) return GEMM_F16_ERR_NULL;
     if (unaligned(A, 2) || unaligned(B, 2) || unaligned(C, type_size(c_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
-    OpsGemm g = grouped_params(T, N, K, E, offsets, type, c_type, stream);
+    OpsGemm g = shaped(GEMM_OPS_FORWARD, T, N, K, E, offsets, type, c_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)C; g.ldc = ldc;
-    g.a_kc = true; g.b_kc = false;
     return launch(g);
 }
 
@@ -237,10 +272,8 @@ int gemm_grouped_grad_a(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
     if (bad_pitch(lddc, N) || bad_pitch(ldb, N) || bad_pitch(ldda, K) || b_stride < 0) return GEMM_F16_ERR_PITCH;
     if (!dA || !offsets || (N > 0 && (!dC || !B))) return GEMM_F16_ERR_NULL;
     if (unaligned(dC, 2) || unaligned(B, 2) || unaligned(dA, type_size(a_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
-    // rows of dC by rows of B[e]: the sum runs over the N that both have contiguous
-    OpsGemm g = grouped_params(T, K, N, E, offsets, type, a_type, stream);
+    OpsGemm g = shaped(GEMM_OPS_GRAD_A, T, N, K, E, offsets, type, a_type, stream);
     g.A = (const char*)dC; g.lda = lddc; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride; g.C = (char*)dA; g.ldc = ldda;
-    g.a_kc = true; g.b_kc = true;
     return launch(g);
 }
 
@@ -253,11 +286,20 @@ int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
     if (bad_pitch(lda, K) || bad_pitch(lddc, N) || bad_pitch(lddb, N) || (E > 1 && db_stride < (K - 1) * lddb + N)) return GEMM_F16_ERR_PITCH;
     if (!dB || !offsets || (T > 0 && (!A || !dC))) return GEMM_F16_ERR_NULL;
     if (unaligned(A, 2) || unaligned(dC, 2) || unaligned(dB, type_size(b_type)) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
-    // columns of A by columns of dC: the sum runs over the group's rows
-    OpsGemm g = grouped_params(K, N, T, E, offsets, type, b_type, stream);
+    OpsGemm g = shaped(GEMM_OPS_GRAD_B, T, N, K, E, offsets, type, b_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)dC; g.ldb = lddc; g.C = (char*)dB; g.ldc = lddb; g.c_stride = db_stride;
-    g.a_kc = false; g.b_kc = false; g.k_ragged = true;
     return launch(g);
+}
+
+const char* gemm_ops_form(int64_t product, int64_t T, int64_t N, int64_t K, int64_t E, int64_t lda, int64_t ldb, int64_t c_type)
+{
+    if (product < GEMM_OPS_E4M3 || product > GEMM_OPS_GRAD_B || bad_size(T) || bad_size(N) || bad_size(K) || E > 65535 || (E < 0 && product != GEMM_OPS_E4M3)) return nullptr;
+    if (E == 0 || (!is_16bit(c_type) && c_type != GEMM_TYPE_F32)) return nullptr;
+    static const int32_t some_offsets = 0;
+    OpsGemm g = shaped(product, T, N, K, E, E < 0 ? nullptr : &some_offsets, GEMM_TYPE_F16, c_type, nullptr);
+    if (g.M == 0 || g.N == 0) return nullptr;
+    g.lda = lda; g.ldb = ldb;
+    return name_of(g, choose(g));
 }
 
 }  // extern "C"

@@ -1,0 +1,63 @@
+"""Which kernel form a product of include/gemm_ops.h runs on, without a GPU: that the shapes which the GPU tests hold for a form reach it, that every form has some, and the
+lines between the forms."""
+import pytest
+
+import ops_form_cases as cases
+from paper_2108_13191_amd import binding
+from paper_2108_13191_amd.binding import PRODUCT_E4M3, PRODUCT_FORWARD, PRODUCT_GRAD_A, PRODUCT_GRAD_B, TYPE_BF16, TYPE_F16, TYPE_F32, product_form
+
+TYPE = {"f16": TYPE_F16, "bf16": TYPE_BF16, "f32": TYPE_F32}
+
+
+def up(n, to):
+    return (n + to - 1) // to * to
+
+
+def e4m3(rows, N, K, c):
+    T, E = (rows, -1) if isinstance(rows, int) else (sum(rows) + cases.EXTRA, len(rows))
+    return product_form(PRODUCT_E4M3, T, N, K, E, up(K, 16), up(K, 16), TYPE[c])
+
+
+def grouped(product, rows, N, K, pad=8):
+    lda, ldb = {PRODUCT_FORWARD: (K, N), PRODUCT_GRAD_A: (N, N), PRODUCT_GRAD_B: (K, N)}[product]
+    return product_form(product, sum(rows) + cases.EXTRA, N, K, len(rows), up(lda, pad), up(ldb, pad), TYPE_F32)
+
+
+@pytest.mark.parametrize("form,rows,N,K,c", cases.E4M3)
+def test_e4m3_forms(form, rows, N, K, c):
+    assert e4m3(rows, N, K, c) == form
+
+
+@pytest.mark.parametrize("product,form,rows,N,K", [(p, *c) for p, some in ((PRODUCT_FORWARD, cases.FORWARD), (PRODUCT_GRAD_A, cases.GRAD_A), (PRODUCT_GRAD_B, cases.GRAD_B)) for c in some])
+def test_16_bit_forms(product, form, rows, N, K):
+    assert grouped(product, rows, N, K) == form
+
+
+@pytest.mark.parametrize("form,rows,N,K", cases.UNALIGNED)
+def test_forms_of_any_alignment(form, rows, N, K):
+    for product in (PRODUCT_FORWARD, PRODUCT_GRAD_A, PRODUCT_GRAD_B):
+        assert grouped(product, rows, N, K, pad=1) == form
+
+
+def test_every_form_has_shapes_that_reach_it():
+    few = [f"few_rows_{t}" for t in ("16x16", "16x32", "32x16", "32x32", "32x64")]
+    wide = ["widened_128x128", "widened_128x128_short_groups", "widened_128x128_two", "widened_256x128", "e4m3_128x128", "e4m3_256x256"]
+    assert {c[0] for c in cases.E4M3} == {*few, *wide}
+    assert {c[0] for c in cases.FORWARD} == {"256x256", "128x256", "128x128"}
+    assert {c[0] for c in cases.GRAD_A} == {c[0] for c in cases.GRAD_B} == {"256x256", "128x128"}
+
+
+def test_forms_of_what_the_tiles_do_not_take():
+    far = (1 << 22) + 16
+    assert product_form(PRODUCT_E4M3, 1300, 1200, 400, -1, 1 << 22, 1 << 22, TYPE_F32) == "widened_128x128"
+    for lda, ldb in ((far, 400), (400, far), (401, 400), (400, 408)):
+        assert product_form(PRODUCT_E4M3, 1300, 1200, 400, -1, lda, ldb, TYPE_F32) == "any_alignment_64x64"
+    assert product_form(PRODUCT_FORWARD, 100, 7, 64, 2, 64, 7, TYPE_F32) == "any_alignment_64x64"
+    assert product_form(PRODUCT_FORWARD, 100, 9, 64, 2, 64, 9, TYPE_F32) == "any_alignment_128x128"
+
+
+def test_nothing_to_run():
+    for args in ((PRODUCT_E4M3, 0, 8, 8, -1), (PRODUCT_E4M3, 8, 0, 8, -1), (PRODUCT_FORWARD, 8, 8, 8, 0), (PRODUCT_FORWARD, 8, 8, 8, -1), (PRODUCT_GRAD_B, 8, 8, 8, 65536), (4, 8, 8, 8, 1),
+                 (-1, 8, 8, 8, 1), (PRODUCT_GRAD_A, 2**31, 8, 8, 1)):
+        assert product_form(*args, 8, 8, TYPE_F32) is None
+    assert product_form(PRODUCT_FORWARD, 8, 8, 8, 1, 8, 8, 3) is None
