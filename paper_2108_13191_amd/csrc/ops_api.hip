@@ -44,8 +44,18 @@ Form any_alignment() { return {Form::ANY, TILE_256, 0, 0}; }
 Form tiles(OpsTile t) { return {Form::TILES, t, 0, 0}; }
 Form few_rows(int fm, int nb) { return {Form::FEW_ROWS, TILE_256, fm, nb}; }
 
-// The choice of it; us measured for the one taken | the other, groups as a random router deals them.
-Form choose(const OpsGemm& g)
+// Whether its workgroups are as many as one launch takes
+bool fits(const OpsGemm& g, const Form& f)
+{
+    const bool wide = f.tile == TILE_256 || f.tile == TILE_128x256, tall = f.tile == TILE_256 || f.tile == TILE_256x128;
+    const int bm = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.fm : tall ? 256 : 128;
+    const int bn = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.nb : wide ? 256 : 128;
+    const int64_t grid = tile_grid(g, bm, bn);
+    return grid >= 0 && fits_a_launch(grid, f.kernel == Form::ANY ? 256 : 512);
+}
+
+// The fastest of them; us measured for the one taken | the other, groups as a random router deals them.
+Form preferred(const OpsGemm& g, bool allow_few_rows)
 {
     if (!tiles_take(g)) return any_alignment();
     // (a form that loads 8 elements at any alignment needs rows that have them)
@@ -66,7 +76,7 @@ Form choose(const OpsGemm& g)
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
         // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
-        if ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0)) {
+        if (allow_few_rows && ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0))) {
             const int fm = rows <= 16.0 ? 1 : 2;
             // the widest tiles that give every compute unit one: (16,8192,8192) 32 columns 13.6, 16 columns 17.1; (16,2048,8192) 13.1, 9.6;
             // (64,8192,8192) 64 columns 25.8, 32 columns 32; (64,4096,4096) 14.8, 10.4
@@ -94,6 +104,15 @@ Form choose(const OpsGemm& g)
     }
     // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
     return tiles(large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128);
+}
+
+// ... of those that fit a launch: thousands of experts with a wide N are more small tiles than that
+Form choose(const OpsGemm& g)
+{
+    Form f = preferred(g, true);
+    if (f.kernel == Form::FEW_ROWS && !fits(g, f)) f = preferred(g, false);
+    if (f.kernel == Form::TILES && f.tile != TILE_128_ANY && !fits(g, f)) f = tiles(g.elem == ELEM_E4M3 && f.tile != TILE_128_FAST ? TILE_256x128 : TILE_256);
+    return f;
 }
 
 int launch(const OpsGemm& g)
@@ -299,7 +318,8 @@ const char* gemm_ops_form(int64_t product, int64_t T, int64_t N, int64_t K, int6
     OpsGemm g = shaped(product, T, N, K, E, E < 0 ? nullptr : &some_offsets, GEMM_TYPE_F16, c_type, nullptr);
     if (g.M == 0 || g.N == 0) return nullptr;
     g.lda = lda; g.ldb = ldb;
-    return name_of(g, choose(g));
+    const Form f = choose(g);
+    return fits(g, f) ? name_of(g, f) : nullptr;
 }
 
 }  // extern "C"

@@ -32,6 +32,14 @@ struct OpsGemm {
 
 // A launch has less than 2^32 threads in a dimension of its grid.
 inline bool fits_a_launch(int64_t workgroups, int threads) { return workgroups <= UINT32_MAX / threads; }
+// Workgroups of a launch on bm x bn tiles, -1: more than an int counts.  k_ragged: E x (M / bm) x (N / bn); rows: as many as the groups may need, each
+// of which may end in a short tile.
+inline int64_t tile_grid(const OpsGemm& g, int bm, int bn)
+{
+    const int64_t M = g.M, tn = ((int64_t)g.N + bn - 1) / bn, tm = (M + bm - 1) / bm;
+    const int64_t rows = g.k_ragged ? tm * g.E : g.offsets ? M / bm + (g.E < M ? g.E : M) : tm;
+    return rows > INT32_MAX / tn ? -1 : rows * tn;
+}
 
 // ops_generic.hip: any alignment, any size
 int ops_launch_generic(const OpsGemm& g);

@@ -113,7 +113,4 @@ __device__ __forceinline__ int group_by_size(const int32_t* offsets, int E, int 
     }
     return __builtin_ctzll(__ballot(lane < E && before == rank));
 }
-// what a launch needs at most: every group may end in a short tile
-inline int64_t max_group_tiles(int64_t rows, int64_t E, int64_t bm) { return rows / bm + (E < rows ? E : rows); }
-
 }  // namespace ops_dev

@@ -135,10 +135,9 @@ __global__ __launch_bounds__(256) void ops_generic_kernel(const OpsGemm g)
 template <int ELEM, bool AKC, bool BKC>
 int launch(const OpsGemm& g)
 {
-    const int64_t tn = ((int64_t)g.N + GT - 1) / GT;
-    const int64_t tm = g.offsets && !g.k_ragged ? max_group_tiles(g.M, g.E, GT) : ((int64_t)g.M + GT - 1) / GT;
-    if (tm > INT32_MAX / tn || !fits_a_launch(tm * tn, 256)) return GEMM_F16_ERR_SIZE;
-    const dim3 grid((unsigned)(tm * tn), g.k_ragged ? (unsigned)g.E : 1u);
+    const int64_t tiles = tile_grid(g, GT, GT);                 // k_ragged: a group's in x, the groups in y
+    if (tiles < 0 || !fits_a_launch(tiles, 256)) return GEMM_F16_ERR_SIZE;
+    const dim3 grid((unsigned)(g.k_ragged ? tiles / g.E : tiles), g.k_ragged ? (unsigned)g.E : 1u);
     switch (g.c_type) {
     case ELEM_F32: hipLaunchKernelGGL((ops_generic_kernel<ELEM, AKC, BKC, float>), grid, dim3(256), 0, g.stream, g); break;
     case ELEM_F16: hipLaunchKernelGGL((ops_generic_kernel<ELEM, AKC, BKC, half_t>), grid, dim3(256), 0, g.stream, g); break;

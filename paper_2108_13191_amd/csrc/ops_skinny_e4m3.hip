@@ -124,7 +124,7 @@ template <int FM, int NB, int OCC>
 int launch_skinny(const OpsGemm& g)
 {
     static_assert(FM * NB <= WAVES, "a wavefront adds one block");
-    const int64_t grid = tile_grid<16 * FM, 16 * NB>(g);
+    const int64_t grid = tile_grid(g, 16 * FM, 16 * NB);
     if (grid < 0 || !fits_a_launch(grid, 64 * WAVES)) return GEMM_F16_ERR_SIZE;
     if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_skinny_kernel<FM, NB, OCC, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
     else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_skinny_kernel<FM, NB, OCC, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);

@@ -592,19 +592,10 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && F
     }
 }
 
-// k_ragged tiles: E x (M / BM) x (N / BN); rows: as many as the groups may need
-template <int BM, int BN>
-inline int64_t tile_grid(const OpsGemm& g)
-{
-    const int64_t tn = ((int64_t)g.N + BN - 1) / BN, tm = ((int64_t)g.M + BM - 1) / BM;
-    const int64_t rows = g.k_ragged ? tm * g.E : g.offsets ? max_group_tiles(g.M, g.E, BM) : tm;
-    return rows > INT32_MAX / tn ? -1 : rows * tn;
-}
-
 template <int ELEM, bool AKC, bool BKC, int BM, int BN, int S, Form FORM = PLAIN>
 int launch_tiles(const OpsGemm& g)
 {
-    const int64_t grid = tile_grid<BM, BN>(g);
+    const int64_t grid = tile_grid(g, BM, BN);
     if (grid < 0 || !fits_a_launch(grid, 512)) return GEMM_F16_ERR_SIZE;
     if (g.c_type == ELEM_F32) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, FORM, float>), dim3((unsigned)grid), dim3(512), 0, g.stream, g);
     else if (ELEM != ELEM_BF16 && g.c_type == ELEM_F16) { if constexpr (ELEM != ELEM_BF16) hipLaunchKernelGGL((ops_tile_kernel<ELEM, AKC, BKC, BM, BN, S, FORM, half_t>), dim3((unsigned)grid), dim3(512), 0, g.stream, g); }

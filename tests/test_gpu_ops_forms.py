@@ -127,3 +127,16 @@ def test_e4m3_tiles_of_rows_far_apart():
     binding.check(binding.gemm_e4m3_block(M, N, K, A, ld, sa, M, B, ld, sb, 4, C, N, TYPE["f32"], stream()))
     want = (a * sa.t().repeat_interleave(128, 1)[:, :K]).double() @ (b * sb.repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]).double().t().contiguous()
     assert torch.equal(C, want.float())
+
+
+@pytest.mark.parametrize("c", ["bf16", "f32"])
+def test_many_experts_of_a_row_and_a_million_columns(c):
+    """More tiles of few rows than a launch has workgroups: larger ones are taken."""
+    E, N, K = 256, 1 << 20, 16
+    assert binding.product_form(binding.PRODUCT_E4M3, E, N, K, E, K, K, TYPE[c]) in ("e4m3_128x128", "widened_128x128_short_groups")
+    g = torch.Generator("cuda").manual_seed(1)
+    a, b = (torch.randint(-4, 5, s, device="cuda", generator=g).float() for s in ((E, K), (N, K)))
+    off, C = torch.arange(E + 1, dtype=torch.int32, device="cuda"), torch.empty(E, N, dtype=DT[c], device="cuda")
+    binding.check(binding.gemm_e4m3_block_grouped(E, N, K, E, off, a.to(DT["e4m3"]), K, torch.ones(1, E, device="cuda"), E, b.to(DT["e4m3"]), K, 0, torch.ones(N // 128, 1, device="cuda"), 1, 0,
+                                                  C, N, TYPE[c], stream()))
+    assert torch.equal(C, (a @ b.t().contiguous()).to(DT[c]))

@@ -61,3 +61,14 @@ def test_nothing_to_run():
                  (-1, 8, 8, 8, 1), (PRODUCT_GRAD_A, 2**31, 8, 8, 1)):
         assert product_form(*args, 8, 8, TYPE_F32) is None
     assert product_form(PRODUCT_FORWARD, 8, 8, 8, 1, 8, 8, 3) is None
+
+
+def test_forms_that_a_launch_has_no_workgroups_for_give_way_to_larger_tiles():
+    def short(E, N, c, T=None):
+        return product_form(PRODUCT_E4M3, T or E, N, 16, E, 16, 16, c)
+    assert short(256, 1 << 18, TYPE_BF16) == short(256, 1 << 18, TYPE_F32) == "few_rows_16x32"
+    assert short(256, 1 << 20, TYPE_BF16) == "e4m3_128x128" and short(256, 1 << 20, TYPE_F32) == "widened_128x128_short_groups"
+    assert short(65535, 14000, TYPE_F32, 65535 * 30) == "widened_256x128"           # 80894 tiles of 128 rows, 73214 of 256, 110 columns of them
+    assert short(65535, 33000, TYPE_BF16) is None                                   # 65535 + 255 of 256 rows, 129 columns of them
+    grad_a = lambda N: product_form(PRODUCT_GRAD_A, 65535, 64, N, 65535, 64, 64, TYPE_F32)          # noqa: E731
+    assert grad_a(16000) == "128x128" and grad_a(32000) == "256x256" and grad_a(33000) is None
