@@ -38,6 +38,7 @@ extern "C" {
 #endif
 
 enum { GEMM_TYPE_F16 = 0, GEMM_TYPE_BF16 = 1, GEMM_TYPE_F32 = 2 };
+enum { GEMM_OPS_EXACT = 16 };        /* beside the type of an e4m3 product's result: exact products whatever its size */
 enum { GEMM_OPS_ACT_NONE = 0, GEMM_OPS_ACT_RELU = 1, GEMM_OPS_ACT_SWIGLU = 2 };
 
 /*
@@ -106,12 +107,16 @@ int rms_norm_grad(int64_t M, int64_t N, int64_t type,
  * weights are stored; scales in the blocks form):
  *     C[i][j] = sum_b a_scale[b][i] * b_scale[j/128][b] * sum_{k in block b} A[i][k] B[j][k]
  * Sums of products, scaled sums and C before its one rounding are f32.  Products are
- * exact (e4m3 values are widened to f16 on their way) but for one case: 16-bit results of
- * products with M * N >= 2^22 results come from the e4m3 matrix instructions,
+ * exact (e4m3 values are widened to f16 on their way) but for one case, which the caller
+ * chooses by the result's type: 16-bit results without GEMM_OPS_EXACT, where there are
+ * 2^22 of them or more (M * N; T * N of a grouped product), come from the e4m3 matrix instructions,
  * at twice the rate, which add the products of 8 neighbouring k with the
  * bits below 2^-13 of the largest one's exponent cut off -- off by 1.4e-5 of a sum
  * of normally distributed values, where the result's rounding is 2.4e-4 (f16) or 2e-3
- * (bf16), and never by more than 2^-10 of the sum of magnitudes.  A
+ * (bf16), and never by more than 2^-10 of the sum of magnitudes.  Where large products
+ * of a group cancel, the small ones beside them are lost (448 * 448 - 448 * 448 and 126 ones: 120), and a
+ * row's result can differ with the number of rows beside it.  c_type | GEMM_OPS_EXACT
+ * has exact products at every size: 8192^3 to bf16 920 us instead of 441.  f32 results always have.  A
  * NaN in a row of A or B reaches that row or column of C only.  K = 0 gives
  * zeros.  Pointers of any alignment are accepted; A and B 16-byte aligned with pitches
  * that are multiples of 16 run the fast kernels (K and N of any size).  The product
@@ -136,7 +141,7 @@ int gemm_e4m3_block(int64_t M, int64_t N, int64_t K,
  * bs_stride for scales, alike).  db_stride is at least the matrix; what is only
  * read may have any stride from 0 (one matrix for all experts) on.
  *
- * gemm_e4m3_block_grouped: as gemm_e4m3_block, with B[e] (N x K).
+ * gemm_e4m3_block_grouped: as gemm_e4m3_block, with B[e] (N x K), GEMM_OPS_EXACT too.
  * gemm_grouped:        C (T x N) = A (T x K) * B[e] (K x N)
  * gemm_grouped_grad_a: dA (T x K) = dC (T x N) * B[e]^T
  * gemm_grouped_grad_b: dB[e] (K x N) = A_e^T * dC_e, a sum over the expert's rows

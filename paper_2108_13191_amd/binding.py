@@ -199,6 +199,7 @@ def gemm_f16_f16acc_bias_act(M, N, K, A, lda, B, ldb, C, ldc, bias, act, stream=
 
 TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
 ACT_SWIGLU = 2
+EXACT = 16              # beside the c_type of an e4m3 product: exact products whatever the result's size
 
 
 def _general(name, args) -> int:
@@ -234,7 +235,7 @@ def rms_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, rstd, dH, lddh, dX, lddx,
 
 
 def gemm_e4m3_block(M, N, K, A, lda, a_scale, ld_as, B, ldb, b_scale, ld_bs, C, ldc, c_type, stream=0) -> int:
-    """C (M x N of `c_type`) = A (M x K e4m3, scales in rows) @ B (N x K e4m3, scales in blocks) transposed."""
+    """C (M x N of `c_type`, which may be | EXACT) = A (M x K e4m3, scales in rows) @ B (N x K e4m3, scales in blocks) transposed."""
     return _call("gemm_e4m3_block", M, N, K, A, lda, a_scale, ld_as, B, ldb, b_scale, ld_bs, C, ldc, c_type, stream)
 
 

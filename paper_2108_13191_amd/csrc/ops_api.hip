@@ -83,11 +83,12 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
             const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
             return few_rows(fm, nb);
         }
-        // 16-bit results of large products: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 437 us, (1593,7232,4552) 65 against 134 widened.
+        // 16-bit results of large products, unless the caller asks for exact ones: the e4m3 matrix instructions (see ops_tile_e4m3.hip), 8192^3 441 us against 920
+        // widened, (1593,7232,4552) 65 against 134, 16384 rows of 16 experts (4096,2048) 162 against 299.
         // Below 2^22 results the widened form costs little or nothing more.  256 x 256 | 128 x 128: groups of 1024 rows
         // (4096,2048) 166 | 189, (8192,8192,1024) 87 | 104; rounds of workgroups that are a quarter empty (4730,6880,272) 45 | 32, (7266,4800,1232) 75 | 70; groups
         // of 128 rows (2048,2048) 173 | 158 (widened 251); one round that is half full (4000,2304,6000) 71 | 88
-        if (g.c_type != ELEM_F32 && (int64_t)g.M * g.N >= (1 << 22)) {
+        if (!g.exact && g.c_type != ELEM_F32 && (int64_t)g.M * g.N >= (1 << 22)) {
             const double rounds = expected_tiles(g, 256, 256) / cus;
             return tiles(large && rounds >= (rounds > 1.0 ? 0.75 : 0.5) * ceil(rounds) ? TILE_256 : TILE_128_FAST);
         }
@@ -153,7 +154,8 @@ OpsGemm shaped(int64_t product, int64_t T, int64_t N, int64_t K, int64_t E, cons
     g.E = E < 0 ? 1 : (int)E;
     g.offsets = offsets;
     g.elem = product == GEMM_OPS_E4M3 ? (int)ELEM_E4M3 : (int)type;
-    g.c_type = (int)c_type;
+    g.c_type = (int)(c_type & ~(int64_t)GEMM_OPS_EXACT);
+    g.exact = (c_type & GEMM_OPS_EXACT) != 0;
     g.a_kc = product != GEMM_OPS_GRAD_B;
     g.b_kc = product == GEMM_OPS_E4M3 || product == GEMM_OPS_GRAD_A;
     g.k_ragged = product == GEMM_OPS_GRAD_B;
@@ -168,12 +170,13 @@ int run_e4m3(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets,
              const float* sb, int64_t ld_bs, int64_t bs_stride, void* C, int64_t ldc, int64_t c_type, void* stream)
 {
     if (bad_size(M) || bad_size(N) || bad_size(K) || E > 65535) return GEMM_F16_ERR_SIZE;
-    if (!is_16bit(c_type) && c_type != GEMM_TYPE_F32) return GEMM_F16_ERR_CONFIG;
+    const int64_t type = c_type & ~(int64_t)GEMM_OPS_EXACT;
+    if (!is_16bit(type) && type != GEMM_TYPE_F32) return GEMM_F16_ERR_CONFIG;
     if (M == 0 || N == 0 || E == 0) return GEMM_F16_OK;
     if (bad_pitch(lda, K) || bad_pitch(ldb, K) || bad_pitch(ldc, N) || b_stride < 0 || bs_stride < 0) return GEMM_F16_ERR_PITCH;
     if (K > 0 && (bad_pitch(ld_as, M) || bad_pitch(ld_bs, blocks128(K)))) return GEMM_F16_ERR_PITCH;
     if (!C || (E > 0 && !offsets) || (K > 0 && (!A || !B || !sa || !sb))) return GEMM_F16_ERR_NULL;
-    if (unaligned(C, type_size(c_type)) || unaligned(sa, 4) || unaligned(sb, 4) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
+    if (unaligned(C, type_size(type)) || unaligned(sa, 4) || unaligned(sb, 4) || unaligned(offsets, 4)) return GEMM_F16_ERR_ALIGN;
     OpsGemm g = shaped(GEMM_OPS_E4M3, M, N, K, E, offsets, 0, c_type, stream);
     g.A = (const char*)A; g.lda = lda; g.B = (const char*)B; g.ldb = ldb; g.b_stride = b_stride;
     g.C = (char*)C; g.ldc = ldc;
@@ -313,7 +316,8 @@ int gemm_grouped_grad_b(int64_t T, int64_t N, int64_t K, int64_t E, const int32_
 const char* gemm_ops_form(int64_t product, int64_t T, int64_t N, int64_t K, int64_t E, int64_t lda, int64_t ldb, int64_t c_type)
 {
     if (product < GEMM_OPS_E4M3 || product > GEMM_OPS_GRAD_B || bad_size(T) || bad_size(N) || bad_size(K) || E > 65535 || (E < 0 && product != GEMM_OPS_E4M3)) return nullptr;
-    if (E == 0 || (!is_16bit(c_type) && c_type != GEMM_TYPE_F32)) return nullptr;
+    const int64_t result = product == GEMM_OPS_E4M3 ? c_type & ~(int64_t)GEMM_OPS_EXACT : c_type;
+    if (E == 0 || (!is_16bit(result) && result != GEMM_TYPE_F32)) return nullptr;
     static const int32_t some_offsets = 0;
     OpsGemm g = shaped(product, T, N, K, E, E < 0 ? nullptr : &some_offsets, GEMM_TYPE_F16, c_type, nullptr);
     if (g.M == 0 || g.N == 0) return nullptr;

@@ -26,6 +26,7 @@ struct OpsGemm {
     int elem, c_type;                                    // OpsElem
     bool a_kc, b_kc;                                     // summed index contiguous
     bool k_ragged;
+    bool exact;                                          // e4m3: products exact whatever the result
     int num_xcd;
     hipStream_t stream;
 };

@@ -1,7 +1,8 @@
 // The tiled kernel on e4m3 operands with block scales.
 //
 // The e4m3 matrix instructions (all four shapes) add the products of neighbouring k with the bits below 2^-13 of the largest one's
-// exponent cut off: a sum of 128 of normally distributed values is off by 1.4e-5 of itself and by up to 2e-5 of its magnitudes.  Products of
+// exponent cut off: a sum of 128 of normally distributed values is off by 1.4e-5 of itself and by up to 2e-5 of its magnitudes, at the most by 2^-10 of them.
+// A caller has them for large 16-bit results, whose own rounding is coarser, unless it asks for exact products.  Products of
 // values widened to f16 are exact and their sums f32, at half the matrix rate: 4000^3 127 us, 1.0 PFLOP/s.  Those are bound by the conversions, 8 cycles each
 // (two values), beside the MFMAs: a SIMD has 256 of them, and 174 other vector instructions, for 128 MFMAs of 16 cycles in a k step of 256 x 128, 4400 cycles in
 // all.  (In one phase, conversions between the MFMAs, and wavefronts of 64 x 64 in place of 128 x 32: 129; in two phases 135.)  Two workgroups of 128 x 128 a compute unit,

@@ -64,10 +64,12 @@ def swiglu(u):
 class ExpertLayer:
     """Weights as products read them: K x N (gemm_grouped) for training; N x K in e4m3 for serving, laid out once by `prepare`."""
 
-    def __init__(self, hidden, ffn, experts, top_k, dtype=torch.bfloat16, eps=1e-5, seed=0, device="cuda"):
+    def __init__(self, hidden, ffn, experts, top_k, dtype=torch.bfloat16, eps=1e-5, seed=0, device="cuda", exact=False):
+        """exact: e4m3 products exact however many tokens there are, at half the rate (binding.EXACT)."""
         if hidden % 8 or ffn % 8 or not 1 <= top_k <= experts:
             raise ValueError("hidden and ffn are multiples of 8, top_k at most the number of experts")
         self.hidden, self.ffn, self.experts, self.top_k, self.dtype, self.eps = hidden, ffn, experts, top_k, dtype, eps
+        self.exact = binding.EXACT if exact else 0
         gen = torch.Generator(device=device).manual_seed(seed)
 
         def random(*shape, scale):
@@ -128,9 +130,9 @@ class ExpertLayer:
         E, N = w.q.shape[:2]
         c = torch.empty(rows, N, dtype=self.dtype, device=q.device)
         if offsets is None:
-            check(binding.gemm_e4m3_block(rows, N, K, q, q.stride(0), scale, rows, w.q, w.q.stride(1), w.scale, _blocks(K), c, N, TYPES[c.dtype], _stream(c)))
+            check(binding.gemm_e4m3_block(rows, N, K, q, q.stride(0), scale, rows, w.q, w.q.stride(1), w.scale, _blocks(K), c, N, TYPES[c.dtype] | self.exact, _stream(c)))
         else:
-            check(binding.gemm_e4m3_block_grouped(rows, N, K, E, offsets, q, q.stride(0), scale, rows, w.q, w.q.stride(1), w.q.stride(0), w.scale, _blocks(K), w.scale.stride(0), c, N, TYPES[c.dtype], _stream(c)))
+            check(binding.gemm_e4m3_block_grouped(rows, N, K, E, offsets, q, q.stride(0), scale, rows, w.q, w.q.stride(1), w.q.stride(0), w.scale, _blocks(K), w.scale.stride(0), c, N, TYPES[c.dtype] | self.exact, _stream(c)))
         return c
 
     def _swiglu8(self, u):

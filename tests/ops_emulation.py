@@ -80,7 +80,7 @@ def spread(Q, scale, rows, K, ld, ld_scale):
 
 
 def gemm_e4m3_block_grouped(T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb, b_stride, b_scale, ld_bs, bs_stride, C, ldc, c_type, stream=0):
-    a, c = spread(A, a_scale, T, K, lda, ld_as), mat(C, KIND[c_type], T, N, ldc)
+    a, c = spread(A, a_scale, T, K, lda, ld_as), mat(C, KIND[c_type & ~binding.EXACT], T, N, ldc)
     b = at(B, E4M3, (E, b_stride), (N, ldb), (K, 1)).float()
     s = at(b_scale, torch.float32, (E, bs_stride), (ceil128(N), ld_bs), (ceil128(K), 1))
     off = offsets.tolist()

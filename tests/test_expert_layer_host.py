@@ -150,3 +150,15 @@ def test_e4m3_rows_begin_at_multiples_of_16(layer, monkeypatch, hidden, ffn):
     made.prepare()
     made.serve(*(torch.randn(T, hidden).bfloat16() for _ in range(2)))
     assert calls.count("gemm_e4m3_block") == 2 and calls.count("gemm_e4m3_block_grouped") == 2
+
+
+@pytest.mark.parametrize("exact", [False, True])
+def test_exact_products_where_the_layer_asks_for_them(layer, monkeypatch, exact):
+    types = []
+    for f in (ops_emulation.gemm_e4m3_block, ops_emulation.gemm_e4m3_block_grouped):
+        monkeypatch.setattr(binding, f.__name__, lambda *args, f=f: (types.append(args[-2]), f(*args))[1])
+    made = expert_layer.ExpertLayer(H, F, E, TOP, seed=1, device="cpu", exact=exact)
+    made.prepare()
+    x, r, _, _ = inputs()
+    assert same(made.serve(x, r), layer.serve(x, r))          # (which has no sums that could be cut off here)
+    assert types[:4] == [binding.TYPE_BF16 | (binding.EXACT if exact else 0)] * 4

@@ -72,3 +72,24 @@ def test_forms_that_a_launch_has_no_workgroups_for_give_way_to_larger_tiles():
     assert short(65535, 33000, TYPE_BF16) is None                                   # 65535 + 255 of 256 rows, 129 columns of them
     grad_a = lambda N: product_form(PRODUCT_GRAD_A, 65535, 64, N, 65535, 64, 64, TYPE_F32)          # noqa: E731
     assert grad_a(16000) == "128x128" and grad_a(32000) == "256x256" and grad_a(33000) is None
+
+
+def test_exact_e4m3_products_never_run_on_the_e4m3_instructions():
+    for rows, N, K, c in ((8192, 8192, 8192, TYPE_BF16), (8192, 8192, 8192, TYPE_F16), (4730, 4399, 1300, TYPE_BF16), ([1000, 257, 0, 1500, 1001], 6001, 1300, TYPE_F16)):
+        T, E = (rows, -1) if isinstance(rows, int) else (sum(rows), len(rows))
+        form = lambda c: product_form(PRODUCT_E4M3, T, N, K, E, up(K, 16), up(K, 16), c)                    # noqa: E731
+        assert form(c).startswith("e4m3_") and form(c | binding.EXACT).startswith("widened_")
+        assert form(TYPE_F32 | binding.EXACT) == form(TYPE_F32) == form(c | binding.EXACT)                  # as f32 results do
+    assert product_form(PRODUCT_E4M3, 8, 8, 8, -1, 16, 16, 3 | binding.EXACT) is None and product_form(PRODUCT_FORWARD, 8, 8, 8, 1, 8, 8, binding.EXACT) is None
+
+
+def test_exactness_beside_the_type_of_a_result():
+    """Taken by the e4m3 products alone; whatever else is refused stays so."""
+    P, exact = 4096, binding.EXACT
+    lone = dict(M=4, N=8, K=16, A=P, lda=16, a_scale=P, ld_as=4, B=P, ldb=16, b_scale=P, ld_bs=1, C=P, ldc=8)
+    for c in (exact | 3, exact << 1, -1, exact | -32):
+        assert binding.gemm_e4m3_block(**lone, c_type=c) == binding.ERR_CONFIG
+    assert binding.gemm_e4m3_block(**{**lone, "C": P + 1}, c_type=exact | TYPE_BF16) == binding.ERR_ALIGN
+    assert binding.gemm_e4m3_block(**{**lone, "C": P + 2}, c_type=exact | TYPE_F32) == binding.ERR_ALIGN
+    assert binding.gemm_e4m3_block(**{**lone, "M": 0}, c_type=exact | TYPE_F32) == binding.OK
+    assert binding.gemm_grouped(T=4, N=8, K=16, E=2, offsets=P, type=TYPE_F16, A=P, lda=16, B=P, ldb=8, b_stride=128, C=P, ldc=8, c_type=exact | TYPE_F16) == binding.ERR_CONFIG
