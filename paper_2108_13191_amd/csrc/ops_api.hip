@@ -34,6 +34,9 @@ double expected_tiles(const OpsGemm& g, int bm, int bn)
     return (g.M / (double)bm + groups * (rows < bm ? 1.0 - 0.5 * rows / bm : 0.5)) * tn;
 }
 
+// The results that bm x bn tiles of an M x N matrix multiply, with the rows and columns behind its ends
+double padded(int64_t M, int64_t N, int bm, int bn) { return (double)((M + bm - 1) / bm * bm) * (double)((N + bn - 1) / bn * bn); }
+
 // What a product runs on: the kernel for any alignment, the tiled one, or the one for few rows on 16 fm x 16 nb results a workgroup.
 struct Form {
     enum Kernel { ANY, TILES, FEW_ROWS } kernel;
@@ -67,7 +70,10 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
         // (16384, 4096 x 2048, 8) 1024 tiles 505 | 563; below one: B's alone, (16384, 2304 x 768, 8) 216 tiles 89 | 77, (2048 x 1024, 4) 128 tiles 139 | 91.
         // Between, with many rows a group, (16384, 4096 x 2048, 3) 384 tiles 231 | 277, (2048 x 2048, 5) 320 tiles 146 | 151, with few (4000, 1408 x 2048, 8) 46 | 40; and
         // one round of a single group's, whose operands 128 x 128 tiles read too often: (16384, 4096 x 4096, 1) 380 | 602, (1000, ..) 40 | 43
-        const double n = expected_tiles(g, 256, 256);
+        // Matrices that fill the larger tiles badly, 1.3 times and more what the smaller ones multiply: 64 experts' 640 x 640 (1.44) 50 | 41, 264 x 1032 (1.48) 52 | 40,
+        // 128 x 4096 (2) 79 | 60, 128 experts' 304 x 304 (1.78) 29 | 20, 1000 experts' 48 x 72 (4) 26 | 11; below: 520 x 1032 (1.33) 69 | 66, 776 x 1032 (1.27) 97 | 97,
+        // 32 experts' 1032 x 2056 (1.18) 160 | 173
+        const double n = padded(g.M, g.N, 256, 256) < 1.3 * padded(g.M, g.N, 128, 128) ? expected_tiles(g, 256, 256) : 0.0;
         return tiles(n >= 2.0 * cus || (n >= 1.25 * cus && (double)g.K / g.E >= 1024.0) || n >= (double)g.E * cus ? TILE_256 : TILE_128);
     }
     // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
@@ -104,7 +110,10 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
         return tiles(tall ? TILE_256x128 : TILE_128_PAIR);
     }
     // forward, groups below 192 rows, 128 x 256 | 128 x 128: (8192 rows, 2048 x 2048, 64 experts) 128 | 140, (64, 4096 x 2048, 16) 42 | 50
-    return tiles(large ? TILE_256 : !g.b_kc && expected_tiles(g, 128, 256) >= cus ? TILE_128x256 : TILE_128);
+    // (but not where N leaves much of the last 256 columns empty: N = 264 of 8 experts of 2048 rows, K = 2048, 56 | 33, 520 of 128 of 64 rows 35 | 21, 1032 of 128 of 16 rows 42 | 39,
+    // 72 of 1000 of 2 rows 58 | 30)
+    const bool wide = !g.b_kc && padded(1, g.N, 1, 256) < 1.1 * padded(1, g.N, 1, 128) && expected_tiles(g, 128, 256) >= cus;
+    return tiles(large ? TILE_256 : wide ? TILE_128x256 : TILE_128);
 }
 
 // ... of those that fit a launch: thousands of experts with a wide N are more small tiles than that

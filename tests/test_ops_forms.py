@@ -93,3 +93,16 @@ def test_exactness_beside_the_type_of_a_result():
     assert binding.gemm_e4m3_block(**{**lone, "C": P + 2}, c_type=exact | TYPE_F32) == binding.ERR_ALIGN
     assert binding.gemm_e4m3_block(**{**lone, "M": 0}, c_type=exact | TYPE_F32) == binding.OK
     assert binding.gemm_grouped(T=4, N=8, K=16, E=2, offsets=P, type=TYPE_F16, A=P, lda=16, B=P, ldb=8, b_stride=128, C=P, ldc=8, c_type=exact | TYPE_F16) == binding.ERR_CONFIG
+
+
+def test_large_tiles_only_where_matrices_fill_them():
+    grad_b = lambda T, K, N, E: product_form(PRODUCT_GRAD_B, T, N, K, E, up(K, 8), up(N, 8), TYPE_F32)        # noqa: E731
+    for T, K, N, E in ((8192, 304, 304, 128), (16384, 264, 1032, 64), (16384, 640, 640, 64), (16384, 128, 4096, 64), (2000, 48, 72, 1000), (8192, 300, 300, 128)):
+        assert grad_b(T, K, N, E) == "128x128"
+    for T, K, N, E in ((16384, 1024, 2048, 32), (16384, 1032, 2056, 32), (16384, 512, 512, 128), (16384, 776, 1032, 64), (16384, 4096, 4096, 1)):
+        assert grad_b(T, K, N, E) == "256x256"
+    forward = lambda T, N, E: product_form(PRODUCT_FORWARD, T, N, 1024, E, 1024, up(N, 8), TYPE_F16)         # noqa: E731
+    for T, N, E in ((8192, 72, 512), (8192, 264, 128), (8192, 520, 64), (2000, 1032, 128)):
+        assert forward(T, N, E) == "128x128"
+    for T, N, E in ((8192, 2048, 64), (64, 4096, 16), (4000, 1160, 128)):
+        assert forward(T, N, E) == "128x256"
