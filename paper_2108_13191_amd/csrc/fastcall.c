@@ -112,10 +112,17 @@ static int to_words(const char* kinds, PyObject* const* a, Py_ssize_t n, uint64_
     return 1;
 }
 
-/* words(address, kinds, ...): int f(...) of as many 64-bit integers and pointers, which the calling convention passes alike.
- * The C side's arguments are int64_t, pointers and nothing else; those behind the last are given as 0 and not looked at. */
-typedef int (*words_fn)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
-                        uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t);
+/* words(address, kinds, ...): int f(...) of as many 64-bit integers and pointers, which the calling conventions of 64-bit Linux pass alike. */
+#define W1 uint64_t
+#define W4 W1, W1, W1, W1
+#define W10 W4, W4, W1, W1
+typedef int (*words10_fn)(W10);
+typedef int (*words11_fn)(W10, W1);
+typedef int (*words15_fn)(W10, W4, W1);
+typedef int (*words17_fn)(W10, W4, W1, W1, W1);
+typedef int (*words19_fn)(W10, W4, W4, W1);
+#define A4(i) w[i], w[i + 1], w[i + 2], w[i + 3]
+#define A10 A4(0), A4(4), w[8], w[9]
 static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
     uint64_t f, w[MOST_WORDS] = {0};
@@ -124,9 +131,16 @@ static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
     if (n < 2 || n - 2 > MOST_WORDS || !PyUnicode_Check(a[1]) || !to_word(a[0], &f)) return other_way();
     const char* const kinds = PyUnicode_AsUTF8AndSize(a[1], &length);
     if (!kinds) PyErr_Clear();
-    if (!kinds || length != n - 2 || !to_words(kinds, a + 2, n - 2, w)) return other_way();
+    n -= 2;
+    if (!kinds || length != n || (n != 10 && n != 11 && n != 15 && n != 17 && n != 19) || !to_words(kinds, a + 2, n, w)) return other_way();
     Py_BEGIN_ALLOW_THREADS
-    rc = ((words_fn)(uintptr_t)f)(w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7], w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15], w[16], w[17], w[18]);
+    switch (n) {
+    case 10: rc = ((words10_fn)(uintptr_t)f)(A10); break;
+    case 11: rc = ((words11_fn)(uintptr_t)f)(A10, w[10]); break;
+    case 15: rc = ((words15_fn)(uintptr_t)f)(A10, A4(10), w[14]); break;
+    case 17: rc = ((words17_fn)(uintptr_t)f)(A10, A4(10), w[14], w[15], w[16]); break;
+    default: rc = ((words19_fn)(uintptr_t)f)(A10, A4(10), A4(14), w[18]); break;
+    }
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
