@@ -57,7 +57,8 @@ bool fits(const OpsGemm& g, const Form& f)
     return grid >= 0 && fits_a_launch(grid, f.kernel == Form::ANY ? 256 : 512);
 }
 
-// The fastest of them; us measured for the one taken | the other, groups as a random router deals them.
+// The fastest of them; us measured for the one taken | the other, groups as a random router deals them.  `rows` is the average group's: who has more is known on the device only.
+// 1280 rows of 64 experts (4096,2048) in e4m3 that all go to one take 102 us on the 32-row tiles of 20 rows each, and 20 to 40 on tiles of 128; dealt evenly they take 155.
 Form preferred(const OpsGemm& g, bool allow_few_rows)
 {
     if (!tiles_take(g)) return any_alignment();

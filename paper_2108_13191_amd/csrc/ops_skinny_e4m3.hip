@@ -5,7 +5,8 @@
 // bytes of a row) and multiplies them.  No LDS, no barrier before the end; what keeps the memory busy is that 16 to 32 wavefronts
 // a compute unit do so.  (A ring of 2 to 6 steps in registers ahead of the multiplication, with fewer wavefronts: (16,8192,8192) e4m3
 // 13.9 to 19.9 us against 13.7, 64 rows of 16 experts (4096,2048) 29.5 to 57 against 26.3.)  e4m3 values are widened to f16: the matrix
-// rate does not matter here.  Measured: (16,8192,8192) 13.5 us, 5.0 TB/s; 64 rows of 16 experts (4096,2048) 26 to 28 us, 4.8 to 5.1 TB/s.  More rows a workgroup
+// rate does not matter here.  Measured: (16,8192,8192) 16.2 us from memory, 4.2 TB/s, 13.5 where B (67 MB) is still in the 256 MB memory-side cache; 64 rows of 16
+// experts (4096,2048) 26 to 29 us, 4.6 to 5.1 TB/s.  More rows a workgroup
 // than 32 make A's reads, once for each 32 columns, the bound: 32 rows each of 16 experts 75 us with 64, 56 with 32.
 #include "ops_tile.h"
 
