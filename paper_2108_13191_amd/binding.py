@@ -1,4 +1,4 @@
-"""Thin binding of the C ABIs in include/gemm_f16.h and include/gemm_ops.h: ctypes, and for the GEMM entry points themselves a small extension
+"""Thin binding of the C ABIs in include/gemm_f16.h, include/gemm_ops.h and include/gemm_layer.h: ctypes, and for the GEMM entry points themselves a small extension
 (csrc/fastcall.c) in front of it that marshals the usual arguments in native code.
 
 Argument marshalling only: every step of the GEMM runs in the HIP kernels of
@@ -73,6 +73,17 @@ _OPS = {
     "gemm_grouped_grad_a": "iiiipipipiipiip",
     "gemm_grouped_grad_b": "iiiipipipipiiip",
 }
+# and of gemm_layer.h
+_LAYER_OPS = {
+    "layer_norm": "iiipipippdpipipipppp",
+    "layer_norm_grad": "iiipipippppipipppip",
+    "quantize_i8_rows": "iiiipipipp",
+    "gemm_i8": "iiipippippiip",
+    "gemm_i8_grouped": "iiiippippiipipiip",
+    "expert_dispatch": "iiiippppiipiipipipipip",
+    "expert_combine": "iiiippippipiip",
+    "expert_combine_grad": "iiiippippipipp",
+}
 
 
 def load() -> ctypes.CDLL:
@@ -109,7 +120,7 @@ def load() -> ctypes.CDLL:
         lib.gemm_f16_force_config.argtypes = [ci]
         lib.gemm_f16_force_config.restype = ci
         kinds = {"i": i64, "p": vp, "d": ctypes.c_double}
-        for name, letters in _OPS.items():
+        for name, letters in {**_OPS, **_LAYER_OPS}.items():
             f = getattr(lib, name)
             f.argtypes = [kinds[k] for k in letters]
             f.restype = ci
@@ -118,6 +129,12 @@ def load() -> ctypes.CDLL:
         lib.rms_norm_grad_workspace_bytes.restype = i64
         lib.gemm_ops_form.argtypes = [i64] * 8
         lib.gemm_ops_form.restype = ctypes.c_char_p
+        lib.layer_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        lib.layer_norm_grad_workspace_bytes.restype = i64
+        lib.expert_dispatch_workspace_bytes.argtypes = [i64] * 3
+        lib.expert_dispatch_workspace_bytes.restype = i64
+        lib.gemm_i8_form.argtypes = [i64] * 7
+        lib.gemm_i8_form.restype = ctypes.c_char_p
         # where the entry points are, for _fastcall
         for name in ("gemm_f16_f32acc", "gemm_f16_f16acc", "gemm_f16_f16acc_static_workspace", "gemm_f16_f32acc_bias_act",
                      "gemm_f16_f16acc_bias_act", "gemm_f16_f16acc_workspace"):
@@ -142,6 +159,7 @@ def _no_fast_way(*args):
 # called nothing, for anything else.
 _plain, _bias_act, _workspace = (_fastcall.plain, _fastcall.bias_act, _fastcall.workspace) if _fastcall else (_no_fast_way,) * 3
 _words, _norm = (_fastcall.words, _fastcall.norm) if _fastcall else (_no_fast_way,) * 2
+_layer_words, _layer_norm = (_fastcall.layer_words, _fastcall.layer_norm) if _fastcall else (_no_fast_way,) * 2
 
 
 def gemm_f16_f32acc(M, N, K, A, lda, B, ldb, C, ldc, stream=0) -> int:
@@ -204,7 +222,8 @@ EXACT = 16              # beside the c_type of an e4m3 product: exact products w
 
 def _general(name, args) -> int:
     """The way through ctypes, for what _fastcall leaves: pointers as ints, None or objects with data_ptr()."""
-    return getattr(load(), name)(*[_ptr(x) if k == "p" else x for x, k in zip(args, _OPS[name], strict=True)])
+    letters = _OPS[name] if name in _OPS else _LAYER_OPS[name]
+    return getattr(load(), name)(*[_ptr(x) if k == "p" else x for x, k in zip(args, letters, strict=True)])
 
 
 def _call(name, *args) -> int:
@@ -271,6 +290,76 @@ def product_form(product, T, N, K, E, lda, ldb, c_type):
     """The name of the kernel that a product would run on (E < 0: gemm_e4m3_block), None where there is nothing to run."""
     name = load().gemm_ops_form(product, T, N, K, E, lda, ldb, c_type)
     return name.decode() if name else None
+
+
+# ---- include/gemm_layer.h: layer norm, 8-bit integers, tokens moved to their experts and back.
+
+INDEX_I32, INDEX_I64 = 0, 1
+
+
+def _call_layer(name, *args) -> int:
+    rc = _layer_words(getattr(load(), name + "_address"), _LAYER_OPS[name], *args)
+    return rc if rc is not NotImplemented else _general(name, args)
+
+
+def layer_norm(M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream=0) -> int:
+    """H = X + R, Y = (H - mean) * rstd * gamma + beta in 16 bits and / or as 8-bit integers in Q and scale; R, beta and any output may be None."""
+    args = (M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream)
+    rc = _layer_norm(load().layer_norm_address, *args)
+    return rc if rc is not NotImplemented else _general("layer_norm", args)
+
+
+def layer_norm_grad_workspace_bytes(M, N) -> int:
+    """Bytes of workspace that layer_norm_grad needs to form dgamma or dbeta."""
+    return load().layer_norm_grad_workspace_bytes(M, N)
+
+
+def layer_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream=0) -> int:
+    """dX (of x and of the residual alike), dgamma and dbeta (f32, None: not formed) from dY and dH (None: no gradient of h itself)."""
+    return _call_layer("layer_norm_grad", M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream)
+
+
+def quantize_i8_rows(M, N, type, act, X, ldx, Q, ldq, scale, stream=0) -> int:
+    """Q (8-bit integers), scale[row] = X (M x N of `type`; M x 2N for ACT_SWIGLU) after `act`, a scale for each row."""
+    return _call_layer("quantize_i8_rows", M, N, type, act, X, ldx, Q, ldq, scale, stream)
+
+
+def gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream=0) -> int:
+    """C (M x N of `c_type`) = A (M x K, a scale a row) @ B (N x K, a scale a row) transposed, 8-bit integers."""
+    return _call_layer("gemm_i8", M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream)
+
+
+def gemm_i8_grouped(T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream=0) -> int:
+    """gemm_i8 of rows offsets[e] .. offsets[e + 1] (int32 on the device) with B[e], for E experts."""
+    return _call_layer("gemm_i8_grouped", T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream)
+
+
+def i8_form(T, N, K, E, lda, ldb, c_type):
+    """The name of the kernel that a product of 8-bit integers would run on (E < 0: gemm_i8), None where there is nothing to run."""
+    name = load().gemm_i8_form(T, N, K, E, lda, ldb, c_type)
+    return name.decode() if name else None
+
+
+def expert_dispatch_workspace_bytes(T, top_k, E) -> int:
+    """Bytes of workspace that expert_dispatch needs (0: none)."""
+    return load().expert_dispatch_workspace_bytes(T, top_k, E)
+
+
+def expert_dispatch(T, top_k, E, index_type, expert, offsets, source, place, N, size, X, ldx, blocks, scale, ld_scale, rows, ld_rows, row_scale, ld_row_scale,
+                    workspace, workspace_bytes, stream=0) -> int:
+    """Sorts the choices `expert` (T x top_k) by expert into offsets, source (None: not written) and place, and copies X's rows and scales to their places (X None: only sorts)."""
+    return _call_layer("expert_dispatch", T, top_k, E, index_type, expert, offsets, source, place, N, size, X, ldx, blocks, scale, ld_scale, rows, ld_rows,
+                       row_scale, ld_row_scale, workspace, workspace_bytes, stream)
+
+
+def expert_combine(T, top_k, N, type, place, Y, ldy, weight, add, ld_add, out, ldo, out_type, stream=0) -> int:
+    """out[t] = add[t] + sum over j of weight[t][j] * Y[place[t][j]]; weight None: 1, add None: 0."""
+    return _call_layer("expert_combine", T, top_k, N, type, place, Y, ldy, weight, add, ld_add, out, ldo, out_type, stream)
+
+
+def expert_combine_grad(T, top_k, N, type, place, dOut, lddo, weight, Y, ldy, dY, lddy, dweight, stream=0) -> int:
+    """dY[place[t][j]] = weight[t][j] * dOut[t] and dweight[t][j] = dOut[t] . Y[place[t][j]] (f32); dY or dweight None: not formed."""
+    return _call_layer("expert_combine_grad", T, top_k, N, type, place, dOut, lddo, weight, Y, ldy, dY, lddy, dweight, stream)
 
 
 def strerror(code: int) -> str:

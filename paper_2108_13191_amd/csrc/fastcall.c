@@ -10,7 +10,8 @@
  * call, as ctypes does.
  *
  * The entry points of gemm_ops.h take up to 19 arguments; `words` calls any of them whose arguments are all 64-bit integers and
- * pointers, told by a text with a letter for each ("i", "p"), and `norm` is for rms_norm, which has a double among them. */
+ * pointers, told by a text with a letter for each ("i", "p"), and `norm` is for rms_norm, which has a double among them; `layer_words` and
+ * `layer_norm` are the same for those of gemm_layer.h, which take up to 22. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -100,7 +101,7 @@ static PyObject* workspace(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-#define MOST_WORDS 19
+#define MOST_WORDS 22
 /* 1: converted, 0: no arguments for this way */
 static int to_words(const char* kinds, PyObject* const* a, Py_ssize_t n, uint64_t* w)
 {
@@ -118,12 +119,16 @@ static int to_words(const char* kinds, PyObject* const* a, Py_ssize_t n, uint64_
 #define W10 W4, W4, W1, W1
 typedef int (*words10_fn)(W10);
 typedef int (*words11_fn)(W10, W1);
+typedef int (*words13_fn)(W10, W1, W1, W1);
+typedef int (*words14_fn)(W10, W4);
 typedef int (*words15_fn)(W10, W4, W1);
 typedef int (*words17_fn)(W10, W4, W1, W1, W1);
 typedef int (*words19_fn)(W10, W4, W4, W1);
+typedef int (*words22_fn)(W10, W4, W4, W4);
 #define A4(i) w[i], w[i + 1], w[i + 2], w[i + 3]
 #define A10 A4(0), A4(4), w[8], w[9]
-static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
+/* Those of the numbers of arguments in `numbers`, a list that ends with 0; others are left to ctypes. */
+static PyObject* call_words(PyObject* const* a, Py_ssize_t n, const int* numbers)
 {
     uint64_t f, w[MOST_WORDS] = {0};
     Py_ssize_t length;
@@ -132,17 +137,31 @@ static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
     const char* const kinds = PyUnicode_AsUTF8AndSize(a[1], &length);
     if (!kinds) PyErr_Clear();
     n -= 2;
-    if (!kinds || length != n || (n != 10 && n != 11 && n != 15 && n != 17 && n != 19) || !to_words(kinds, a + 2, n, w)) return other_way();
+    while (*numbers && *numbers != n) numbers++;
+    if (!kinds || length != n || !*numbers || !to_words(kinds, a + 2, n, w)) return other_way();
     Py_BEGIN_ALLOW_THREADS
     switch (n) {
     case 10: rc = ((words10_fn)(uintptr_t)f)(A10); break;
     case 11: rc = ((words11_fn)(uintptr_t)f)(A10, w[10]); break;
+    case 13: rc = ((words13_fn)(uintptr_t)f)(A10, w[10], w[11], w[12]); break;
+    case 14: rc = ((words14_fn)(uintptr_t)f)(A10, A4(10)); break;
     case 15: rc = ((words15_fn)(uintptr_t)f)(A10, A4(10), w[14]); break;
     case 17: rc = ((words17_fn)(uintptr_t)f)(A10, A4(10), w[14], w[15], w[16]); break;
-    default: rc = ((words19_fn)(uintptr_t)f)(A10, A4(10), A4(14), w[18]); break;
+    case 19: rc = ((words19_fn)(uintptr_t)f)(A10, A4(10), A4(14), w[18]); break;
+    default: rc = ((words22_fn)(uintptr_t)f)(A10, A4(10), A4(14), A4(18)); break;
     }
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
+}
+static PyObject* words(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    static const int numbers[] = {10, 11, 15, 17, 19, 0};
+    return call_words(a, n, numbers);
+}
+static PyObject* layer_words(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    static const int numbers[] = {10, 13, 14, 17, 19, 22, 0};
+    return call_words(a, n, numbers);
 }
 
 typedef int (*norm_fn)(int64_t, int64_t, int64_t, const void*, int64_t, const void*, int64_t, const void*, double, void*, int64_t, void*, int64_t,
@@ -159,10 +178,25 @@ static PyObject* norm(PyObject* self, PyObject* const* a, Py_ssize_t n)
     rc = ((norm_fn)(uintptr_t)f)(I(b[0]), I(b[1]), I(b[2]), P(b[3]), I(b[4]), P(b[5]), I(b[6]), P(b[7]), eps, P(c[0]), I(c[1]), P(c[2]), I(c[3]),
                                  P(c[4]), I(c[5]), P(c[6]), I(c[7]), P(c[8]), P(c[9]));
     Py_END_ALLOW_THREADS
-#undef P
-#undef I
     return PyLong_FromLong(rc);
 }
+
+typedef int (*layer_norm_fn)(int64_t, int64_t, int64_t, const void*, int64_t, const void*, int64_t, const void*, const void*, double, void*, int64_t, void*, int64_t,
+                             void*, int64_t, void*, void*, void*, void*);
+static PyObject* layer_norm(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    uint64_t f, b[9], c[10];
+    int rc;
+    if (n != 21 || !to_word(a[0], &f) || !to_words("iiipipipp", a + 1, 9, b) || !PyFloat_CheckExact(a[10]) || !to_words("pipipipppp", a + 11, 10, c)) return other_way();
+    const double eps = PyFloat_AS_DOUBLE(a[10]);
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((layer_norm_fn)(uintptr_t)f)(I(b[0]), I(b[1]), I(b[2]), P(b[3]), I(b[4]), P(b[5]), I(b[6]), P(b[7]), P(b[8]), eps, P(c[0]), I(c[1]), P(c[2]), I(c[3]),
+                                       P(c[4]), I(c[5]), P(c[6]), P(c[7]), P(c[8]), P(c[9]));
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+#undef P
+#undef I
 
 static PyMethodDef methods[] = {
     {"plain", (PyCFunction)(void (*)(void))plain, METH_FASTCALL, "plain(address, M, N, K, A, lda, B, ldb, C, ldc, stream)"},
@@ -170,6 +204,8 @@ static PyMethodDef methods[] = {
     {"workspace", (PyCFunction)(void (*)(void))workspace, METH_FASTCALL, "workspace(address, M, N, K, A, lda, B, ldb, C, ldc, workspace, workspace_bytes, stream)"},
     {"words", (PyCFunction)(void (*)(void))words, METH_FASTCALL, "words(address, kinds, ...)"},
     {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, "norm(address, M, N, type, X, ldx, R, ldr, gamma, eps, H, ldh, Y, ldy, Q, ldq, scale, ld_scale, rstd, stream)"},
+    {"layer_words", (PyCFunction)(void (*)(void))layer_words, METH_FASTCALL, "layer_words(address, kinds, ...)"},
+    {"layer_norm", (PyCFunction)(void (*)(void))layer_norm, METH_FASTCALL, "layer_norm(address, M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream)"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "Calls into the C ABI of libgemm_f16.so", -1, methods, NULL, NULL, NULL, NULL};

@@ -5,12 +5,8 @@
 
 namespace {
 
-bool bad_size(int64_t n) { return n < 0 || n > INT32_MAX; }
-bool bad_pitch(int64_t ld, int64_t row) { return ld < row || ld > INT32_MAX; }
-bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 int64_t blocks128(int64_t n) { return (n + 127) / 128; }
-bool is_16bit(int64_t type) { return type == GEMM_TYPE_F16 || type == GEMM_TYPE_BF16; }
-int type_size(int64_t type) { return type == GEMM_TYPE_F32 ? 4 : 2; }
+bool is_8bit(const OpsGemm& g) { return g.elem == ELEM_E4M3 || g.elem == ELEM_I8; }
 
 // What the tiled kernels take: operands whose offsets within a tile fit 32 bits, and but for one form of the 16-bit ones 16-byte aligned ones
 bool tiles_take(const OpsGemm& g)
@@ -19,7 +15,7 @@ bool tiles_take(const OpsGemm& g)
 }
 bool is_aligned(const OpsGemm& g)
 {
-    const int64_t chunk = g.elem == ELEM_E4M3 ? 16 : 8;
+    const int64_t chunk = is_8bit(g) ? 16 : 8;
     return !unaligned(g.A, 16) && !unaligned(g.B, 16) && g.lda % chunk == 0 && g.ldb % chunk == 0 && g.b_stride % chunk == 0;
 }
 
@@ -63,7 +59,7 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
 {
     if (!tiles_take(g)) return any_alignment();
     // (a form that loads 8 elements at any alignment needs rows that have them)
-    if (!is_aligned(g)) return g.elem == ELEM_E4M3 || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8 ? any_alignment() : tiles(TILE_128_ANY);
+    if (!is_aligned(g)) return is_8bit(g) || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8 ? any_alignment() : tiles(TILE_128_ANY);
     const int cus = chip().cus;
     const double rows = (double)g.M / g.E;                                  // of a group
     if (g.k_ragged) {
@@ -80,6 +76,14 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
     // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
     // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
     const bool large = rows >= 192.0 && expected_tiles(g, 128, 128) >= 2.0 * cus;
+    if (g.elem == ELEM_I8) {
+        if (allow_few_rows && ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0))) {
+            const int fm = rows <= 16.0 ? 1 : 2;
+            const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
+            return few_rows(fm, nb);
+        }
+        return tiles(large ? TILE_256 : TILE_128);
+    }
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
         // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
@@ -130,7 +134,8 @@ int launch(const OpsGemm& g)
 {
     const Form f = choose(g);
     if (f.kernel == Form::ANY) return ops_launch_generic(g);
-    if (f.kernel == Form::FEW_ROWS) return ops_launch_skinny_e4m3(g, f.fm, f.nb);
+    if (f.kernel == Form::FEW_ROWS) return ops_launch_skinny(g, f.fm, f.nb);
+    if (g.elem == ELEM_I8) return ops_launch_tiles_i8(g, f.tile);
     return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, f.tile) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, f.tile) : ops_launch_tiles_bf16(g, f.tile);
 }
 
@@ -203,6 +208,13 @@ int check_grouped(int64_t T, int64_t N, int64_t K, int64_t E, int64_t type, int6
 }
 
 }  // namespace
+
+int ops_run_product(const OpsGemm& g) { return launch(g); }
+const char* ops_product_form(const OpsGemm& g)
+{
+    const Form f = choose(g);
+    return fits(g, f) ? name_of(g, f) : nullptr;
+}
 
 extern "C" {
 
@@ -332,8 +344,7 @@ const char* gemm_ops_form(int64_t product, int64_t T, int64_t N, int64_t K, int6
     OpsGemm g = shaped(product, T, N, K, E, E < 0 ? nullptr : &some_offsets, GEMM_TYPE_F16, c_type, nullptr);
     if (g.M == 0 || g.N == 0) return nullptr;
     g.lda = lda; g.ldb = ldb;
-    const Form f = choose(g);
-    return fits(g, f) ? name_of(g, f) : nullptr;
+    return ops_product_form(g);
 }
 
 }  // extern "C"

@@ -6,8 +6,9 @@
 typedef __bf16 bf16_t;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
 
-enum OpsElem { ELEM_E4M3 = 3, ELEM_F16 = 0, ELEM_BF16 = 1, ELEM_F32 = 2 };      // the 16- and 32-bit ones as GEMM_TYPE_*
+enum OpsElem { ELEM_E4M3 = 3, ELEM_I8 = 4, ELEM_F16 = 0, ELEM_BF16 = 1, ELEM_F32 = 2 };      // the 16- and 32-bit ones as GEMM_TYPE_*
 
 // One product C = A B in groups.  What is ragged:
 //   offsets == nullptr   nothing: one product of M x N x K
@@ -21,7 +22,7 @@ struct OpsGemm {
     const char* A; int64_t lda;                          // pitches and strides in elements
     const char* B; int64_t ldb, b_stride;
     char* C; int64_t ldc, c_stride;
-    const float* sa; int64_t ld_sa;                      // e4m3: scales of A [k block][row], of B [column block][k block]
+    const float* sa; int64_t ld_sa;                      // e4m3: scales of A [k block][row], of B [column block][k block]; i8: of A [row], of B [column]
     const float* sb; int64_t ld_sb, sb_stride;
     int elem, c_type;                                    // OpsElem
     bool a_kc, b_kc;                                     // summed index contiguous
@@ -30,6 +31,13 @@ struct OpsGemm {
     int num_xcd;
     hipStream_t stream;
 };
+
+// What the entry points check of their arguments
+inline bool bad_size(int64_t n) { return n < 0 || n > INT32_MAX; }
+inline bool bad_pitch(int64_t ld, int64_t row) { return ld < row || ld > INT32_MAX; }
+inline bool unaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
+inline bool is_16bit(int64_t type) { return type == ELEM_F16 || type == ELEM_BF16; }
+inline int type_size(int64_t type) { return type == ELEM_F32 ? 4 : 2; }
 
 // A launch has less than 2^32 threads in a dimension of its grid.
 inline bool fits_a_launch(int64_t workgroups, int threads) { return workgroups <= UINT32_MAX / threads; }
@@ -42,6 +50,10 @@ inline int64_t tile_grid(const OpsGemm& g, int bm, int bn)
     return rows > INT32_MAX / tn ? -1 : rows * tn;
 }
 
+// ops_api.hip: a checked product on the kernel that suits it, and that kernel's name (nullptr: nothing to run, or more workgroups than a launch has)
+int ops_run_product(const OpsGemm& g);
+const char* ops_product_form(const OpsGemm& g);
+
 // ops_generic.hip: any alignment, any size
 int ops_launch_generic(const OpsGemm& g);
 
@@ -51,9 +63,10 @@ enum OpsTile { TILE_256, TILE_256x128, TILE_128x256, TILE_128, TILE_128_ANY, TIL
 int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_f16(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_bf16(const OpsGemm& g, OpsTile tile);
+int ops_launch_tiles_i8(const OpsGemm& g, OpsTile tile);
 
-// ops_skinny_e4m3.hip: few rows; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
-int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb);
+// ops_skinny.hip: few rows, e4m3 and i8; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
+int ops_launch_skinny(const OpsGemm& g, int fm, int nb);
 
 // ops_norm.hip
 struct NormArgs {
@@ -79,3 +92,54 @@ int ops_norm_grad_parts(int64_t M, int64_t N);            // rows of N floats of
 int ops_launch_norm_grad(int type, const NormGradArgs& a, hipStream_t stream);
 int ops_launch_quant_rows(int type, const QuantArgs& a, hipStream_t stream);
 int ops_launch_quant_blocks(int type, const QuantArgs& a, hipStream_t stream);
+
+// ops_layer_norm.hip
+struct LayerNormArgs {
+    int M, N;
+    const void *X, *R, *gamma, *beta; int64_t ldx, ldr;
+    void *H, *Y; int64_t ldh, ldy;
+    uint8_t* Q; int64_t ldq; float* scale;
+    float *mean, *rstd; float eps;
+};
+struct LayerNormGradArgs {
+    int M, N;
+    const void *dY, *H, *gamma, *dH; const float *mean, *rstd; int64_t lddy, ldh, lddh;
+    void* dX; int64_t lddx;
+    float *dgamma, *dbeta, *ws;
+};
+int ops_launch_layer_norm(int type, const LayerNormArgs& a, hipStream_t stream);
+int ops_layer_norm_grad_parts(int64_t M, int64_t N);      // rows of 2 N floats of workspace
+int ops_launch_layer_norm_grad(int type, const LayerNormGradArgs& a, hipStream_t stream);
+int ops_launch_quant_i8(int type, const QuantArgs& a, hipStream_t stream);
+
+// ops_experts.hip.  T tokens with top_k choices each
+struct DispatchArgs {
+    int64_t T; int top_k, E;
+    bool index64; const void* expert;
+    int32_t *offsets, *source, *place;
+    int N, size;                                         // elements of a row, bytes of one
+    const void* X; int64_t ldx;
+    int64_t blocks; const float* scale; int64_t ld_scale;
+    void* rows; int64_t ld_rows; float* row_scale; int64_t ld_row_scale;
+};
+struct CombineArgs {
+    int64_t T, rows; int top_k, N;                       // rows: of Y
+    const int32_t* place;
+    const void* Y; int64_t ldy;
+    const float* weight;
+    const void* add; int64_t ld_add;
+    void* out; int64_t ldo;
+};
+struct CombineGradArgs {
+    int64_t T, rows; int top_k, N;
+    const int32_t* place;
+    const void* dOut; int64_t lddo;
+    const float* weight;
+    const void* Y; int64_t ldy;
+    void* dY; int64_t lddy;
+    float* dweight;
+};
+int64_t ops_dispatch_workspace_bytes(int64_t choices, int64_t E);
+int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stream);
+int ops_launch_combine(int type, int out_type, const CombineArgs& a, hipStream_t stream);
+int ops_launch_combine_grad(int type, const CombineGradArgs& a, hipStream_t stream);

@@ -11,9 +11,18 @@ template <> struct Elem<ELEM_F16> { typedef half_t type; static constexpr int si
 template <> struct Elem<ELEM_BF16> { typedef bf16_t type; static constexpr int size = 2; };
 template <> struct Elem<ELEM_F32> { typedef float type; static constexpr int size = 4; };
 template <> struct Elem<ELEM_E4M3> { typedef uint8_t type; static constexpr int size = 1; };
+template <> struct Elem<ELEM_I8> { typedef int8_t type; static constexpr int size = 1; };
 
 // 8 elements of 16 bits at element alignment (one 16-byte access)
 template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8), aligned(2))); };
+
+// 16 x 16 sums of 64 products of 8-bit integers; the accumulators' 32-bit integers in registers that the kernels have as f32
+__device__ __forceinline__ floatx4 mfma_i8(uintx4 a, uintx4 b, floatx4 c)
+{
+    return __builtin_bit_cast(floatx4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, a), __builtin_bit_cast(intx4, b), __builtin_bit_cast(intx4, c), 0, 0, 0));
+}
+// a sum (bits of an integer) times the scales of its row and column, in this order: the scales' own product may leave f32's range
+__device__ __forceinline__ float scaled_sum(float bits, float row) { return (float)__builtin_bit_cast(int, bits) * row; }
 
 // magnitude as an integer: ordered as the magnitudes are, infinity above every number and NaN above infinity
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }

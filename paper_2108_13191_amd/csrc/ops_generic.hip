@@ -1,6 +1,6 @@
-// The products of include/gemm_ops.h for operands of any alignment: 64 x 64 tiles, four wavefronts of 32 x 32, every element
+// The products of include/gemm_ops.h and include/gemm_layer.h for operands of any alignment: 64 x 64 tiles, four wavefronts of 32 x 32, every element
 // loaded by itself (64 consecutive ones by a wavefront), brought to f16 or bf16 (e4m3 values are exact in f16) on the way into
-// LDS, and multiplied with 16 x 16 x 32 MFMAs.  e4m3: the sum over a block of 128 is formed by itself and added with its scales.
+// LDS, and multiplied with 16 x 16 x 32 MFMAs (8-bit integers stay what they are).  e4m3: the sum over a block of 128 is formed by itself and added with its scales.
 //
 // Bound by the element loads (32 a lane and k step of 64 against 8 MFMAs): 40 TFLOP/s.  Takes what the other forms do not: e4m3 operands that are not 16-byte
 // aligned, 16-bit ones with less than 8 elements a row, pitches beyond 2^22 elements.
@@ -14,15 +14,24 @@ using namespace ops_dev;
 constexpr int GT = 64, GK = 64, GP = GK + 8;      // tile, k step, LDS row pitch (elements): rows 16-byte aligned
 
 __device__ __forceinline__ half_t stage_value(uint8_t v) { return (half_t)__builtin_amdgcn_cvt_f32_fp8((int)v, 0); }
+__device__ __forceinline__ int8_t stage_value(int8_t v) { return v; }
 __device__ __forceinline__ half_t stage_value(half_t v) { return v; }
 __device__ __forceinline__ bf16_t stage_value(bf16_t v) { return v; }
 
 __device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ floatx4 mfma16(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+typedef int8_t int8x8 __attribute__((ext_vector_type(8)));
+// (half of the k of the instruction: its other half is zeros)
+__device__ __forceinline__ floatx4 mfma16(int8x8 a, int8x8 b, floatx4 c)
+{
+    const uintx2 x = __builtin_bit_cast(uintx2, a), y = __builtin_bit_cast(uintx2, b);
+    return mfma_i8(uintx4{x[0], x[1], 0u, 0u}, uintx4{y[0], y[1], 0u, 0u}, c);
+}
 
 template <int ELEM> struct Staged { typedef typename Elem<ELEM>::type type; typedef bf16x8 vec; };
 template <> struct Staged<ELEM_F16> { typedef half_t type; typedef half8 vec; };
 template <> struct Staged<ELEM_E4M3> { typedef half_t type; typedef half8 vec; };
+template <> struct Staged<ELEM_I8> { typedef int8_t type; typedef int8x8 vec; };
 
 // rows r0 .. of an operand (rows at or behind `rows` are zeros), k from k0 on (zeros at or behind `kend`) into LDS as [row][k]
 template <int ELEM, bool KC>
@@ -127,7 +136,9 @@ __global__ __launch_bounds__(256) void ops_generic_kernel(const OpsGemm g)
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 const int64_t col = n0 + wn + 16 * j + 4 * kq + r;
-                if (col < g.N) C[row * g.ldc + col] = (CT)(ELEM == ELEM_E4M3 ? acc[i][j][r] : part[i][j][r]);
+                if (col >= g.N) continue;
+                if constexpr (ELEM == ELEM_I8) C[row * g.ldc + col] = (CT)(scaled_sum(part[i][j][r], g.sa[row]) * g.sb[(int64_t)e * g.sb_stride + col]);
+                else C[row * g.ldc + col] = (CT)(ELEM == ELEM_E4M3 ? acc[i][j][r] : part[i][j][r]);
             }
     }
 }
@@ -158,5 +169,6 @@ int launch_layout(const OpsGemm& g)
 int ops_launch_generic(const OpsGemm& g)
 {
     if (g.elem == ELEM_E4M3) return launch<ELEM_E4M3, true, true>(g);
+    if (g.elem == ELEM_I8) return launch<ELEM_I8, true, true>(g);
     return g.elem == ELEM_F16 ? launch_layout<ELEM_F16>(g) : launch_layout<ELEM_BF16>(g);
 }

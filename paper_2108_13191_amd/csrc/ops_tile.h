@@ -1,9 +1,9 @@
 // The tiled kernel of the products of include/gemm_ops.h for 16-byte aligned operands: BM x BN results a workgroup, eight wavefronts,
-// k steps of 128 bytes a row (128 e4m3 values, 64 of 16 bits), f32 accumulators in registers.
+// k steps of 128 bytes a row (128 e4m3 values or 8-bit integers, 64 of 16 bits), 32-bit accumulators in registers.
 //
 // Operands with the summed index contiguous ("k rows") are staged as rows of 128 bytes and read 16 bytes a lane; those with the
 // other index contiguous as 64 k rows, read through transposing LDS reads.  Either way a fragment is 8 registers for 16 rows and a
-// whole k step: one 16 x 16 x 128 MFMA in e4m3, two 16 x 16 x 32 ones in 16 bits.  (e4m3: lanes 16 q .. of an operand hold
+// whole k step: one 16 x 16 x 128 MFMA in e4m3, two 16 x 16 x 64 ones in 8-bit integers, two 16 x 16 x 32 ones in 16 bits.  (8 bits: lanes 16 q .. of an operand hold
 // 16-byte chunks q and q + 4 of their row.  Which k a lane holds does not matter as long as A and B agree.)
 //
 // Schedule: wavefronts 0-3 (X) own the top half of the tile's rows, 4-7 (Y) the bottom half, each a quarter of the columns;
@@ -22,6 +22,7 @@
 // e4m3: each MFMA starts from zero and its 4 results are added to the accumulators times a_scale * b_scale, in f32.  With the B
 // fragment first a lane holds 4 columns of one row, so the factor is one register for a block of 16 x 16; the columns of a
 // wavefront lie in one block of 128, whose scale is a scalar.  The scales of the tile's rows come into LDS with the operands.
+// 8-bit integers: 32-bit integer sums all the way, scaled where they leave the registers.
 //
 // Measured.  256 x 256 x 8192^2 in e4m3: 437 us, 2.5 PFLOP/s, MFMAs busy 63 % at 1.87 GHz: the chip's power (zero operands: 354 us).  Shorter sums are bound by
 // what a tile does around its loop -- its group, the first copies, its stores, which all compute units do at once -- and by the last round of tiles: f16
@@ -78,6 +79,8 @@ template <int ELEM> __device__ __forceinline__ floatx4 mfma_step(const Frag& a, 
         const intx8 x = __builtin_bit_cast(intx8, (uintx8)__builtin_shufflevector(a.lo, a.hi, 0, 1, 2, 3, 4, 5, 6, 7));
         const intx8 y = __builtin_bit_cast(intx8, (uintx8)__builtin_shufflevector(b.lo, b.hi, 0, 1, 2, 3, 4, 5, 6, 7));
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 0, 0, 0, 0, 0, 0);
+    } else if constexpr (ELEM == ELEM_I8) {
+        return mfma_i8(a.hi, b.hi, mfma_i8(a.lo, b.lo, c));
     } else if constexpr (ELEM == ELEM_F16) {
         c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.lo), __builtin_bit_cast(half8, b.lo), c, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a.hi), __builtin_bit_cast(half8, b.hi), c, 0, 0, 0);
@@ -565,16 +568,32 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && F
     const int col = t.n0 + wn * WN + ocol, row_first = t.row0 + grp * HM + orow;
     CT* const C = (CT*)g.C + (int64_t)t.e * g.c_stride + (int64_t)row_first * g.ldc + col;
     typedef typename CVec4<CT>::type ctx4;
+    // i8: a lane has elements of FM rows here, and of 4 columns where it stores them
+    float row_scale[ELEM == ELEM_I8 ? FM : 1];
+    floatx4 col_scale = {1.0f, 1.0f, 1.0f, 1.0f};
+    if constexpr (ELEM == ELEM_I8) {
+#pragma unroll
+        for (int m = 0; m < FM; m++) row_scale[m] = g.sa[min(t.row0 + grp * HM + 16 * m + l16, t.row_end - 1)];
+        const float* const cs = g.sb + (int64_t)t.e * g.sb_stride;
+#pragma unroll
+        for (int e = 0; e < 4; e++) col_scale[e] = cs[min(col + e, g.N - 1)];
+    }
 #pragma unroll
     for (int m2 = 0; m2 < FM / 2; m2++) {
 #pragma unroll
         for (int r = 0; r < 2; r++)
 #pragma unroll
-            for (int n = 0; n < FN; n++)
+            for (int n = 0; n < FN; n++) {
+                if constexpr (ELEM == ELEM_I8) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[2 * m2 + r][n][e] = scaled_sum(acc[2 * m2 + r][n][e], row_scale[2 * m2 + r]);
+                }
                 *(__attribute__((address_space(3))) floatx4*)(uintptr_t)(buf + (16 * r + l16) * PITCH + (16 * n + 4 * q) * 4) = acc[2 * m2 + r][n];
+            }
 #pragma unroll
         for (int ps = 0; ps < 32 / RPP; ps++) {
-            const floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (RPP * ps + orow) * PITCH + ocol * 4);
+            floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (RPP * ps + orow) * PITCH + ocol * 4);
+            if constexpr (ELEM == ELEM_I8) v *= col_scale;
             const int r = 32 * m2 + RPP * ps;
             if (row_first + r < t.row_end) {
                 CT* const dst = C + (int64_t)r * g.ldc;
