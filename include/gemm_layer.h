@@ -59,9 +59,9 @@ int layer_norm_grad(int64_t M, int64_t N, int64_t type,
 /*
  * Quantise the rows of X (M x N of `type`, f16 or bf16; M x 2N for SWIGLU) to 8-bit integers, a scale for each row: a token's of
  * activations, a channel's of weights.
- *     scale[i] = max(largest |x| of row i, 2^-96) / 127 in f32,  element = the integer nearest to x / scale[i] (ties to even), from -127 to 127
+ *     scale[i] = max(largest |x| of row i, 2^-96) * (1/127) in f32, one product with the f32 value nearest to 1/127 (127 gives 1),  element = the integer nearest to x / scale[i] (ties to even), from -127 to 127
  * act is applied first, in f32, as in quantize_e4m3_rows.  A row that holds a NaN or an infinity gets the scale NaN and elements 0, so
- * that it shows in any product; a row of zeros is zeros with the scale 2^-96 / 127.
+ * that it shows in any product; a row of zeros is zeros with the scale 2^-96 * (1/127).
  */
 int quantize_i8_rows(int64_t M, int64_t N, int64_t type, int64_t act,
                      const void* X, int64_t ldx, void* Q, int64_t ldq, float* scale, void* stream);

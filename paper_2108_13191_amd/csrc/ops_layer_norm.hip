@@ -70,7 +70,7 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(uint32_t bits)
 {
     if (bits >= 0x7f800000u) return {__builtin_nanf(""), 0.0f, false};
-    const float scale = fmaxf(__builtin_bit_cast(float, bits), SCALE_FLOOR) / 127.0f;
+    const float scale = fmaxf(__builtin_bit_cast(float, bits), SCALE_FLOOR) * (1.0f / 127.0f);
     return {scale, 1.0f / scale, true};
 }
 __device__ __forceinline__ uintx2 to_i8(const float (&y)[8], const RowScale& s)

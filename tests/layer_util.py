@@ -51,7 +51,7 @@ def rounded(x, kind):
 def row_scales(y):
     """Of exactly known values: to the bit, as f32 has them; NaN of a row that is not finite."""
     most = np.maximum(np.abs(y).max(1).astype(np.float32), SCALE_FLOOR)
-    return np.where(np.isfinite(most), most / np.float32(127.0), np.float32(np.nan))
+    return np.where(np.isfinite(most), most * (np.float32(1) / np.float32(127)), np.float32(np.nan))
 
 
 def quantized(y):
