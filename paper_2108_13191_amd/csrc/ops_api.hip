@@ -77,9 +77,11 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
     // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
     const bool large = rows >= 192.0 && expected_tiles(g, 128, 128) >= 2.0 * cus;
     if (g.elem == ELEM_I8) {
+        // few rows, by streaming B, as in e4m3; up to 16 rows on 64 columns where that gives every compute unit a tile, as A comes to each by the same
+        // way as B: 16 rows of (16384,8192) 27.8 | 34 us (32 columns), (16384,4096) 13.2 | 14.2, 64 rows of 16 experts (4096,2048) 27.0 | 29.7
         if (allow_few_rows && ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0))) {
             const int fm = rows <= 16.0 ? 1 : 2;
-            const int nb = fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
+            const int nb = (fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus) || (fm == 1 && expected_tiles(g, 16, 64) >= cus) ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
             return few_rows(fm, nb);
         }
         return tiles(large ? TILE_256 : TILE_128);
@@ -143,7 +145,7 @@ const char* name_of(const OpsGemm& g, const Form& f)
 {
     if (f.kernel == Form::ANY) return "any_alignment_64x64";
     if (f.kernel == Form::FEW_ROWS)
-        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : "few_rows_16x32") : f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
+        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
     const bool e4m3 = g.elem == ELEM_E4M3;
     switch (f.tile) {
     case TILE_256: return e4m3 ? "e4m3_256x256" : "256x256";

@@ -65,7 +65,7 @@ int ops_launch_tiles_f16(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_bf16(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_i8(const OpsGemm& g, OpsTile tile);
 
-// ops_skinny.hip: few rows, e4m3 and i8; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
+// ops_skinny.hip: few rows, e4m3 and i8; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 1 x 4 (i8), 2 x 1, 2 x 2 or 2 x 4
 int ops_launch_skinny(const OpsGemm& g, int fm, int nb);
 
 // ops_norm.hip

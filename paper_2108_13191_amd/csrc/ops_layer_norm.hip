@@ -9,44 +9,59 @@ namespace {
 
 using namespace ops_dev;
 
+int launched() { return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH; }
+
 // ---- statistics of a row -----------------------------------------------------------------------------------------------------
-// Mean and sum of squares about it, of which each wavefront has those of its own elements: mean = sum of sums / N, and
-// squares about the row's mean = squares about the wavefront's own + n (its mean - the row's)^2.  So one exchange serves both.
-struct Moments { float mean, squares; };
-// W wavefronts a row; n_of(w): elements of the row's w-th wavefront; lds: 2 floats for each wavefront of the workgroup
-template <int W, typename F>
-__device__ __forceinline__ Moments row_moments(float sum, float squares, int N, float* lds, F n_of)
+// the sum of the L neighbouring threads that share a row, of a wavefront's where those are more than one
+template <int L>
+__device__ __forceinline__ float sum_lanes(float x)
 {
-    if constexpr (W == 1) return {sum / (float)N, squares};
+    if constexpr (L >= 64) return sum64(x);
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
+    return x;
+}
+// Mean and sum of squares about it, of which each wavefront has those of its own elements: the row's mean is that of the wavefronts' by their elements, and
+// squares about it are those about the wavefront's mean + n (its mean - the row's)^2.  So one exchange serves both.
+struct Moments { float mean, squares; };
+// n_of(w): elements of the row's w-th wavefront; lds: 2 floats for each wavefront of the workgroup
+template <int L, typename F>
+__device__ __forceinline__ Moments row_moments(float own_mean, float squares, int N, float* lds, F n_of)
+{
+    if constexpr (L <= 64) return {own_mean, squares};
+    constexpr int W = L > 64 ? L / 64 : 1;
     const int wave = threadIdx.x >> 6, first = wave / W * W;
-    if ((threadIdx.x & 63) == 0) { lds[2 * wave] = sum; lds[2 * wave + 1] = squares; }
+    if ((threadIdx.x & 63) == 0) { lds[2 * wave] = own_mean; lds[2 * wave + 1] = squares; }
     __syncthreads();
     float total = 0.0f, out = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W; w++) total += lds[2 * (first + w)];
+    for (int w = 0; w < W; w++) total += (float)n_of(w) * lds[2 * (first + w)];
     const float mean = total / (float)N;
 #pragma unroll
     for (int w = 0; w < W; w++) {
-        const int n = n_of(w);
-        const float d = n ? lds[2 * (first + w)] / (float)n - mean : 0.0f;
-        out += lds[2 * (first + w) + 1] + (float)n * d * d;
+        const float d = lds[2 * (first + w)] - mean, n = (float)n_of(w);
+        out += lds[2 * (first + w) + 1] + (n > 0.0f ? n * d * d : 0.0f);
     }
     return {mean, out};
 }
 
-// the largest of a row's magnitudes over its W wavefronts; lds: a word for each wavefront of the workgroup, used for nothing else
-template <int W>
+// the largest of a row's magnitudes over its L threads; lds: a word for each wavefront of the workgroup, used for nothing else
+template <int L>
 __device__ __forceinline__ uint32_t max_row(uint32_t m, uint32_t* lds)
 {
-    m = max16(m);
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-    if constexpr (W > 1) {
-        const int wave = threadIdx.x >> 6, first = wave / W * W;
+    if constexpr (L >= 16) m = max16(m);
+    else {
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+    }
+    if constexpr (L >= 32) m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+    if constexpr (L >= 64) m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    if constexpr (L > 64) {
+        const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
         if ((threadIdx.x & 63) == 0) lds[wave] = m;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; w++) m = max(m, lds[first + w]);
+        for (int w = 0; w < L / 64; w++) m = max(m, lds[first + w]);
     }
     return m;
 }
@@ -83,259 +98,386 @@ __device__ __forceinline__ uintx2 to_i8(const float (&y)[8], const RowScale& s)
 }
 
 // ---- the norm --------------------------------------------------------------------------------------------------------------------
-// W wavefronts a row, each lane with P chunks of 8 columns in registers; R rows a workgroup.  LOOP: rows of any length, whose chunks are gone
-// through once for each of: the mean, the squares, the largest magnitude, the outputs.
-template <typename T, int W, int P, int R, bool LOOP>
-__global__ __launch_bounds__(64 * W * R) void layer_norm_kernel(const LayerNormArgs a)
+// L threads a row, each with P chunks of 8 columns in registers; R rows a workgroup.
+template <typename T, int L, int P, int R>
+__global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a)
 {
-    __shared__ float lds[3 * W * R];
-    const int lane = threadIdx.x % (64 * W);
-    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / (64 * W);
+    __shared__ float lds[L * R / 64 * 3];
+    const int lane = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L, there = min(row, (int64_t)a.M - 1);
     const bool live = row < a.M;
+    const T* const x = (const T*)a.X + there * a.ldx;
+    const T* const r = a.R ? (const T*)a.R + there * a.ldr : nullptr;
+
+    Raw8<T> raw[P], res[P], gamma[P], beta[P];            // all asked for ahead of the sums
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p);
+        raw[p] = load8_of(x, c, a.N);
+        if (r) res[p] = load8_of(r, c, a.N);
+        gamma[p] = load8_of((const T*)a.gamma, c, a.N);
+        if (a.beta) beta[p] = load8_of((const T*)a.beta, c, a.N);
+    }
+    float v[P][8], sum = 0.0f, squares = 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p);
+        raw[p] = settled<T>(raw[p], c, a.N);
+        if (r) res[p] = settled<T>(res[p], c, a.N);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            v[p][i] = (float)raw[p][i];
+            if (r) v[p][i] = rounded<T>(v[p][i] + (float)res[p][i]);         // h as it is stored is what is normed
+            sum += v[p][i];
+        }
+        if (a.H && live && c < a.N) store8((T*)a.H + row * a.ldh + c, a.N - c, v[p]);
+    }
+    auto n_of = [&](int w) {                              // elements of the row's w-th wavefront
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < P; p++) n += min(max(a.N - 8 * (64 * w + L * p), 0), 512);
+        return n;
+    };
+    sum = sum_lanes<L>(sum);
+    const int own = L <= 64 ? a.N : n_of((threadIdx.x >> 6) % (L >= 64 ? L / 64 : 1));
+    const float centre = own ? sum / (float)own : 0.0f;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        const int left = a.N - 8 * (lane + L * p);
+#pragma unroll
+        for (int i = 0; i < 8; i++) { const float d = i < left ? v[p][i] - centre : 0.0f; squares += d * d; }
+    }
+    const Moments m = row_moments<L>(centre, sum_lanes<L>(squares), a.N, lds, n_of);
+    const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
+    if (live && lane == 0) {
+        if (a.mean) a.mean[row] = m.mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    if (!a.Y && !a.Q) return;
+    uint32_t big = 0;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p), left = a.N - c;
+        gamma[p] = settled<T>(gamma[p], c, a.N);
+        if (a.beta) beta[p] = settled<T>(beta[p], c, a.N);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float y = (v[p][i] - m.mean) * rstd * (float)gamma[p][i];
+            if (a.beta) y += (float)beta[p][i];
+            v[p][i] = i < left ? y : 0.0f;
+            big = max(big, magnitude(v[p][i]));
+        }
+        if (a.Y && live && left > 0) store8((T*)a.Y + row * a.ldy + c, left, v[p]);
+    }
+    if (!a.Q) return;
+    const RowScale s = row_scale(max_row<L>(big, (uint32_t*)&lds[L * R / 64 * 2]));
+    if (!live) return;
+    if (lane == 0) a.scale[row] = s.scale;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p);
+        if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
+    }
+}
+
+// Rows of any length, a workgroup each: its chunks are gone through once for each of the mean, the squares, the largest magnitude, the outputs.
+constexpr int LONG = 1024;
+template <typename T>
+__global__ __launch_bounds__(LONG) void layer_norm_long_kernel(const LayerNormArgs a)
+{
+    __shared__ float lds[LONG / 64 * 3];
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x, first = 8 * (int64_t)lane, step = 8 * LONG;
     const T* const x = (const T*)a.X + row * a.ldx;
     const T* const r = a.R ? (const T*)a.R + row * a.ldr : nullptr;
     T* const h = a.H ? (T*)a.H + row * a.ldh : nullptr;
-    auto form = [&](int64_t c, float (&o)[8]) {
+    float sum = 0.0f, squares = 0.0f, o[8];
+    auto form = [&](int64_t c) {
         load8(x + c, (int)(a.N - c), o);
         if (r) {
             float s[8];
             load8(r + c, (int)(a.N - c), s);
 #pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = rounded<T>(o[i] + s[i]);      // h as it is stored is what is normed
+            for (int i = 0; i < 8; i++) o[i] = rounded<T>(o[i] + s[i]);
         }
     };
-    // y from h, zeros behind the row's end
-    auto normed = [&](float (&o)[8], int left, float mean, float rstd, const Raw8<T>& gm, const Raw8<T>& bt) {
+    auto again = [&](int64_t c) { if (h) load8((const T*)h + c, (int)(a.N - c), o); else form(c); };
+    for (int64_t c = first; c < a.N; c += step) {
+        form(c);
+        if (h) store8(h + c, (int)(a.N - c), o);
 #pragma unroll
-        for (int i = 0; i < 8; i++) { const float y = (o[i] - mean) * rstd * (float)gm[i] + (float)bt[i]; o[i] = i < left ? y : 0.0f; }
+        for (int i = 0; i < 8; i++) sum += o[i];
+    }
+    sum = sum64(sum);
+    auto n_of = [&](int w) {                              // whole rounds of the workgroup, and what the last one leaves
+        const int rounds = a.N / (8 * LONG), rest = a.N - rounds * (8 * LONG);
+        return 512 * rounds + min(max(rest - 512 * w, 0), 512);
     };
-    auto beta_at = [&](int64_t c) { return load8_raw((const T*)a.beta + c, a.beta ? (int)(a.N - c) : 0); };
-    uint32_t* const most = (uint32_t*)&lds[2 * W * R];
-
-    if constexpr (!LOOP) {
-        float v[P][8], sum = 0.0f, squares = 0.0f;
-        Raw8<T> gamma[P], beta[P];                        // asked for ahead of the sums
+    const int own = n_of(threadIdx.x >> 6);
+    const float centre = own ? sum / (float)own : 0.0f;
+    for (int64_t c = first; c < a.N; c += step) {
+        again(c);
 #pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (live && c < a.N) {
-                form(c, v[p]);
-                gamma[p] = load8_raw((const T*)a.gamma + c, a.N - c);
-                beta[p] = beta_at(c);
-            } else {
+        for (int i = 0; i < 8; i++) { const float d = c + i < a.N ? o[i] - centre : 0.0f; squares += d * d; }
+    }
+    const Moments m = row_moments<LONG>(centre, sum64(squares), a.N, lds, n_of);
+    const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = m.mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    if (!a.Y && !a.Q) return;
+    uint32_t big = 0;
+    auto output = [&](int64_t c) {
+        const int left = (int)min((int64_t)8, a.N - c);
+        again(c);
+        const Raw8<T> gm = load8_raw((const T*)a.gamma + c, left), bt = load8_raw((const T*)a.beta + c, a.beta ? left : 0);
 #pragma unroll
-                for (int i = 0; i < 8; i++) { v[p][i] = 0.0f; gamma[p][i] = beta[p][i] = (T)0.0f; }
-            }
-        }
+        for (int i = 0; i < 8; i++) { const float y = (o[i] - m.mean) * rstd * (float)gm[i] + (float)bt[i]; o[i] = i < left ? y : 0.0f; }
+    };
+    for (int64_t c = first; c < a.N; c += step) {
+        output(c);
+        if (a.Y) store8((T*)a.Y + row * a.ldy + c, (int)(a.N - c), o);
 #pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (h && live && c < a.N) store8(h + c, a.N - c, v[p]);
-#pragma unroll
-            for (int i = 0; i < 8; i++) sum += v[p][i];
-        }
-        auto n_of = [&](int w) {
-            int n = 0;
-#pragma unroll
-            for (int p = 0; p < P; p++) n += min(max(a.N - 512 * (w + W * p), 0), 512);
-            return n;
-        };
-        sum = sum64(sum);
-        const int own = n_of((threadIdx.x >> 6) % W);
-        const float centre = own ? sum / (float)own : 0.0f;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int left = a.N - 8 * (lane + 64 * W * p);
-#pragma unroll
-            for (int i = 0; i < 8; i++) { const float d = i < left ? v[p][i] - centre : 0.0f; squares += d * d; }
-        }
-        const Moments m = row_moments<W>(sum, sum64(squares), a.N, lds, n_of);
-        const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
-        if (live && lane == 0) {
-            if (a.mean) a.mean[row] = m.mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        if (!a.Y && !a.Q) return;
-        uint32_t big = 0;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            normed(v[p], a.N - c, m.mean, rstd, gamma[p], beta[p]);
-            if (a.Y && live && c < a.N) store8((T*)a.Y + row * a.ldy + c, a.N - c, v[p]);
-#pragma unroll
-            for (int i = 0; i < 8; i++) big = max(big, magnitude(v[p][i]));
-        }
-        if (!a.Q) return;
-        const RowScale s = row_scale(max_row<W>(big, most));
-        if (!live) return;
-        if (lane == 0) a.scale[row] = s.scale;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
-        }
-    } else {
-        static_assert(R == 1, "a workgroup has one row, which is there");
-        float sum = 0.0f, squares = 0.0f, o[8];
-        int own = 0;
-        auto again = [&](int64_t c) { if (h) load8((const T*)h + c, (int)(a.N - c), o); else form(c, o); };
-        const int64_t first = 8 * (int64_t)lane, step = 512 * W;
-        for (int64_t c = first; c < a.N; c += step) {
-            form(c, o);
-            if (h) store8(h + c, (int)(a.N - c), o);
-#pragma unroll
-            for (int i = 0; i < 8; i++) sum += o[i];
-        }
-        sum = sum64(sum);
-        auto n_of = [&](int w) {                          // whole rounds of 512 W columns, and what the last one leaves
-            const int rounds = a.N / (512 * W), rest = a.N - rounds * (512 * W);
-            return 512 * rounds + min(max(rest - 512 * w, 0), 512);
-        };
-        own = n_of(threadIdx.x >> 6);
-        const float centre = own ? sum / (float)own : 0.0f;
-        for (int64_t c = first; c < a.N; c += step) {
-            again(c);
-#pragma unroll
-            for (int i = 0; i < 8; i++) { const float d = c + i < a.N ? o[i] - centre : 0.0f; squares += d * d; }
-        }
-        const Moments m = row_moments<W>(sum, sum64(squares), a.N, lds, n_of);
-        const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
-        if (lane == 0) {
-            if (a.mean) a.mean[row] = m.mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        if (!a.Y && !a.Q) return;
-        uint32_t big = 0;
-        auto output = [&](int64_t c) {
-            const int left = (int)min((int64_t)8, a.N - c);
-            again(c);
-            normed(o, left, m.mean, rstd, load8_raw((const T*)a.gamma + c, left), beta_at(c));
-        };
-        for (int64_t c = first; c < a.N; c += step) {
-            output(c);
-            if (a.Y) store8((T*)a.Y + row * a.ldy + c, (int)(a.N - c), o);
-#pragma unroll
-            for (int i = 0; i < 8; i++) big = max(big, magnitude(o[i]));
-        }
-        if (!a.Q) return;
-        const RowScale s = row_scale(max_row<W>(big, most));
-        if (lane == 0) a.scale[row] = s.scale;
-        for (int64_t c = first; c < a.N; c += step) {
-            output(c);
-            store_bytes(a.Q + row * a.ldq + c, (int)(a.N - c), to_i8(o, s));
-        }
+        for (int i = 0; i < 8; i++) big = max(big, magnitude(o[i]));
+    }
+    if (!a.Q) return;
+    const RowScale s = row_scale(max_row<LONG>(big, (uint32_t*)&lds[LONG / 64 * 2]));
+    if (lane == 0) a.scale[row] = s.scale;
+    for (int64_t c = first; c < a.N; c += step) {
+        output(c);
+        store_bytes(a.Q + row * a.ldq + c, (int)(a.N - c), to_i8(o, s));
     }
 }
 
-template <typename T, int W, int P, int R, bool LOOP = false>
+template <typename T, int L, int P, int R>
 int launch_norm(const LayerNormArgs& a, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)(((int64_t)a.M + R - 1) / R);
-    hipLaunchKernelGGL((layer_norm_kernel<T, W, P, R, LOOP>), dim3(grid), dim3(64 * W * R), 0, stream, a);
-    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+    hipLaunchKernelGGL((layer_norm_kernel<T, L, P, R>), dim3((unsigned)(((int64_t)a.M + R - 1) / R)), dim3(L * R), 0, stream, a);
+    return launched();
 }
 template <typename T>
 int norm_of_type(const LayerNormArgs& a, hipStream_t stream)
 {
-    if (a.M <= 2 * chip().cus && a.N > 2048 && a.N <= 8192) return launch_norm<T, 16, 1, 1>(a, stream);
-    if (a.N <= 512) return launch_norm<T, 1, 1, 4>(a, stream);
-    if (a.N <= 1024) return launch_norm<T, 1, 2, 4>(a, stream);
-    if (a.N <= 2048) return launch_norm<T, 1, 4, 4>(a, stream);
-    if (a.N <= 4096) return launch_norm<T, 4, 2, 1>(a, stream);
-    if (a.N <= 8192) return launch_norm<T, 4, 4, 1>(a, stream);
-    if (a.N <= 16384) return launch_norm<T, 8, 4, 1>(a, stream);
-    return launch_norm<T, 16, 1, 1, true>(a, stream);
+    if (a.M <= 2 * chip().cus && a.N > 2048 && a.N <= 8192) return launch_norm<T, 1024, 1, 1>(a, stream);
+    if (a.N <= 64) return launch_norm<T, 8, 1, 32>(a, stream);
+    if (a.N <= 128) return launch_norm<T, 16, 1, 16>(a, stream);
+    if (a.N <= 256) return launch_norm<T, 32, 1, 8>(a, stream);
+    if (a.N <= 512) return launch_norm<T, 64, 1, 4>(a, stream);
+    if (a.N <= 1024) return launch_norm<T, 64, 2, 4>(a, stream);
+    if (a.N <= 2048) return launch_norm<T, 64, 4, 4>(a, stream);
+    if (a.N <= 4096) return launch_norm<T, 256, 2, 1>(a, stream);
+    if (a.N <= 8192) return launch_norm<T, 256, 4, 1>(a, stream);
+    if (a.N <= 16384) return launch_norm<T, 512, 4, 1>(a, stream);
+    hipLaunchKernelGGL(layer_norm_long_kernel<T>, dim3((unsigned)a.M), dim3(LONG), 0, stream, a);
+    return launched();
 }
 
 // ---- its gradients -----------------------------------------------------------------------------------------------------------------
-// dX row by row; the columns' sums of dy xhat and dy stay in registers over all rows of a workgroup, which writes them as one row of the
-// workspace; a second kernel adds those.  Every sum has a fixed order.
-template <typename T, int W, int P, int R>
-__global__ __launch_bounds__(64 * W * R) void layer_norm_grad_kernel(const LayerNormGradArgs a)
+// A row of dY, H and dH, chunks of 8 columns of one of its L threads; rows behind the last one are that one, with nothing in dy
+template <typename T, int L, int P>
+struct GradRow {
+    Raw8<T> dy[P], h[P], dh[P];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const LayerNormGradArgs& a, int lane, int64_t row)
+    {
+        row = min(row, (int64_t)a.M - 1);
+        rstd = a.rstd[row];
+        mean = a.mean[row];
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + L * p);
+            dy[p] = load8_of((const T*)a.dY + row * a.lddy, c, a.N);
+            h[p] = load8_of((const T*)a.H + row * a.ldh, c, a.N);
+            if (a.dH) dh[p] = load8_of((const T*)a.dH + row * a.lddh, c, a.N);
+        }
+    }
+    __device__ __forceinline__ void settle(const LayerNormGradArgs& a, int lane, bool live)
+    {
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + L * p);
+            dy[p] = settled<T>(dy[p], live ? c : (int64_t)a.N + 8, a.N);
+            h[p] = settled<T>(h[p], c, a.N);
+            if (a.dH) dh[p] = settled<T>(dh[p], c, a.N);
+        }
+    }
+    // from the sums of g and g xhat
+    __device__ __forceinline__ void store(const LayerNormGradArgs& a, int lane, int64_t row, const Raw8<T> (&gamma)[P], float s1, float s2) const
+    {
+        const float m1 = s1 / (float)a.N, m2 = s2 / (float)a.N;
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int c = 8 * (lane + L * p);
+            if (c >= a.N) continue;
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                o[i] = rstd * ((float)dy[p][i] * (float)gamma[p][i] - m1 - ((float)h[p][i] - mean) * rstd * m2);
+                if (a.dH) o[i] += (float)dh[p][i];
+            }
+            store8((T*)a.dX + row * a.lddx + c, a.N - c, o);
+        }
+    }
+};
+// two sums over the L threads that share a row; set: 2 floats for each wavefront of the workgroup
+template <int L>
+__device__ __forceinline__ void sum_pair(float& x, float& y, float* set)
 {
-    extern __shared__ float dyn[];                        // 4 W R floats, then R * 512 W of sums
-    const int lane = threadIdx.x % (64 * W), sub = threadIdx.x / (64 * W), wave = threadIdx.x >> 6;
+    if constexpr (L < 64) {
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) { x += __shfl_xor(x, d); y += __shfl_xor(y, d); }
+    } else {
+        x = sum64(x);
+        y = sum64(y);
+    }
+    if constexpr (L > 64) {
+        const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
+        if ((threadIdx.x & 63) == 0) { set[2 * wave] = x; set[2 * wave + 1] = y; }
+        __syncthreads();
+        x = y = 0.0f;
+#pragma unroll
+        for (int i = 0; i < L / 64; i++) { x += set[2 * (first + i)]; y += set[2 * (first + i) + 1]; }
+    }
+}
+
+// dX row by row; the columns' sums of dy xhat and dy stay in registers over all rows of a workgroup, which writes them as one row of the
+// workspace; a second kernel adds those.  Every sum has a fixed order.  L threads a row, R rows a workgroup, P chunks of 8 columns a thread.
+template <typename T, int L, int P, int R>
+__global__ __launch_bounds__(L * R) void layer_norm_grad_kernel(const LayerNormGradArgs a)
+{
+    extern __shared__ float dyn[];                        // 4 floats for each wavefront, then R * 8 L of sums
+    const int lane = threadIdx.x % L, sub = threadIdx.x / L;
+    constexpr int WAVES = L * R / 64;
     float dg[P][8] = {}, db[P][8] = {};
     Raw8<T> gamma[P];
 #pragma unroll
-    for (int p = 0; p < P; p++) gamma[p] = load8_raw((const T*)a.gamma + 8 * (lane + 64 * W * p), a.N - 8 * (lane + 64 * W * p));
+    for (int p = 0; p < P; p++) gamma[p] = settled<T>(load8_of((const T*)a.gamma, 8 * (lane + L * p), a.N), 8 * (lane + L * p), a.N);
+    // the values as they were loaded, to be widened again: kept widened over the sums they would take twice the registers
+    auto again = [](Raw8<T>& x) { uintx4 r = __builtin_bit_cast(uintx4, x); asm volatile("" : "+v"(r)); x = __builtin_bit_cast(Raw8<T>, r); };
 
     const int64_t step = (int64_t)gridDim.x * R;
     int slot = 0;
+    constexpr bool AHEAD = L * R <= 512;                  // the next row's loads ahead: registers for it where a workgroup has 512 threads
+    GradRow<T, L, P> next;
+    if constexpr (AHEAD) next.load(a, lane, (int64_t)blockIdx.x * R + sub);
     for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.M; row0 += step) {      // the same number of trips for the whole workgroup
         const int64_t row = row0 + sub;
         const bool live = row < a.M;
-        Raw8<T> dyr[P], hr[P], dhr[P];
-        const float rstd = live ? a.rstd[row] : 0.0f, mean = live ? a.mean[row] : 0.0f;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p), left = live ? a.N - c : 0;      // not above 0: nothing is read
-            dyr[p] = load8_raw((const T*)a.dY + row * a.lddy + c, left);
-            hr[p] = load8_raw((const T*)a.H + row * a.ldh + c, left);
-        }
-        if (a.dH) {
-#pragma unroll
-            for (int p = 0; p < P; p++) dhr[p] = load8_raw((const T*)a.dH + row * a.lddh + 8 * (lane + 64 * W * p), live ? a.N - 8 * (lane + 64 * W * p) : 0);
-        }
+        if constexpr (!AHEAD) next.load(a, lane, row);
+        GradRow<T, L, P> x = next;
+        x.settle(a, lane, live);
         float s1 = 0.0f, s2 = 0.0f;                       // of g and g xhat; dy is zero behind the row's end
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float dy = (float)dyr[p][i], xhat = ((float)hr[p][i] - mean) * rstd, g = dy * (float)gamma[p][i];
+                const float dy = (float)x.dy[p][i], xhat = ((float)x.h[p][i] - x.mean) * x.rstd, g = dy * (float)gamma[p][i];
                 dg[p][i] += dy * xhat;
                 db[p][i] += dy;
                 s1 += g;
                 s2 += g * xhat;
             }
-        s1 = sum64(s1);
-        s2 = sum64(s2);
-        if constexpr (W > 1) {                            // two sets of partial sums in turn: one barrier a row
-            float* const set = dyn + slot * 2 * W * R;
-            if ((threadIdx.x & 63) == 0) { set[2 * wave] = s1; set[2 * wave + 1] = s2; }
-            __syncthreads();
-            s1 = s2 = 0.0f;
+        if constexpr (AHEAD) next.load(a, lane, row + step);      // while this row's sums are exchanged and its gradient is formed
 #pragma unroll
-            for (int i = 0; i < W; i++) { s1 += set[2 * (wave / W * W + i)]; s2 += set[2 * (wave / W * W + i) + 1]; }
-            slot ^= 1;
-        }
-        const float m1 = s1 / (float)a.N, m2 = s2 / (float)a.N;
-        if (!live) continue;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (c >= a.N) continue;
-            float o[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                o[i] = rstd * ((float)dyr[p][i] * (float)gamma[p][i] - m1 - ((float)hr[p][i] - mean) * rstd * m2);
-                if (a.dH) o[i] += (float)dhr[p][i];
-            }
-            store8((T*)a.dX + row * a.lddx + c, a.N - c, o);
-        }
+        for (int p = 0; p < P; p++) { again(x.dy[p]); again(x.h[p]); again(gamma[p]); }
+        sum_pair<L>(s1, s2, dyn + slot * 2 * WAVES);      // two sets of partial sums in turn: one barrier a row
+        slot ^= 1;
+        if (live) x.store(a, lane, row, gamma, s1, s2);
     }
     if (!a.dgamma && !a.dbeta) return;
-    // sums of the workgroup's row slots, in their order, 512 W columns at a time
-    float* const sums = dyn + 4 * W * R;
+    // sums of the workgroup's row slots, in their order, 8 L columns at a time
+    float* const sums = dyn + 4 * WAVES;
     const bool only = gridDim.x == 1;                     // one workgroup's sums are the result
     auto put = [&](const float (&d)[P][8], float* out) {
 #pragma unroll
         for (int p = 0; p < P; p++) {
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) *(floatx4*)&sums[sub * 512 * W + 8 * lane + i] = floatx4{d[p][i], d[p][i + 1], d[p][i + 2], d[p][i + 3]};
+            for (int i = 0; i < 8; i += 4) *(floatx4*)&sums[sub * 8 * L + 8 * lane + i] = floatx4{d[p][i], d[p][i + 1], d[p][i + 2], d[p][i + 3]};
             __syncthreads();
-            for (int j = threadIdx.x; j < 512 * W; j += 64 * W * R) {
-                const int c = 512 * W * p + j;
+            for (int j = threadIdx.x; j < 8 * L; j += L * R) {
+                const int c = 8 * L * p + j;
                 float s = sums[j];
 #pragma unroll
-                for (int r = 1; r < R; r++) s += sums[r * 512 * W + j];
+                for (int r = 1; r < R; r++) s += sums[r * 8 * L + j];
                 if (c < a.N) out[c] = s;
             }
         }
     };
     if (a.dgamma) put(dg, only ? a.dgamma : a.ws + (int64_t)blockIdx.x * 2 * a.N);
     if (a.dbeta) put(db, only ? a.dbeta : a.ws + ((int64_t)blockIdx.x * 2 + 1) * a.N);
+}
+
+// Few rows: one launch.  The columns' sums need nothing of the rows' sums, so some workgroups form dX and others read the rows once more for 64 columns of dgamma and dbeta: 8
+// threads of 8 columns, 64 rows at a time.
+template <typename T, int L, int P>
+__global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNormGradArgs a, int row_groups)
+{
+    __shared__ float lds[2][64][65];
+    if ((int)blockIdx.x < row_groups) {
+        const int lane = threadIdx.x % L;
+        const int64_t row = (int64_t)blockIdx.x * (512 / L) + threadIdx.x / L;
+        const bool live = row < a.M;
+        GradRow<T, L, P> x;
+        Raw8<T> gamma[P];
+        x.load(a, lane, row);
+#pragma unroll
+        for (int p = 0; p < P; p++) gamma[p] = load8_of((const T*)a.gamma, 8 * (lane + L * p), a.N);
+        x.settle(a, lane, live);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            gamma[p] = settled<T>(gamma[p], 8 * (lane + L * p), a.N);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float g = (float)x.dy[p][i] * (float)gamma[p][i];
+                s1 += g;
+                s2 += g * (((float)x.h[p][i] - x.mean) * x.rstd);
+            }
+        }
+        sum_pair<L>(s1, s2, &lds[0][0][0]);
+        if (live) x.store(a, lane, row, gamma, s1, s2);
+        return;
+    }
+    const int lane = threadIdx.x & 7, sub = threadIdx.x >> 3;
+    const int64_t c = ((int64_t)blockIdx.x - row_groups) * 64 + 8 * lane;
+    float dg[8] = {}, db[8] = {};
+    auto add = [&](Raw8<T> dy, Raw8<T> h, float mean, float rstd, bool live) {
+        dy = settled<T>(dy, live ? c : (int64_t)a.N + 8, a.N);
+        h = settled<T>(h, c, a.N);
+#pragma unroll
+        for (int i = 0; i < 8; i++) { dg[i] += (float)dy[i] * (((float)h[i] - mean) * rstd); db[i] += (float)dy[i]; }
+    };
+    constexpr int AT_ONCE = 4;
+    for (int64_t row0 = sub; row0 - sub < a.M; row0 += 64 * AT_ONCE) {
+        Raw8<T> dy[AT_ONCE], h[AT_ONCE];
+        float mean[AT_ONCE], rstd[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const int64_t row = min(row0 + 64 * u, (int64_t)a.M - 1);
+            dy[u] = load8_of((const T*)a.dY + row * a.lddy, c, a.N);
+            h[u] = load8_of((const T*)a.H + row * a.ldh, c, a.N);
+            mean[u] = a.mean[row];
+            rstd[u] = a.rstd[row];
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) add(dy[u], h[u], mean[u], rstd[u], row0 + 64 * u < a.M);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) { lds[0][8 * lane + i][sub] = dg[i]; lds[1][8 * lane + i][sub] = db[i]; }
+    __syncthreads();
+    // a wavefront adds the 64 rows' slots of a column: 8 of each kind
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const int64_t col = ((int64_t)blockIdx.x - row_groups) * 64 + 8 * wave + i;
+        const float g = sum64(lds[0][8 * wave + i][threadIdx.x & 63]), b = sum64(lds[1][8 * wave + i][threadIdx.x & 63]);
+        if ((threadIdx.x & 63) == 0 && col < a.N) {
+            if (a.dgamma) a.dgamma[col] = g;
+            if (a.dbeta) a.dbeta[col] = b;
+        }
+    }
 }
 
 // Rows longer than the registers hold: dX in two passes over a row ...
@@ -402,122 +544,162 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restri
     }
 }
 
-// rows a workgroup of the gradient takes at a time
-inline int grad_rows(int64_t N) { return N <= 1024 ? 16 : N <= 2048 ? 8 : N <= 4096 ? 4 : N <= 8192 ? 2 : 1; }
+// threads that share a row in the gradient, and rows that a workgroup takes at a time
+inline int grad_rows(int64_t N) { return N <= 64 ? 64 : N <= 128 ? 32 : N <= 512 ? 16 : N <= 1024 ? 8 : N <= 2048 ? 4 : N <= 4096 ? 2 : 1; }
+// Whether one launch forms everything, us | two launches.  Up to 512 rows, 768 of more than 512 columns: (512,768) 6.0 | 7.7, (512,4096) 8.5 | 12.8, (768,8192) 15.6 | 18.2, (512,64) 5.7 | 5.9; more:
+// (700,64) 7.0 | 6.1, (1024,768) 9.2 | 8.4, (2048,4096) 28 | 20.  Rows of more than 8192, whose columns' sums leave no registers for the next row: (2048,16384) 70 | 93, (6000,10000) 141 | 193.
+// Not where dX takes dY's place, which is read twice.
+inline bool grad_few(const LayerNormGradArgs& a)
+{
+    if (a.N > 16384 || a.M > LAUNCH_ROWS) return false;
+    if (!a.dgamma && !a.dbeta) return true;
+    return a.dX != a.dY && (a.M <= 512 || (a.N > 512 && a.M <= 768) || a.N > 8192);
+}
 
-template <typename T, int W, int P, int R>
+template <typename T, int L, int P, int R>
 int launch_norm_grad(const LayerNormGradArgs& a, int parts, hipStream_t stream)
 {
-    hipLaunchKernelGGL((layer_norm_grad_kernel<T, W, P, R>), dim3((unsigned)parts), dim3(64 * W * R), (4 * W * R + R * 512 * W) * sizeof(float), stream, a);
-    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+    hipLaunchKernelGGL((layer_norm_grad_kernel<T, L, P, R>), dim3((unsigned)parts), dim3(L * R), (L * R / 16 + R * 8 * L) * sizeof(float), stream, a);
+    return launched();
+}
+template <typename T, int L, int P>
+int launch_norm_grad_few(const LayerNormGradArgs& a, hipStream_t stream)
+{
+    const int row_groups = (a.M + 512 / L - 1) / (512 / L), columns = a.dgamma || a.dbeta ? (a.N + 63) / 64 : 0;
+    hipLaunchKernelGGL((layer_norm_grad_few_kernel<T, L, P>), dim3((unsigned)(row_groups + columns)), dim3(512), 0, stream, a, row_groups);
+    return launched();
 }
 template <typename T>
 int norm_grad_of_type(const LayerNormGradArgs& a, hipStream_t stream)
 {
-    const int parts = ops_layer_norm_grad_parts(a.M, a.N);
     const bool columns = a.dgamma || a.dbeta;
+    if (a.M > 0 && grad_few(a)) {
+        if (a.N <= 64) return launch_norm_grad_few<T, 8, 1>(a, stream);
+        if (a.N <= 256) return launch_norm_grad_few<T, 32, 1>(a, stream);
+        if (a.N <= 512) return launch_norm_grad_few<T, 64, 1>(a, stream);
+        if (a.N <= 1024) return launch_norm_grad_few<T, 128, 1>(a, stream);
+        if (a.N <= 2048) return launch_norm_grad_few<T, 256, 1>(a, stream);
+        if (a.N <= 4096) return launch_norm_grad_few<T, 512, 1>(a, stream);
+        return a.N <= 8192 ? launch_norm_grad_few<T, 512, 2>(a, stream) : launch_norm_grad_few<T, 512, 4>(a, stream);
+    }
+    const int parts = ops_layer_norm_grad_parts(a.M, a.N);
     int rc = GEMM_F16_OK;
     if (a.M > 0) {
-        if (a.N <= 512) rc = launch_norm_grad<T, 1, 1, 16>(a, parts, stream);
-        else if (a.N <= 1024) rc = launch_norm_grad<T, 1, 2, 16>(a, parts, stream);
-        else if (a.N <= 2048) rc = launch_norm_grad<T, 2, 2, 8>(a, parts, stream);
-        else if (a.N <= 4096) rc = launch_norm_grad<T, 4, 2, 4>(a, parts, stream);
-        else if (a.N <= 8192) rc = launch_norm_grad<T, 8, 2, 2>(a, parts, stream);
-        else if (a.N <= 16384) rc = launch_norm_grad<T, 16, 2, 1>(a, parts, stream);
+        if (a.N <= 64) rc = launch_norm_grad<T, 8, 1, 64>(a, parts, stream);
+        else if (a.N <= 128) rc = launch_norm_grad<T, 16, 1, 32>(a, parts, stream);
+        else if (a.N <= 256) rc = launch_norm_grad<T, 32, 1, 16>(a, parts, stream);
+        else if (a.N <= 512) rc = launch_norm_grad<T, 64, 1, 16>(a, parts, stream);
+        else if (a.N <= 1024) rc = launch_norm_grad<T, 64, 2, 8>(a, parts, stream);
+        else if (a.N <= 2048) rc = launch_norm_grad<T, 128, 2, 4>(a, parts, stream);
+        else if (a.N <= 4096) rc = launch_norm_grad<T, 256, 2, 2>(a, parts, stream);
+        else if (a.N <= 8192) rc = launch_norm_grad<T, 512, 2, 1>(a, parts, stream);
+        else if (a.N <= 16384) rc = launch_norm_grad<T, 1024, 2, 1>(a, parts, stream);
         else {
             if (!fits_a_launch(a.M, 1024)) return GEMM_F16_ERR_SIZE;
             if (columns) hipLaunchKernelGGL(layer_norm_columns_long_kernel<T>, dim3((unsigned)(((int64_t)a.N + 2047) / 2048), (unsigned)parts), dim3(256), 0, stream, a);
             hipLaunchKernelGGL(layer_norm_grad_long_kernel<T>, dim3((unsigned)a.M), dim3(1024), 0, stream, a);
-            rc = hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+            rc = launched();
         }
         if (rc != GEMM_F16_OK) return rc;
     }
     if (!columns || (parts == 1 && a.N <= 16384)) return rc;
     hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)(((int64_t)a.N + 63) / 64), 2), dim3(1024), 0, stream, a.ws, parts, a.N, a.dgamma, a.dbeta);
-    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+    return launched();
 }
 
 // ---- rows to 8-bit integers ----------------------------------------------------------------------------------------------------------
+// values of x (and u, of SWIGLU) after the activation
 template <typename T, int ACT>
-__device__ __forceinline__ void activated8(const T* x, int64_t N, int64_t c, float (&v)[8])
+__device__ __forceinline__ void activated8(const Raw8<T>& x, const Raw8<T>& u, float (&v)[8])
 {
-    load8(x + c, (int)(N - c), v);
-    if constexpr (ACT == GEMM_OPS_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = v[i] < 0.0f ? 0.0f : v[i];
-    } else if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) {
-        float u[8];
-        load8(x + N + c, (int)(N - c), u);
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = silu(v[i]) * u[i];
+    for (int i = 0; i < 8; i++) {
+        v[i] = (float)x[i];
+        if constexpr (ACT == GEMM_OPS_ACT_RELU) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+        else if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) v[i] = silu(v[i]) * (float)u[i];
     }
 }
-// W wavefronts a row, P chunks of 8 columns a lane, R rows a workgroup; LOOP: two passes over a row of any length
-template <typename T, int ACT, int W, int P, int R, bool LOOP>
-__global__ __launch_bounds__(64 * W * R) void quantize_i8_kernel(const QuantArgs a)
+// L threads a row, P chunks of 8 columns a thread, R rows a workgroup
+template <typename T, int ACT, int L, int P, int R>
+__global__ __launch_bounds__(L * R) void quantize_i8_kernel(const QuantArgs a)
 {
-    __shared__ uint32_t most[W * R];
-    const int lane = threadIdx.x % (64 * W);
-    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / (64 * W);
-    const bool live = row < a.M;
-    const T* const x = (const T*)a.X + row * a.ldx;
+    __shared__ uint32_t most[L * R / 64];
+    const int lane = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    const T* const x = (const T*)a.X + min(row, (int64_t)a.M - 1) * a.ldx;
+    Raw8<T> xr[P], ur[P];
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        xr[p] = load8_of(x, 8 * (lane + L * p), a.N);
+        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = load8_of(x + a.N, 8 * (lane + L * p), a.N);
+    }
+    float v[P][8];
     uint32_t big = 0;
-    if constexpr (!LOOP) {
-        float v[P][8];
 #pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (live && c < a.N) activated8<T, ACT>(x, a.N, c, v[p]);
-            else {
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p);
+        xr[p] = settled<T>(xr[p], c, a.N);
+        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = settled<T>(ur[p], c, a.N);
+        activated8<T, ACT>(xr[p], ur[p], v[p]);
 #pragma unroll
-                for (int i = 0; i < 8; i++) v[p][i] = 0.0f;
-            }
-        }
+        for (int i = 0; i < 8; i++) big = max(big, magnitude(v[p][i]));
+    }
+    const RowScale s = row_scale(max_row<L>(big, most));
+    if (row >= a.M) return;
+    if (lane == 0) a.scale[row] = s.scale;
 #pragma unroll
-        for (int p = 0; p < P; p++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) big = max(big, magnitude(v[p][i]));
-        const RowScale s = row_scale(max_row<W>(big, most));
-        if (!live) return;
-        if (lane == 0) a.scale[row] = s.scale;
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int c = 8 * (lane + 64 * W * p);
-            if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
-        }
-    } else {
-        static_assert(R == 1, "a workgroup has one row, which is there");
-        float v[8];
-        for (int64_t c = 8 * (int64_t)lane; c < a.N; c += 512 * W) {
-            activated8<T, ACT>(x, a.N, c, v);
-#pragma unroll
-            for (int i = 0; i < 8; i++) big = max(big, magnitude(v[i]));
-        }
-        const RowScale s = row_scale(max_row<W>(big, most));
-        if (lane == 0) a.scale[row] = s.scale;
-        for (int64_t c = 8 * (int64_t)lane; c < a.N; c += 512 * W) {
-            activated8<T, ACT>(x, a.N, c, v);
-            store_bytes(a.Q + row * a.ldq + c, (int)(a.N - c), to_i8(v, s));
-        }
+    for (int p = 0; p < P; p++) {
+        const int c = 8 * (lane + L * p);
+        if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
     }
 }
-template <typename T, int ACT, int W, int P, int R, bool LOOP = false>
+// rows of any length, a workgroup each, in two passes
+template <typename T, int ACT>
+__global__ __launch_bounds__(LONG) void quantize_i8_long_kernel(const QuantArgs a)
+{
+    __shared__ uint32_t most[LONG / 64];
+    const int64_t row = blockIdx.x;
+    const T* const x = (const T*)a.X + row * a.ldx;
+    float v[8];
+    auto at = [&](int64_t c) {
+        const int left = (int)min((int64_t)8, a.N - c);
+        const Raw8<T> xr = load8_raw(x + c, left), ur = ACT == GEMM_OPS_ACT_SWIGLU ? load8_raw(x + a.N + c, left) : xr;
+        activated8<T, ACT>(xr, ur, v);
+    };
+    uint32_t big = 0;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.N; c += 8 * LONG) {
+        at(c);
+#pragma unroll
+        for (int i = 0; i < 8; i++) big = max(big, magnitude(v[i]));
+    }
+    const RowScale s = row_scale(max_row<LONG>(big, most));
+    if (threadIdx.x == 0) a.scale[row] = s.scale;
+    for (int64_t c = 8 * (int64_t)threadIdx.x; c < a.N; c += 8 * LONG) {
+        at(c);
+        store_bytes(a.Q + row * a.ldq + c, (int)(a.N - c), to_i8(v, s));
+    }
+}
+template <typename T, int ACT, int L, int P, int R>
 int launch_quant(const QuantArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((quantize_i8_kernel<T, ACT, W, P, R, LOOP>), dim3((unsigned)(((int64_t)a.M + R - 1) / R)), dim3(64 * W * R), 0, stream, a);
-    return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
+    hipLaunchKernelGGL((quantize_i8_kernel<T, ACT, L, P, R>), dim3((unsigned)(((int64_t)a.M + R - 1) / R)), dim3(L * R), 0, stream, a);
+    return launched();
 }
 template <typename T, int ACT>
 int quant_of_act(const QuantArgs& a, hipStream_t stream)
 {
-    if (a.M <= 2 * chip().cus && a.N > 2048 && a.N <= 8192) return launch_quant<T, ACT, 16, 1, 1>(a, stream);
-    if (a.N <= 512) return launch_quant<T, ACT, 1, 1, 4>(a, stream);
-    if (a.N <= 1024) return launch_quant<T, ACT, 1, 2, 4>(a, stream);
-    if (a.N <= 2048) return launch_quant<T, ACT, 1, 4, 4>(a, stream);
-    if (a.N <= 4096) return launch_quant<T, ACT, 4, 2, 1>(a, stream);
-    if (a.N <= 8192) return launch_quant<T, ACT, 4, 4, 1>(a, stream);
-    if (a.N <= 16384) return launch_quant<T, ACT, 8, 4, 1>(a, stream);
-    return launch_quant<T, ACT, 16, 1, 1, true>(a, stream);
+    if (a.M <= 2 * chip().cus && a.N > 2048 && a.N <= 8192) return launch_quant<T, ACT, 1024, 1, 1>(a, stream);
+    if (a.N <= 64) return launch_quant<T, ACT, 8, 1, 32>(a, stream);
+    if (a.N <= 128) return launch_quant<T, ACT, 16, 1, 16>(a, stream);
+    if (a.N <= 256) return launch_quant<T, ACT, 32, 1, 8>(a, stream);
+    if (a.N <= 512) return launch_quant<T, ACT, 64, 1, 4>(a, stream);
+    if (a.N <= 1024) return launch_quant<T, ACT, 64, 2, 4>(a, stream);
+    if (a.N <= 2048) return launch_quant<T, ACT, 64, 4, 4>(a, stream);
+    if (a.N <= 4096) return launch_quant<T, ACT, 256, 2, 1>(a, stream);
+    if (a.N <= 8192) return launch_quant<T, ACT, 256, 4, 1>(a, stream);
+    if (a.N <= 16384) return launch_quant<T, ACT, 512, 4, 1>(a, stream);
+    hipLaunchKernelGGL((quantize_i8_long_kernel<T, ACT>), dim3((unsigned)a.M), dim3(LONG), 0, stream, a);
+    return launched();
 }
 template <typename T>
 int quant_of_type(const QuantArgs& a, hipStream_t stream)

@@ -5,7 +5,7 @@
 // bytes of a row) and multiplies them.  No LDS, no barrier before the end; what keeps the memory busy is that 16 to 32 wavefronts
 // a compute unit do so.  (A ring of 2 to 6 steps in registers ahead of the multiplication, with fewer wavefronts: (16,8192,8192) e4m3
 // 13.9 to 19.9 us against 13.7, 64 rows of 16 experts (4096,2048) 29.5 to 57 against 26.3.)  e4m3 values are widened to f16: the matrix
-// rate does not matter here.  Measured: (16,8192,8192) 16.2 us from memory, 4.2 TB/s, 13.5 where B (67 MB) is still in the 256 MB memory-side cache; 64 rows of 16
+// rate does not matter here.  8-bit integers are multiplied as they are.  Measured: (16,8192,8192) 16.2 us from memory, 4.2 TB/s, 13.5 where B (67 MB) is still in the 256 MB memory-side cache; 64 rows of 16
 // experts (4096,2048) 26 to 29 us, 4.6 to 5.1 TB/s.  More rows a workgroup
 // than 32 make A's reads, once for each 32 columns, the bound: 32 rows each of 16 experts 75 us with 64, 56 with 32.
 #include "ops_tile.h"
@@ -16,8 +16,8 @@ using namespace ops_tile;
 
 constexpr int WAVES = 8;      // (16 for the fewest workgroups: no faster)
 
-// OCC: wavefronts a SIMD that the registers leave room for
-template <int ELEM, int FM, int NB, int OCC, typename CT>
+// OCC: wavefronts a SIMD that the registers leave room for; U: k steps of a wavefront whose loads are asked for together
+template <int ELEM, int FM, int NB, int OCC, int U, typename CT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGemm g)
 {
     constexpr bool I8 = ELEM == ELEM_I8;                                     // integer sums, scaled at the end
@@ -101,7 +101,18 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
     };
 
     Step x;
-    for (int k = wave; k < k_full; k += WAVES) { load(x, k); multiply(x); }
+    int k = wave;
+    if constexpr (U > 1) {                                                   // U k steps' loads ahead of their products
+        for (; k + (U - 1) * WAVES < k_full; k += U * WAVES) {
+            Step s[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) load(s[u], k + u * WAVES);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < U; u++) multiply(s[u]);
+        }
+    }
+    for (; k < k_full; k += WAVES) { load(x, k); multiply(x); }
     if (k_full < KT && k_full % WAVES == wave) { load_tail(x, k_full); multiply(x); }
 
     // ---- the wavefronts' sums, in their order -----------------------------------------------------------------------------
@@ -137,24 +148,32 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
     }
 }
 
-template <int ELEM, int FM, int NB, int OCC>
+template <int ELEM, int FM, int NB, int OCC, int U>
 int launch_skinny(const OpsGemm& g)
 {
     static_assert(FM * NB <= WAVES, "a wavefront adds one block");
     const int64_t grid = tile_grid(g, 16 * FM, 16 * NB);
     if (grid < 0 || !fits_a_launch(grid, 64 * WAVES)) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else                           hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else                           hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
-template <int ELEM>
-int launch_of(const OpsGemm& g, int fm, int nb)
+int launch_e4m3(const OpsGemm& g, int fm, int nb)
 {
-    if (fm == 1) return nb == 1 ? launch_skinny<ELEM, 1, 1, 8>(g) : launch_skinny<ELEM, 1, 2, 4>(g);
-    return nb == 1 ? launch_skinny<ELEM, 2, 1, 6>(g) : nb == 2 ? launch_skinny<ELEM, 2, 2, 4>(g) : launch_skinny<ELEM, 2, 4, 3>(g);
+    if (fm == 1) return nb == 1 ? launch_skinny<ELEM_E4M3, 1, 1, 8, 1>(g) : launch_skinny<ELEM_E4M3, 1, 2, 4, 1>(g);
+    return nb == 1 ? launch_skinny<ELEM_E4M3, 2, 1, 6, 1>(g) : nb == 2 ? launch_skinny<ELEM_E4M3, 2, 2, 4, 1>(g) : launch_skinny<ELEM_E4M3, 2, 4, 3, 1>(g);
+}
+int launch_i8(const OpsGemm& g, int fm, int nb)
+{
+    // From 4096 k on a wavefront has four k steps, whose loads go ahead together, with registers for them: 16 rows of (8192,8192) 14.1 us against 15.4, of (16384,8192) 27.8 against
+    // 32.9, one row of (8192,8192) 12.3 against 13.4.  With fewer k, or for 32 rows, no faster or slower: 64 rows of 16 experts (4096,2048) 32.9 against 27.0.
+    const bool ahead = g.K >= 4 * WAVES * STEP;
+    if (fm == 1 && nb == 4) return ahead ? launch_skinny<ELEM_I8, 1, 4, 2, 4>(g) : launch_skinny<ELEM_I8, 1, 4, 4, 1>(g);
+    if (fm == 1) return nb == 1 ? launch_skinny<ELEM_I8, 1, 1, 8, 1>(g) : ahead ? launch_skinny<ELEM_I8, 1, 2, 2, 4>(g) : launch_skinny<ELEM_I8, 1, 2, 4, 1>(g);
+    return nb == 1 ? launch_skinny<ELEM_I8, 2, 1, 6, 1>(g) : nb == 2 ? launch_skinny<ELEM_I8, 2, 2, 4, 1>(g) : launch_skinny<ELEM_I8, 2, 4, 3, 1>(g);
 }
 
 }  // namespace
 
-int ops_launch_skinny(const OpsGemm& g, int fm, int nb) { return g.elem == ELEM_I8 ? launch_of<ELEM_I8>(g, fm, nb) : launch_of<ELEM_E4M3>(g, fm, nb); }
+int ops_launch_skinny(const OpsGemm& g, int fm, int nb) { return g.elem == ELEM_I8 ? launch_i8(g, fm, nb) : launch_e4m3(g, fm, nb); }
