@@ -21,6 +21,18 @@ __device__ __forceinline__ float sum_lanes(float x)
     for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
     return x;
 }
+// the sum of W values, lane i of a wavefront having the i % W-th: of 16 neighbouring lanes, which have each 16 / W times
+template <int W>
+__device__ __forceinline__ float sum_waves(float x)
+{
+    static_assert(W <= 16 && (W & (W - 1)) == 0);
+    auto add = [&](uint32_t y) { x += __builtin_bit_cast(float, y); };
+    if constexpr (W >= 16) add(dpp_u32<0x128>(__builtin_bit_cast(uint32_t, x)));
+    if constexpr (W >= 8) add(dpp_u32<0x124>(__builtin_bit_cast(uint32_t, x)));
+    if constexpr (W >= 4) add(dpp_u32<0x122>(__builtin_bit_cast(uint32_t, x)));
+    if constexpr (W >= 2) add(dpp_u32<0x121>(__builtin_bit_cast(uint32_t, x)));
+    return x;
+}
 // Mean and sum of squares about it, of which each wavefront has those of its own elements: the row's mean is that of the wavefronts' by their elements, and
 // squares about it are those about the wavefront's mean + n (its mean - the row's)^2.  So one exchange serves both.
 struct Moments { float mean, squares; };
@@ -30,19 +42,13 @@ __device__ __forceinline__ Moments row_moments(float own_mean, float squares, in
 {
     if constexpr (L <= 64) return {own_mean, squares};
     constexpr int W = L > 64 ? L / 64 : 1;
-    const int wave = threadIdx.x >> 6, first = wave / W * W;
+    const int wave = threadIdx.x >> 6, w = threadIdx.x & (W - 1);
     if ((threadIdx.x & 63) == 0) { lds[2 * wave] = own_mean; lds[2 * wave + 1] = squares; }
     __syncthreads();
-    float total = 0.0f, out = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; w++) total += (float)n_of(w) * lds[2 * (first + w)];
-    const float mean = total / (float)N;
-#pragma unroll
-    for (int w = 0; w < W; w++) {
-        const float d = lds[2 * (first + w)] - mean, n = (float)n_of(w);
-        out += lds[2 * (first + w) + 1] + (n > 0.0f ? n * d * d : 0.0f);
-    }
-    return {mean, out};
+    const float* const pair = &lds[2 * (wave / W * W + w)];
+    const float at = pair[0], n = (float)n_of(w);
+    const float mean = sum_waves<W>(n * at) / (float)N, d = at - mean;
+    return {mean, sum_waves<W>(pair[1] + (n > 0.0f ? n * d * d : 0.0f))};
 }
 
 // the largest of a row's magnitudes over its L threads; lds: a word for each wavefront of the workgroup, used for nothing else
@@ -60,8 +66,7 @@ __device__ __forceinline__ uint32_t max_row(uint32_t m, uint32_t* lds)
         const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
         if ((threadIdx.x & 63) == 0) lds[wave] = m;
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < L / 64; w++) m = max(m, lds[first + w]);
+        m = max16(lds[first + (threadIdx.x & (L / 64 - 1))]);
     }
     return m;
 }
@@ -99,7 +104,7 @@ __device__ __forceinline__ uintx2 to_i8(const float (&y)[8], const RowScale& s)
 
 // ---- the norm --------------------------------------------------------------------------------------------------------------------
 // L threads a row, each with P chunks of 8 columns in registers; R rows a workgroup.
-template <typename T, int L, int P, int R>
+template <typename T, bool WHOLE, int L, int P, int R>
 __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a)
 {
     __shared__ float lds[L * R / 64 * 3];
@@ -113,24 +118,24 @@ __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p);
-        raw[p] = load8_of(x, c, a.N);
-        if (r) res[p] = load8_of(r, c, a.N);
-        gamma[p] = load8_of((const T*)a.gamma, c, a.N);
-        if (a.beta) beta[p] = load8_of((const T*)a.beta, c, a.N);
+        raw[p] = load8_of<WHOLE>(x, c, a.N);
+        if (r) res[p] = load8_of<WHOLE>(r, c, a.N);
+        gamma[p] = load8_of<WHOLE>((const T*)a.gamma, c, a.N);
+        if (a.beta) beta[p] = load8_of<WHOLE>((const T*)a.beta, c, a.N);
     }
     float v[P][8], sum = 0.0f, squares = 0.0f;
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p);
-        raw[p] = settled<T>(raw[p], c, a.N);
-        if (r) res[p] = settled<T>(res[p], c, a.N);
+        raw[p] = settled<T, WHOLE>(raw[p], c, a.N);
+        if (r) res[p] = settled<T, WHOLE>(res[p], c, a.N);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             v[p][i] = (float)raw[p][i];
             if (r) v[p][i] = rounded<T>(v[p][i] + (float)res[p][i]);         // h as it is stored is what is normed
             sum += v[p][i];
         }
-        if (a.H && live && c < a.N) store8((T*)a.H + row * a.ldh + c, a.N - c, v[p]);
+        if (a.H && live && c < a.N) store8_of<WHOLE>((T*)a.H + row * a.ldh + c, a.N - c, v[p]);
     }
     auto n_of = [&](int w) {                              // elements of the row's w-th wavefront
         int n = 0;
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a
     for (int p = 0; p < P; p++) {
         const int left = a.N - 8 * (lane + L * p);
 #pragma unroll
-        for (int i = 0; i < 8; i++) { const float d = i < left ? v[p][i] - centre : 0.0f; squares += d * d; }
+        for (int i = 0; i < 8; i++) { const float d = (WHOLE ? left > 0 : i < left) ? v[p][i] - centre : 0.0f; squares += d * d; }
     }
     const Moments m = row_moments<L>(centre, sum_lanes<L>(squares), a.N, lds, n_of);
     const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
@@ -158,16 +163,16 @@ __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p), left = a.N - c;
-        gamma[p] = settled<T>(gamma[p], c, a.N);
-        if (a.beta) beta[p] = settled<T>(beta[p], c, a.N);
+        gamma[p] = settled<T, WHOLE>(gamma[p], c, a.N);
+        if (a.beta) beta[p] = settled<T, WHOLE>(beta[p], c, a.N);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             float y = (v[p][i] - m.mean) * rstd * (float)gamma[p][i];
             if (a.beta) y += (float)beta[p][i];
-            v[p][i] = i < left ? y : 0.0f;
+            v[p][i] = (WHOLE ? left > 0 : i < left) ? y : 0.0f;
             big = max(big, magnitude(v[p][i]));
         }
-        if (a.Y && live && left > 0) store8((T*)a.Y + row * a.ldy + c, left, v[p]);
+        if (a.Y && live && left > 0) store8_of<WHOLE>((T*)a.Y + row * a.ldy + c, left, v[p]);
     }
     if (!a.Q) return;
     const RowScale s = row_scale(max_row<L>(big, (uint32_t*)&lds[L * R / 64 * 2]));
@@ -176,7 +181,7 @@ __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p);
-        if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
+        if (c < a.N) store_bytes<WHOLE>(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
     }
 }
 
@@ -253,7 +258,9 @@ __global__ __launch_bounds__(LONG) void layer_norm_long_kernel(const LayerNormAr
 template <typename T, int L, int P, int R>
 int launch_norm(const LayerNormArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((layer_norm_kernel<T, L, P, R>), dim3((unsigned)(((int64_t)a.M + R - 1) / R)), dim3(L * R), 0, stream, a);
+    const dim3 grid((unsigned)(((int64_t)a.M + R - 1) / R));
+    if (a.N % 8 == 0) hipLaunchKernelGGL((layer_norm_kernel<T, true, L, P, R>), grid, dim3(L * R), 0, stream, a);
+    else hipLaunchKernelGGL((layer_norm_kernel<T, false, L, P, R>), grid, dim3(L * R), 0, stream, a);
     return launched();
 }
 template <typename T>
@@ -275,7 +282,7 @@ int norm_of_type(const LayerNormArgs& a, hipStream_t stream)
 
 // ---- its gradients -----------------------------------------------------------------------------------------------------------------
 // A row of dY, H and dH, chunks of 8 columns of one of its L threads; rows behind the last one are that one, with nothing in dy
-template <typename T, int L, int P>
+template <typename T, bool WHOLE, int L, int P>
 struct GradRow {
     Raw8<T> dy[P], h[P], dh[P];
     float mean, rstd;
@@ -287,9 +294,9 @@ struct GradRow {
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int c = 8 * (lane + L * p);
-            dy[p] = load8_of((const T*)a.dY + row * a.lddy, c, a.N);
-            h[p] = load8_of((const T*)a.H + row * a.ldh, c, a.N);
-            if (a.dH) dh[p] = load8_of((const T*)a.dH + row * a.lddh, c, a.N);
+            dy[p] = load8_of<WHOLE>((const T*)a.dY + row * a.lddy, c, a.N);
+            h[p] = load8_of<WHOLE>((const T*)a.H + row * a.ldh, c, a.N);
+            if (a.dH) dh[p] = load8_of<WHOLE>((const T*)a.dH + row * a.lddh, c, a.N);
         }
     }
     __device__ __forceinline__ void settle(const LayerNormGradArgs& a, int lane, bool live)
@@ -297,9 +304,9 @@ struct GradRow {
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int c = 8 * (lane + L * p);
-            dy[p] = settled<T>(dy[p], live ? c : (int64_t)a.N + 8, a.N);
-            h[p] = settled<T>(h[p], c, a.N);
-            if (a.dH) dh[p] = settled<T>(dh[p], c, a.N);
+            dy[p] = settled<T, WHOLE>(dy[p], live ? c : (int64_t)a.N + 8, a.N);
+            h[p] = settled<T, WHOLE>(h[p], c, a.N);
+            if (a.dH) dh[p] = settled<T, WHOLE>(dh[p], c, a.N);
         }
     }
     // from the sums of g and g xhat
@@ -316,7 +323,7 @@ struct GradRow {
                 o[i] = rstd * ((float)dy[p][i] * (float)gamma[p][i] - m1 - ((float)h[p][i] - mean) * rstd * m2);
                 if (a.dH) o[i] += (float)dh[p][i];
             }
-            store8((T*)a.dX + row * a.lddx + c, a.N - c, o);
+            store8_of<WHOLE>((T*)a.dX + row * a.lddx + c, a.N - c, o);
         }
     }
 };
@@ -335,15 +342,15 @@ __device__ __forceinline__ void sum_pair(float& x, float& y, float* set)
         const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
         if ((threadIdx.x & 63) == 0) { set[2 * wave] = x; set[2 * wave + 1] = y; }
         __syncthreads();
-        x = y = 0.0f;
-#pragma unroll
-        for (int i = 0; i < L / 64; i++) { x += set[2 * (first + i)]; y += set[2 * (first + i) + 1]; }
+        const float* const pair = &set[2 * (first + (threadIdx.x & (L / 64 - 1)))];
+        x = sum_waves<L / 64>(pair[0]);
+        y = sum_waves<L / 64>(pair[1]);
     }
 }
 
 // dX row by row; the columns' sums of dy xhat and dy stay in registers over all rows of a workgroup, which writes them as one row of the
 // workspace; a second kernel adds those.  Every sum has a fixed order.  L threads a row, R rows a workgroup, P chunks of 8 columns a thread.
-template <typename T, int L, int P, int R>
+template <typename T, bool WHOLE, int L, int P, int R>
 __global__ __launch_bounds__(L * R) void layer_norm_grad_kernel(const LayerNormGradArgs a)
 {
     extern __shared__ float dyn[];                        // 4 floats for each wavefront, then R * 8 L of sums
@@ -352,20 +359,20 @@ __global__ __launch_bounds__(L * R) void layer_norm_grad_kernel(const LayerNormG
     float dg[P][8] = {}, db[P][8] = {};
     Raw8<T> gamma[P];
 #pragma unroll
-    for (int p = 0; p < P; p++) gamma[p] = settled<T>(load8_of((const T*)a.gamma, 8 * (lane + L * p), a.N), 8 * (lane + L * p), a.N);
+    for (int p = 0; p < P; p++) gamma[p] = settled<T, WHOLE>(load8_of<WHOLE>((const T*)a.gamma, 8 * (lane + L * p), a.N), 8 * (lane + L * p), a.N);
     // the values as they were loaded, to be widened again: kept widened over the sums they would take twice the registers
     auto again = [](Raw8<T>& x) { uintx4 r = __builtin_bit_cast(uintx4, x); asm volatile("" : "+v"(r)); x = __builtin_bit_cast(Raw8<T>, r); };
 
     const int64_t step = (int64_t)gridDim.x * R;
     int slot = 0;
     constexpr bool AHEAD = L * R <= 512;                  // the next row's loads ahead: registers for it where a workgroup has 512 threads
-    GradRow<T, L, P> next;
+    GradRow<T, WHOLE, L, P> next;
     if constexpr (AHEAD) next.load(a, lane, (int64_t)blockIdx.x * R + sub);
     for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.M; row0 += step) {      // the same number of trips for the whole workgroup
         const int64_t row = row0 + sub;
         const bool live = row < a.M;
         if constexpr (!AHEAD) next.load(a, lane, row);
-        GradRow<T, L, P> x = next;
+        GradRow<T, WHOLE, L, P> x = next;
         x.settle(a, lane, live);
         float s1 = 0.0f, s2 = 0.0f;                       // of g and g xhat; dy is zero behind the row's end
 #pragma unroll
@@ -411,7 +418,7 @@ __global__ __launch_bounds__(L * R) void layer_norm_grad_kernel(const LayerNormG
 
 // Few rows: one launch.  The columns' sums need nothing of the rows' sums, so some workgroups form dX and others read the rows once more for 64 columns of dgamma and dbeta: 8
 // threads of 8 columns, 64 rows at a time.
-template <typename T, int L, int P>
+template <typename T, bool WHOLE, int L, int P>
 __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNormGradArgs a, int row_groups)
 {
     __shared__ float lds[2][64][65];
@@ -419,16 +426,16 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
         const int lane = threadIdx.x % L;
         const int64_t row = (int64_t)blockIdx.x * (512 / L) + threadIdx.x / L;
         const bool live = row < a.M;
-        GradRow<T, L, P> x;
+        GradRow<T, WHOLE, L, P> x;
         Raw8<T> gamma[P];
         x.load(a, lane, row);
 #pragma unroll
-        for (int p = 0; p < P; p++) gamma[p] = load8_of((const T*)a.gamma, 8 * (lane + L * p), a.N);
+        for (int p = 0; p < P; p++) gamma[p] = load8_of<WHOLE>((const T*)a.gamma, 8 * (lane + L * p), a.N);
         x.settle(a, lane, live);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int p = 0; p < P; p++) {
-            gamma[p] = settled<T>(gamma[p], 8 * (lane + L * p), a.N);
+            gamma[p] = settled<T, WHOLE>(gamma[p], 8 * (lane + L * p), a.N);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float g = (float)x.dy[p][i] * (float)gamma[p][i];
@@ -444,8 +451,8 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
     const int64_t c = ((int64_t)blockIdx.x - row_groups) * 64 + 8 * lane;
     float dg[8] = {}, db[8] = {};
     auto add = [&](Raw8<T> dy, Raw8<T> h, float mean, float rstd, bool live) {
-        dy = settled<T>(dy, live ? c : (int64_t)a.N + 8, a.N);
-        h = settled<T>(h, c, a.N);
+        dy = settled<T, WHOLE>(dy, live ? c : (int64_t)a.N + 8, a.N);
+        h = settled<T, WHOLE>(h, c, a.N);
 #pragma unroll
         for (int i = 0; i < 8; i++) { dg[i] += (float)dy[i] * (((float)h[i] - mean) * rstd); db[i] += (float)dy[i]; }
     };
@@ -456,8 +463,8 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
 #pragma unroll
         for (int u = 0; u < AT_ONCE; u++) {
             const int64_t row = min(row0 + 64 * u, (int64_t)a.M - 1);
-            dy[u] = load8_of((const T*)a.dY + row * a.lddy, c, a.N);
-            h[u] = load8_of((const T*)a.H + row * a.ldh, c, a.N);
+            dy[u] = load8_of<WHOLE>((const T*)a.dY + row * a.lddy, c, a.N);
+            h[u] = load8_of<WHOLE>((const T*)a.H + row * a.ldh, c, a.N);
             mean[u] = a.mean[row];
             rstd[u] = a.rstd[row];
         }
@@ -559,14 +566,18 @@ inline bool grad_few(const LayerNormGradArgs& a)
 template <typename T, int L, int P, int R>
 int launch_norm_grad(const LayerNormGradArgs& a, int parts, hipStream_t stream)
 {
-    hipLaunchKernelGGL((layer_norm_grad_kernel<T, L, P, R>), dim3((unsigned)parts), dim3(L * R), (L * R / 16 + R * 8 * L) * sizeof(float), stream, a);
+    constexpr size_t lds = (L * R / 16 + R * 8 * L) * sizeof(float);
+    if (a.N % 8 == 0) hipLaunchKernelGGL((layer_norm_grad_kernel<T, true, L, P, R>), dim3((unsigned)parts), dim3(L * R), lds, stream, a);
+    else hipLaunchKernelGGL((layer_norm_grad_kernel<T, false, L, P, R>), dim3((unsigned)parts), dim3(L * R), lds, stream, a);
     return launched();
 }
 template <typename T, int L, int P>
 int launch_norm_grad_few(const LayerNormGradArgs& a, hipStream_t stream)
 {
     const int row_groups = (a.M + 512 / L - 1) / (512 / L), columns = a.dgamma || a.dbeta ? (a.N + 63) / 64 : 0;
-    hipLaunchKernelGGL((layer_norm_grad_few_kernel<T, L, P>), dim3((unsigned)(row_groups + columns)), dim3(512), 0, stream, a, row_groups);
+    const dim3 grid((unsigned)(row_groups + columns));
+    if (a.N % 8 == 0) hipLaunchKernelGGL((layer_norm_grad_few_kernel<T, true, L, P>), grid, dim3(512), 0, stream, a, row_groups);
+    else hipLaunchKernelGGL((layer_norm_grad_few_kernel<T, false, L, P>), grid, dim3(512), 0, stream, a, row_groups);
     return launched();
 }
 template <typename T>
@@ -620,7 +631,7 @@ __device__ __forceinline__ void activated8(const Raw8<T>& x, const Raw8<T>& u, f
     }
 }
 // L threads a row, P chunks of 8 columns a thread, R rows a workgroup
-template <typename T, int ACT, int L, int P, int R>
+template <typename T, int ACT, bool WHOLE, int L, int P, int R>
 __global__ __launch_bounds__(L * R) void quantize_i8_kernel(const QuantArgs a)
 {
     __shared__ uint32_t most[L * R / 64];
@@ -630,16 +641,16 @@ __global__ __launch_bounds__(L * R) void quantize_i8_kernel(const QuantArgs a)
     Raw8<T> xr[P], ur[P];
 #pragma unroll
     for (int p = 0; p < P; p++) {
-        xr[p] = load8_of(x, 8 * (lane + L * p), a.N);
-        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = load8_of(x + a.N, 8 * (lane + L * p), a.N);
+        xr[p] = load8_of<WHOLE>(x, 8 * (lane + L * p), a.N);
+        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = load8_of<WHOLE>(x + a.N, 8 * (lane + L * p), a.N);
     }
     float v[P][8];
     uint32_t big = 0;
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p);
-        xr[p] = settled<T>(xr[p], c, a.N);
-        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = settled<T>(ur[p], c, a.N);
+        xr[p] = settled<T, WHOLE>(xr[p], c, a.N);
+        if constexpr (ACT == GEMM_OPS_ACT_SWIGLU) ur[p] = settled<T, WHOLE>(ur[p], c, a.N);
         activated8<T, ACT>(xr[p], ur[p], v[p]);
 #pragma unroll
         for (int i = 0; i < 8; i++) big = max(big, magnitude(v[p][i]));
@@ -650,7 +661,7 @@ __global__ __launch_bounds__(L * R) void quantize_i8_kernel(const QuantArgs a)
 #pragma unroll
     for (int p = 0; p < P; p++) {
         const int c = 8 * (lane + L * p);
-        if (c < a.N) store_bytes(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
+        if (c < a.N) store_bytes<WHOLE>(a.Q + row * a.ldq + c, a.N - c, to_i8(v[p], s));
     }
 }
 // rows of any length, a workgroup each, in two passes
@@ -682,7 +693,9 @@ __global__ __launch_bounds__(LONG) void quantize_i8_long_kernel(const QuantArgs 
 template <typename T, int ACT, int L, int P, int R>
 int launch_quant(const QuantArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((quantize_i8_kernel<T, ACT, L, P, R>), dim3((unsigned)(((int64_t)a.M + R - 1) / R)), dim3(L * R), 0, stream, a);
+    const dim3 grid((unsigned)(((int64_t)a.M + R - 1) / R));
+    if (a.N % 8 == 0) hipLaunchKernelGGL((quantize_i8_kernel<T, ACT, true, L, P, R>), grid, dim3(L * R), 0, stream, a);
+    else hipLaunchKernelGGL((quantize_i8_kernel<T, ACT, false, L, P, R>), grid, dim3(L * R), 0, stream, a);
     return launched();
 }
 template <typename T, int ACT>

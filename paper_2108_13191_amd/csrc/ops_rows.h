@@ -32,10 +32,13 @@ __device__ __forceinline__ void store8(T* p, int left, const float (&v)[8])
         for (int i = 0; i < 8; i++) if (i < left) p[i] = (T)v[i];
     }
 }
+// (left above 0, and 8 or more where rows are WHOLE)
+template <bool WHOLE, typename T> __device__ __forceinline__ void store8_of(T* p, int left, const float (&v)[8]) { store8(p, WHOLE ? 8 : left, v); }
 typedef uintx2 uintx2_any __attribute__((aligned(1)));
+template <bool WHOLE = false>
 __device__ __forceinline__ void store_bytes(uint8_t* p, int left, uintx2 q)
 {
-    if (left >= 8) {
+    if (WHOLE || left >= 8) {
         *(uintx2_any*)p = q;
     } else {
 #pragma unroll
@@ -76,17 +79,18 @@ __device__ __forceinline__ Raw8<T> moved_down(Raw8<T> v, int n)
 // Elements c .. c + 7 of a row of N, zeros behind its end, in two steps: load8_of asks for them, and what would leave the row as its last 8 elements instead; settled
 // moves those to their place once they are used.  So no loaded value is touched, and no branch parted, before all of a row's loads have been asked for:
 // lanes behind the end that had a way of their own made their wavefront wait for each load by itself (gradients of (8191,4000) 81 us, of (8191,4096) 62).
-template <typename T>
+// WHOLE: rows are whole chunks of 8, so that one is there or not: a third of the code, whose fetch is most of a small call's time (norm of 16 rows of 8192 4.5 us with all of it)
+template <bool WHOLE, typename T>
 __device__ __forceinline__ Raw8<T> load8_of(const T* row, int64_t c, int64_t N)
 {
-    if (N < 8) return load8_raw(row, (int)N);
+    if (!WHOLE && N < 8) return load8_raw(row, (int)N);
     return *(const typename Vec8<T>::type*)(row + min(c, N - 8));
 }
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ Raw8<T> settled(Raw8<T> v, int64_t c, int64_t N)
 {
-    const int n = (int)min(c - (N < 8 ? 0 : min(c, N - 8)), (int64_t)8);
-    if (N & 7) v = moved_down<T>(v, n);
+    const int n = WHOLE ? (c < N ? 0 : 8) : (int)min(c - (N < 8 ? 0 : min(c, N - 8)), (int64_t)8);
+    if (!WHOLE && (N & 7)) v = moved_down<T>(v, n);
     if constexpr (sizeof(T) == 2) {
         const uint32_t keep = n >= 8 ? 0u : ~0u;
         uintx4 w = __builtin_bit_cast(uintx4, v);
