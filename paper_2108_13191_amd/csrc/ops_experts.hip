@@ -3,6 +3,7 @@
 // The order is a counting sort: how many choices of each expert lie before a choice's own, and how many of its own.  Nothing atomic
 // decides a place, so the order is always the same.  Rows move by token: a token's row is read once and stored to its places,
 // and on the way back a lane adds the elements of a token's rows in their order.  Both are bound by memory.
+#include <type_traits>
 #include "ops_rows.h"
 #include "../../include/gemm_layer.h"
 
@@ -40,11 +41,16 @@ struct RowPiece {
             for (int b = 0; b < bytes; b++) v[0][b >> 2] |= (uint32_t)(uint8_t)row[b] << (8 * (b & 3));
         }
     }
+    // PAST: past the caches
+    template <bool PAST = false>
     __device__ __forceinline__ void store(char* row, int64_t bytes) const
     {
 #pragma unroll
         for (int i = 0; i < ROW_CHUNKS; i++)
-            if (at[i] >= 0 && bytes >= 16) *(uintx4_any*)(row + at[i]) = v[i];
+            if (at[i] >= 0 && bytes >= 16) {
+                if constexpr (PAST) __builtin_nontemporal_store(v[i], (uintx4_any*)(row + at[i]));
+                else                *(uintx4_any*)(row + at[i]) = v[i];
+            }
         if (bytes < 16 && at[0] >= 0)
             for (int b = 0; b < bytes; b++) row[b] = (char)(v[0][b >> 2] >> (8 * (b & 3)));
     }
@@ -119,16 +125,16 @@ __global__ __launch_bounds__(256) void dispatch_few_kernel(const DispatchArgs a,
     }
 }
 
-// ---- many choices: a counting sort by one digit ------------------------------------------------------------------------------------
+// ---- more choices or experts: counting sorts by two digits ------------------------------------------------------------------------------------
 // `parts` workgroups of part_rows choices each count their digits; a second launch makes of each digit's counts the sums of those before;
-// a third one finds each choice's place.  Up to 2047 experts are one digit; more are sorted by the low 8 bits and then by the rest.
+// a third one finds each choice's place.  The choices are sorted by the experts' low 8 bits and then by the rest.
 struct SortPass {
     DispatchArgs a;
     const int32_t* seq;                                    // the choices in the order that this pass goes by; NULL: as they are
     int shift, bins, part_rows, parts;
     int32_t *counts, *totals;                              // [digit][part], [digit]
     int32_t* out;                                          // the choices as this pass orders them; NULL: the places and sources are written
-    int32_t* keys;                                         // the experts in order, of the last of two passes; NULL: there is one pass, which writes offsets
+    int32_t* keys;                                         // the experts in order, of the last pass
 };
 __device__ __forceinline__ int digit_of(const SortPass& s, int key) { return s.shift < 0 ? key & 255 : key >> s.shift; }
 
@@ -143,14 +149,15 @@ __global__ __launch_bounds__(256) void sort_count_kernel(const SortPass s)
     for (int b = threadIdx.x; b < s.bins; b += 256) s.counts[(int64_t)b * s.parts + blockIdx.x] = hist[b];
 }
 
-__device__ __forceinline__ int scan64(int x)               // sums of all lanes up to and with this one
+// sums of all lanes up to and with this one: within rows of 16 lanes, then the last lane of a row to the next, then of the first two rows to the others
+__device__ __forceinline__ int scan64(int x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(x, d);
-        if (lane >= d) x += v;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
 
@@ -163,7 +170,7 @@ __global__ __launch_bounds__(256) void sort_scan_kernel(const SortPass s)
     for (int p = 0; p < s.parts; p += 64) {
         const int v = p + lane < s.parts ? c[p + lane] : 0, incl = scan64(v);
         if (p + lane < s.parts) c[p + lane] = before + incl - v;
-        before += __shfl(incl, 63);
+        before += __builtin_amdgcn_readlane(incl, 63);
     }
     if (lane == 0) s.totals[b] = before;
 }
@@ -181,21 +188,14 @@ __global__ __launch_bounds__(256) void sort_place_kernel(const SortPass s)
     const int64_t end = min(n, first + s.part_rows / 4);
     for (int64_t i = first + lane; i < end; i += 64) atomicAdd(&own[digit_of(s, key_of(s.a, s.seq ? s.seq[i] : i))], 1);
     __syncthreads();
-    // where each digit begins: sums over the digits before, 8 of them a thread
-    int sum = 0;
-    for (int i = 0; i < 8; i++) { const int b = threadIdx.x * 8 + i; if (b < s.bins) sum += s.totals[b]; }
-    const int incl = scan64(sum);
+    // where each digit begins: sums over the digits before, a thread each (there are 256 at most)
+    const int b = threadIdx.x, sum = b < s.bins ? s.totals[b] : 0, incl = scan64(sum);
     if (lane == 63) wave_sums[wave] = incl;
     __syncthreads();
-    int start = incl - sum;
-    for (int w = 0; w < wave; w++) start += wave_sums[w];
-    for (int i = 0; i < 8; i++) {
-        const int b = threadIdx.x * 8 + i;
-        if (b >= s.bins) break;
-        if (blockIdx.x == 0 && !s.out && !s.keys) s.a.offsets[b] = start;
-        int at = start + s.counts[(int64_t)b * s.parts + blockIdx.x];
+    if (b < s.bins) {
+        int at = incl - sum + s.counts[(int64_t)b * s.parts + blockIdx.x];
+        for (int w = 0; w < wave; w++) at += wave_sums[w];
         for (int w = 0; w < 4; w++) { const int c = base[w * s.bins + b]; base[w * s.bins + b] = at; at += c; }
-        start += s.totals[b];
     }
     __syncthreads();
     // 64 choices at a time: lanes of one digit find each other, the first of them moves the digit's place on
@@ -220,7 +220,90 @@ __global__ __launch_bounds__(256) void sort_place_kernel(const SortPass s)
         const bool valid = key < s.a.E;
         s.a.place[choice] = valid ? at : -1;
         if (s.a.source) s.a.source[at] = valid ? (int32_t)(choice / s.a.top_k) : -1;
-        if (s.keys) s.keys[at] = key;
+        s.keys[at] = key;
+    }
+}
+
+// ---- up to 2047 experts and 2^19 choices: places and rows in one launch, behind two short ones -----------------------------------------
+// The tokens go in `parts` parts, of 64 choices each where there are no more than a thousand of those.  One launch counts the experts of each part, a second one adds the counts of
+// the parts in front (sort_scan_kernel).  In the third each wavefront finds its token's places by itself, from the counts and the choices of its part in front of its own, while
+// the piece of the token's row that it copies is on its way.
+struct Parts {
+    DispatchArgs a;
+    int tokens, parts;                                     // tokens of a part
+    int32_t *counts, *totals;                              // [expert][part], [expert]
+};
+__global__ __launch_bounds__(256) void part_count_kernel(const Parts s)
+{
+    extern __shared__ int hist[];
+    const int lane = threadIdx.x & 63, bins = s.a.E + 1;
+    const int64_t part = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    int* const own = hist + (threadIdx.x >> 6) * bins;
+    for (int b = lane; b < bins; b += 64) own[b] = 0;
+    __builtin_amdgcn_wave_barrier();                       // a wavefront's LDS accesses are in order
+    if (part >= s.parts) return;
+    const int64_t rows = (int64_t)s.tokens * s.a.top_k, first = part * rows, end = min(s.a.T * s.a.top_k, first + rows);
+    for (int64_t i = first + lane; i < end; i += 64) atomicAdd(&own[key_of(s.a, i)], 1);
+    __builtin_amdgcn_wave_barrier();
+    for (int b = lane; b < bins; b += 64) s.counts[(int64_t)b * s.parts + part] = own[b];
+}
+
+// Sums of the totals of the experts in front of each lane's.  (e: E + 1 where a lane has none)
+__device__ __forceinline__ int rows_before(const Parts& s, int e)
+{
+    const int lane = threadIdx.x & 63, bins = s.a.E + 1;
+    int run = 0, start = 0;
+    for (int b0 = 0; b0 < bins; b0 += 64) {
+        const int v = b0 + lane < bins ? s.totals[b0 + lane] : 0, incl = scan64(v);
+        const int at = __shfl(incl - v, e & 63);
+        if (e >> 6 == b0 >> 6) start = run + at;
+        run += __builtin_amdgcn_readlane(incl, 63);
+    }
+    return start;
+}
+template <bool PAST>
+__global__ __launch_bounds__(256) void part_move_kernel(const Parts s, int64_t pieces, int64_t items)
+{
+    const DispatchArgs& a = s.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= items) {                                   // offsets, 64 a wavefront
+        const int64_t e = (item - items) * 64 + lane;
+        if ((item - items) * 64 > a.E) return;
+        const int start = rows_before(s, (int)e);
+        if (e <= a.E) a.offsets[e] = start;
+        return;
+    }
+    const int64_t t = item / pieces, piece = item % pieces, bytes = (int64_t)a.N * a.size, part = t / s.tokens, n = a.T * a.top_k;
+    RowPiece row;
+    if (a.X) row.load((const char*)a.X + t * a.ldx * a.size, piece * PIECE, bytes);
+    for (int j0 = 0; j0 < a.top_k; j0 += 64) {             // 64 of the token's choices at a time, a lane each
+        const int64_t first = t * a.top_k + j0;
+        const int mine = min(a.top_k - j0, 64), own = lane < mine ? key_of(a, first + lane) : a.E + 1;
+        const int front = lane < mine ? s.counts[(int64_t)own * s.parts + part] : 0;
+        const int base = rows_before(s, own) + front;
+        int at = base;                                     // and the equal ones of the part in front of it
+        for (int64_t i0 = part * s.tokens * a.top_k; i0 < first + mine - 1; i0 += 64) {
+            const int64_t i = i0 + lane;
+            const int key = i < n ? key_of(a, i) : a.E + 1;
+            const int64_t in_front = first - i0;           // lanes in front of the token's choice 0 here
+            for (int j = 0; j < mine; j++) {
+                const uint64_t front_of_j = in_front + j >= 64 ? ~0ull : (1ull << (in_front + j)) - 1;
+                const int c = __popcll(__ballot(key == __builtin_amdgcn_readlane(own, j)) & front_of_j);
+                if (lane == j) at += c;
+            }
+        }
+        if (piece == 0 && lane < mine) {
+            a.place[first + lane] = own < a.E ? at : -1;
+            if (a.source) a.source[at] = own < a.E ? (int32_t)t : -1;
+        }
+        if (!a.X) continue;
+        for (int j = 0; j < mine; j++) {
+            if (__builtin_amdgcn_readlane(own, j) >= a.E) continue;
+            const int64_t place = __builtin_amdgcn_readlane(at, j);
+            row.store<PAST>((char*)a.rows + place * a.ld_rows * a.size, bytes);
+            if (piece == 0) move_scales(a, t, place);
+        }
     }
 }
 
@@ -245,6 +328,8 @@ __global__ __launch_bounds__(256) void zero_offsets_kernel(int32_t* offsets, int
 
 constexpr int FEW = 1024, ONE_DIGIT = 2047;                // choices of one launch; experts of one pass
 constexpr int MOST_PARTS = 256;
+constexpr int64_t SOME = 1 << 19;                          // choices that are placed by part
+int64_t most_parts(int64_t E) { return E < 1024 ? 1024 : 512; }      // at most 4 MB of counts
 
 int parts_of(int64_t n, int& part_rows)
 {
@@ -266,110 +351,199 @@ int sort_pass(SortPass s, hipStream_t stream)
 }
 
 // ---- and back ------------------------------------------------------------------------------------------------------------------------
-// 8 elements a lane, a wavefront for 512 columns of a token.  Products are rounded before they are added, in the order of the choices.
-template <typename T, typename OT>
+// L threads for 8 L columns of a token, 8 each.  Rows of up to four choices are asked for together; products are rounded before they are added, in the
+// order of the choices.
+template <typename T, typename OT, bool WHOLE, int L>
 __global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a, int64_t pieces, int64_t items)
 {
 #pragma clang fp contract(off)
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t item = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    if constexpr (L == 64) item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= items) return;
-    const int64_t t = item / pieces, c = item % pieces * 512 + 8 * (threadIdx.x & 63);
+    const int64_t t = item / pieces, c = (item % pieces * L + threadIdx.x % L) * 8;
     if (c >= a.N) return;
-    const int left = (int)min((int64_t)8, a.N - c);
     float sum[8] = {};
-    for (int j = 0; j < a.top_k; j++) {
-        const int place = __builtin_amdgcn_readfirstlane(a.place[t * a.top_k + j]);
-        if (place < 0 || place >= a.rows) continue;
-        const float w = a.weight ? a.weight[t * a.top_k + j] : 1.0f;
-        float v[8];
-        load8((const T*)a.Y + (int64_t)place * a.ldy + c, left, v);
+    auto choices = [&](int j, auto number) {
+        constexpr int U = decltype(number)::value;
+        Raw8<T> v[U] = {};
+        float w[U];
+        bool there[U];
 #pragma unroll
-        for (int i = 0; i < 8; i++) sum[i] += w * v[i];
-    }
+        for (int u = 0; u < U; u++) {
+            const int place = a.place[t * a.top_k + j + u];
+            there[u] = place >= 0 && place < a.rows;
+            w[u] = a.weight ? a.weight[t * a.top_k + j + u] : 1.0f;
+            if (there[u]) v[u] = load8_of<WHOLE>((const T*)a.Y + (int64_t)place * a.ldy, c, a.N);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            v[u] = settled<T, WHOLE>(v[u], c, a.N);
+#pragma unroll
+            for (int i = 0; i < 8; i++) { const float next = sum[i] + w[u] * (float)v[u][i]; sum[i] = there[u] ? next : sum[i]; }
+        }
+    };
+    int j = 0;
+    for (; j + 4 <= a.top_k; j += 4) choices(j, std::integral_constant<int, 4>{});
+    if (j + 2 <= a.top_k) { choices(j, std::integral_constant<int, 2>{}); j += 2; }
+    if (j < a.top_k) choices(j, std::integral_constant<int, 1>{});
     if (a.add) {
-        float v[8];
-        load8((const T*)a.add + t * a.ld_add + c, left, v);
+        const Raw8<T> v = settled<T, WHOLE>(load8_of<WHOLE>((const T*)a.add + t * a.ld_add, c, a.N), c, a.N);
 #pragma unroll
-        for (int i = 0; i < 8; i++) sum[i] += v[i];
+        for (int i = 0; i < 8; i++) sum[i] += (float)v[i];
     }
-    store8((OT*)a.out + t * a.ldo + c, left, sum);
+    store8_of<WHOLE>((OT*)a.out + t * a.ldo + c, (int)min((int64_t)8, a.N - c), sum);
 }
 
 // ---- the gradients of that -----------------------------------------------------------------------------------------------------------
-// W wavefronts a token, R tokens a workgroup, P chunks of 8 columns a lane in registers; LOOP: rows of any length, gone through again for each choice
-template <typename T, int W, int P, int R, bool LOOP>
-__global__ __launch_bounds__(64 * W * R) void combine_grad_kernel(const CombineGradArgs a)
+// L threads a token, R tokens a workgroup, P chunks of 8 columns a thread, U choices at a time
+template <typename T, bool WHOLE, int L, int P, int R, int U>
+__global__ __launch_bounds__(L * R) void combine_grad_kernel(const CombineGradArgs a)
 {
-    __shared__ float lds[W * R];
-    const int lane = threadIdx.x % (64 * W);
-    const int64_t t = (int64_t)blockIdx.x * R + threadIdx.x / (64 * W);
+    constexpr int WAVES = L * R / 64, W = L > 64 ? L / 64 : 1;
+    __shared__ float lds[2][U][WAVES];
+    const int lane = threadIdx.x % L, wave = threadIdx.x >> 6;
+    int64_t t = (int64_t)blockIdx.x * R + threadIdx.x / L;
+    if constexpr (L == 64) t = (int64_t)blockIdx.x * R + __builtin_amdgcn_readfirstlane(wave);
     const bool live = t < a.T;
-    const T* const d = (const T*)a.dOut + t * a.lddo;
+    t = min(t, a.T - 1);
     Raw8<T> dout[P];
-    if constexpr (!LOOP) {
 #pragma unroll
-        for (int p = 0; p < P; p++) dout[p] = load8_raw(d + 8 * (lane + 64 * W * p), live ? a.N - 8 * (lane + 64 * W * p) : 0);
-    }
-    for (int j = 0; j < a.top_k; j++) {
-        const int place = live ? a.place[t * a.top_k + j] : -1;
-        const bool there = place >= 0 && place < a.rows;
-        const float w = there && a.weight ? a.weight[t * a.top_k + j] : 1.0f;
-        const T* const y = (const T*)a.Y + (int64_t)place * a.ldy;
-        T* const dy = (T*)a.dY + (int64_t)place * a.lddy;
-        float dot = 0.0f;
-        auto chunk = [&](int64_t c, const Raw8<T>& g) {
-            const int left = (int)min((int64_t)8, a.N - c);
-            if (a.dweight) {
-                float v[8];
-                load8(y + c, left, v);
+    for (int p = 0; p < P; p++) dout[p] = load8_of<WHOLE>((const T*)a.dOut + t * a.lddo, 8 * (lane + L * p), a.N);
+    int slot = 0;
+    for (int j0 = 0; j0 < a.top_k; j0 += U) {
+        Raw8<T> y[U][P] = {};
+        float w[U], dot[U] = {};
+        int place[U];
 #pragma unroll
-                for (int i = 0; i < 8; i++) dot += (float)g[i] * v[i];
-            }
-            if (a.dY) {
-                float o[8];
+        for (int u = 0; u < U; u++) {
+            const int64_t at = t * a.top_k + min(j0 + u, a.top_k - 1);
+            place[u] = a.place[at];
+            if (!live || j0 + u >= a.top_k || place[u] >= a.rows) place[u] = -1;
+            w[u] = a.weight ? a.weight[at] : 1.0f;
+            if (a.dweight && place[u] >= 0) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) o[i] = w * (float)g[i];
-                store8(dy + c, left, o);
-            }
-        };
-        if (there) {
-            if constexpr (LOOP) {
-                for (int64_t c = 8 * (int64_t)lane; c < a.N; c += 512 * W) chunk(c, load8_raw(d + c, (int)min((int64_t)8, a.N - c)));
-            } else {
-#pragma unroll
-                for (int p = 0; p < P; p++) if (8 * (lane + 64 * W * p) < a.N) chunk(8 * (lane + 64 * W * p), dout[p]);
+                for (int p = 0; p < P; p++) y[u][p] = load8_of<WHOLE>((const T*)a.Y + (int64_t)place[u] * a.ldy, 8 * (lane + L * p), a.N);
             }
         }
+        if (j0 == 0) {
+#pragma unroll
+            for (int p = 0; p < P; p++) dout[p] = settled<T, WHOLE>(dout[p], 8 * (lane + L * p), a.N);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+#pragma unroll
+            for (int p = 0; p < P; p++) {
+                const int c = 8 * (lane + L * p);
+                y[u][p] = settled<T, WHOLE>(y[u][p], c, a.N);
+#pragma unroll
+                for (int i = 0; i < 8; i++) dot[u] += (float)dout[p][i] * (float)y[u][p][i];
+                if (a.dY && place[u] >= 0 && c < a.N) {
+                    float o[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) o[i] = w[u] * (float)dout[p][i];
+                    store8_of<WHOLE>((T*)a.dY + (int64_t)place[u] * a.lddy + c, a.N - c, o);
+                }
+            }
+        }
+        if (!a.dweight) continue;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if constexpr (L >= 64) dot[u] = sum64(dot[u]);
+            else {
+#pragma unroll
+                for (int d = 1; d < L; d <<= 1) dot[u] += __shfl_xor(dot[u], d);
+            }
+        }
+        if constexpr (L > 64) {                            // two sets in turn: one barrier for U choices
+#pragma unroll
+            for (int u = 0; u < U; u++) if ((threadIdx.x & 63) == 0) lds[slot][u][wave] = dot[u];
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                dot[u] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < W; i++) dot[u] += lds[slot][u][wave / W * W + i];
+            }
+            slot ^= 1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) if (live && lane == 0 && j0 + u < a.top_k) a.dweight[t * a.top_k + j0 + u] = place[u] >= 0 ? dot[u] : 0.0f;
+    }
+}
+// rows of any length, a workgroup a token, gone through again for each choice
+template <typename T>
+__global__ __launch_bounds__(512) void combine_grad_long_kernel(const CombineGradArgs a)
+{
+    __shared__ float lds[8];
+    const int64_t t = blockIdx.x;
+    const T* const d = (const T*)a.dOut + t * a.lddo;
+    for (int j = 0; j < a.top_k; j++) {
+        const int place = a.place[t * a.top_k + j];
+        const bool there = place >= 0 && place < a.rows;
+        const float w = a.weight ? a.weight[t * a.top_k + j] : 1.0f;
+        float dot = 0.0f;
+        for (int64_t c = 8 * (int64_t)threadIdx.x; there && c < a.N; c += 4096) {
+            const int left = (int)min((int64_t)8, a.N - c);
+            float g[8], v[8], o[8];
+            load8(d + c, left, g);
+            if (a.dweight) {
+                load8((const T*)a.Y + (int64_t)place * a.ldy + c, left, v);
+#pragma unroll
+                for (int i = 0; i < 8; i++) dot += g[i] * v[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) o[i] = w * g[i];
+            if (a.dY) store8((T*)a.dY + (int64_t)place * a.lddy + c, left, o);
+        }
         if (a.dweight) {
-            dot = sum_row<W>(dot, lds);
-            if (live && lane == 0) a.dweight[t * a.top_k + j] = dot;
+            dot = sum_row<8>(dot, lds);
+            if (threadIdx.x == 0) a.dweight[t * a.top_k + j] = dot;
         }
     }
 }
 
-template <typename T, int W, int P, int R, bool LOOP = false>
+template <typename T, int L, int P, int R, int U>
 int launch_combine_grad(const CombineGradArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((combine_grad_kernel<T, W, P, R, LOOP>), dim3((unsigned)((a.T + R - 1) / R)), dim3(64 * W * R), 0, stream, a);
+    const dim3 grid((unsigned)((a.T + R - 1) / R));
+    if (a.N % 8 == 0) hipLaunchKernelGGL((combine_grad_kernel<T, true, L, P, R, U>), grid, dim3(L * R), 0, stream, a);
+    else hipLaunchKernelGGL((combine_grad_kernel<T, false, L, P, R, U>), grid, dim3(L * R), 0, stream, a);
+    return launched();
+}
+template <typename T>
+int launch_combine_grad_long(const CombineGradArgs& a, hipStream_t stream)
+{
+    hipLaunchKernelGGL(combine_grad_long_kernel<T>, dim3((unsigned)a.T), dim3(512), 0, stream, a);
     return launched();
 }
 template <typename T>
 int combine_grad_of_type(const CombineGradArgs& a, hipStream_t stream)
 {
-    if (a.N <= 512) return launch_combine_grad<T, 1, 1, 4>(a, stream);
-    if (a.N <= 1024) return launch_combine_grad<T, 1, 2, 4>(a, stream);
-    if (a.N <= 2048) return launch_combine_grad<T, 1, 4, 4>(a, stream);
-    if (a.N <= 4096) return launch_combine_grad<T, 4, 2, 1>(a, stream);
-    if (a.N <= 8192) return launch_combine_grad<T, 4, 4, 1>(a, stream);
-    return launch_combine_grad<T, 8, 1, 1, true>(a, stream);
+    if (a.N == 0) return launch_combine_grad_long<T>(a, stream);             // zeros to dweight: the others read a row's last 8 elements in place of what it has not
+    if (a.T <= 2 * chip().cus && a.N > 1024 && a.N <= 8192) return a.N <= 4096 ? launch_combine_grad<T, 512, 1, 1, 4>(a, stream) : launch_combine_grad<T, 1024, 1, 1, 4>(a, stream);
+    if (a.N <= 64) return launch_combine_grad<T, 8, 1, 32, 4>(a, stream);
+    if (a.N <= 128) return launch_combine_grad<T, 16, 1, 16, 4>(a, stream);
+    if (a.N <= 256) return launch_combine_grad<T, 32, 1, 8, 4>(a, stream);
+    if (a.N <= 512) return launch_combine_grad<T, 64, 1, 4, 4>(a, stream);
+    if (a.N <= 1024) return launch_combine_grad<T, 64, 2, 4, 2>(a, stream);
+    if (a.N <= 2048) return launch_combine_grad<T, 64, 4, 4, 2>(a, stream);
+    if (a.N <= 4096) return launch_combine_grad<T, 256, 2, 1, 2>(a, stream);
+    return a.N <= 8192 ? launch_combine_grad<T, 256, 4, 1, 2>(a, stream) : launch_combine_grad_long<T>(a, stream);
 }
 
-template <typename T, typename OT>
+template <typename T, typename OT, int L>
 int launch_combine(const CombineArgs& a, hipStream_t stream)
 {
-    const int64_t pieces = ((int64_t)a.N + 511) / 512, items = a.T * pieces;
-    hipLaunchKernelGGL((combine_kernel<T, OT>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, a, pieces, items);
+    const int64_t pieces = ((int64_t)a.N + 8 * L - 1) / (8 * L), items = a.T * pieces;
+    const dim3 grid((unsigned)((items + 256 / L - 1) / (256 / L)));
+    if (a.N % 8 == 0) hipLaunchKernelGGL((combine_kernel<T, OT, true, L>), grid, dim3(256), 0, stream, a, pieces, items);
+    else hipLaunchKernelGGL((combine_kernel<T, OT, false, L>), grid, dim3(256), 0, stream, a, pieces, items);
     return launched();
+}
+template <typename T, typename OT>
+int combine_of_type(const CombineArgs& a, hipStream_t stream)
+{
+    return a.N <= 64 ? launch_combine<T, OT, 8>(a, stream) : a.N <= 128 ? launch_combine<T, OT, 16>(a, stream) : a.N <= 256 ? launch_combine<T, OT, 32>(a, stream) : launch_combine<T, OT, 64>(a, stream);
 }
 
 // Tokens need nothing of each other: more than the grid of one launch has wavefronts for (pieces of a token each) go in several.
@@ -389,9 +563,9 @@ const char* ahead(const void* p, int64_t bytes) { return p ? (const char*)p + by
 int64_t ops_dispatch_workspace_bytes(int64_t n, int64_t E)
 {
     if (n <= FEW) return 0;
+    if (E <= ONE_DIGIT && n <= SOME) return up16(4 * (E + 1) * (most_parts(E) + 1));
     int part_rows;
-    const int64_t parts = parts_of(n, part_rows), bins = E <= ONE_DIGIT ? E + 1 : 256;
-    return up16(4 * bins * (parts + 1)) + (E <= ONE_DIGIT ? 0 : 2 * up16(4 * n));
+    return up16(4 * 256 * ((int64_t)parts_of(n, part_rows) + 1)) + 2 * up16(4 * n);
 }
 
 int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stream)
@@ -410,27 +584,39 @@ int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stre
         else hipLaunchKernelGGL(dispatch_few_kernel<16>, grid, dim3(256), 0, stream, a, pieces, items);
         return launched();
     }
+    if (a.E <= ONE_DIGIT && n <= SOME) {
+        Parts s = {};
+        s.a = a;
+        const int bins = a.E + 1;
+        const int64_t some = a.top_k < 64 ? 64 / a.top_k : 1, enough = (a.T + most_parts(a.E) - 1) / most_parts(a.E);
+        s.tokens = (int)(some > enough ? some : enough);
+        s.parts = (int)((a.T + s.tokens - 1) / s.tokens);
+        s.totals = (int32_t*)workspace;
+        s.counts = s.totals + bins;
+        SortPass scan = {};
+        scan.bins = bins; scan.parts = s.parts; scan.counts = s.counts; scan.totals = s.totals;
+        const int64_t waves = items + (bins + 63) / 64;
+        if (!fits_a_launch((waves + 3) / 4, 256)) return GEMM_F16_ERR_SIZE;
+        hipLaunchKernelGGL(part_count_kernel, dim3((s.parts + 3) / 4), dim3(256), 4 * bins * sizeof(int), stream, s);
+        hipLaunchKernelGGL(sort_scan_kernel, dim3((bins + 3) / 4), dim3(256), 0, stream, scan);
+        // rows that are more than half of the 256 MB cache go past it: 8192 tokens to 2 of 16, bf16 rows of 4096, 37 us against 47, and 99 against 97 with a copy of the rows after it; below
+        // that what reads them next is faster with them in the cache: 4096 tokens 54 against 49 with the copy, 5000 to 8 of 64, rows of 1000, 64 against 52
+        if (n * bytes >= 128e6) hipLaunchKernelGGL(part_move_kernel<true>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, pieces, items);
+        else hipLaunchKernelGGL(part_move_kernel<false>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, pieces, items);
+        return launched();
+    }
     SortPass s = {};
     s.a = a;
     s.parts = parts_of(n, s.part_rows);
-    int rc;
-    if (a.E <= ONE_DIGIT) {
-        s.shift = 0;
-        s.bins = a.E + 1;
-        s.totals = (int32_t*)workspace;
-        s.counts = s.totals + s.bins;
-        rc = sort_pass(s, stream);
-    } else {
-        s.totals = (int32_t*)workspace;
-        s.counts = s.totals + 256;
-        int32_t* const order = (int32_t*)((char*)workspace + up16(4 * 256 * ((int64_t)s.parts + 1)));
-        int32_t* const keys = (int32_t*)((char*)order + up16(4 * n));
-        s.shift = -1; s.bins = 256; s.out = order;
-        rc = sort_pass(s, stream);
-        s.seq = order; s.shift = 8; s.bins = (a.E >> 8) + 1; s.out = nullptr; s.keys = keys;
-        if (rc == GEMM_F16_OK) rc = sort_pass(s, stream);
-        if (rc == GEMM_F16_OK) hipLaunchKernelGGL(sort_offsets_kernel, dim3((unsigned)(((int64_t)a.E + 256) / 256)), dim3(256), 0, stream, keys, n, a.E, a.offsets);
-    }
+    s.totals = (int32_t*)workspace;
+    s.counts = s.totals + 256;
+    int32_t* const order = (int32_t*)((char*)workspace + up16(4 * 256 * ((int64_t)s.parts + 1)));
+    int32_t* const keys = (int32_t*)((char*)order + up16(4 * n));
+    s.shift = -1; s.bins = 256; s.out = order;
+    int rc = sort_pass(s, stream);
+    s.seq = order; s.shift = 8; s.bins = (a.E >> 8) + 1; s.out = nullptr; s.keys = keys;
+    if (rc == GEMM_F16_OK) rc = sort_pass(s, stream);
+    if (rc == GEMM_F16_OK) hipLaunchKernelGGL(sort_offsets_kernel, dim3((unsigned)(((int64_t)a.E + 256) / 256)), dim3(256), 0, stream, keys, n, a.E, a.offsets);
     if (rc == GEMM_F16_OK) rc = launched();
     if (rc != GEMM_F16_OK || !a.X) return rc;
     return by_tokens(a.T, pieces, [&](int64_t t, int64_t tokens) {
@@ -454,9 +640,9 @@ int ops_launch_combine(int type, int out_type, const CombineArgs& all, hipStream
         a.weight = (const float*)ahead(all.weight, 4 * t * all.top_k);
         a.add = ahead(all.add, t * all.ld_add * size);
         a.out = (char*)all.out + t * all.ldo * out_size;
-        if (type == GEMM_TYPE_F32) return launch_combine<float, float>(a, stream);
-        if (type == GEMM_TYPE_F16) return out_type == GEMM_TYPE_F32 ? launch_combine<half_t, float>(a, stream) : launch_combine<half_t, half_t>(a, stream);
-        return out_type == GEMM_TYPE_F32 ? launch_combine<bf16_t, float>(a, stream) : launch_combine<bf16_t, bf16_t>(a, stream);
+        if (type == GEMM_TYPE_F32) return combine_of_type<float, float>(a, stream);
+        if (type == GEMM_TYPE_F16) return out_type == GEMM_TYPE_F32 ? combine_of_type<half_t, float>(a, stream) : combine_of_type<half_t, half_t>(a, stream);
+        return out_type == GEMM_TYPE_F32 ? combine_of_type<bf16_t, float>(a, stream) : combine_of_type<bf16_t, bf16_t>(a, stream);
     });
 }
 int ops_launch_combine_grad(int type, const CombineGradArgs& all, hipStream_t stream)
