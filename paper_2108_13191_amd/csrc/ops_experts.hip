@@ -132,7 +132,7 @@ struct SortPass {
     DispatchArgs a;
     const int32_t* seq;                                    // the choices in the order that this pass goes by; NULL: as they are
     int shift, bins, part_rows, parts;
-    int32_t *counts, *totals;                              // [digit][part], [digit]
+    int32_t *counts, *totals;                              // [digit][part], [digit]; the former become the sums of those in front
     int32_t* out;                                          // the choices as this pass orders them; NULL: the places and sources are written
     int32_t* keys;                                         // the experts in order, of the last pass
 };
@@ -161,18 +161,24 @@ __device__ __forceinline__ int scan64(int x)
     return x;
 }
 
-__global__ __launch_bounds__(256) void sort_scan_kernel(const SortPass s)
+// a workgroup for each digit
+__global__ __launch_bounds__(1024) void sort_scan_kernel(int32_t* counts, int32_t* totals, int parts)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b >= s.bins) return;
-    int32_t* const c = s.counts + (int64_t)b * s.parts;
-    int before = 0;
-    for (int p = 0; p < s.parts; p += 64) {
-        const int v = p + lane < s.parts ? c[p + lane] : 0, incl = scan64(v);
-        if (p + lane < s.parts) c[p + lane] = before + incl - v;
-        before += __builtin_amdgcn_readlane(incl, 63);
+    __shared__ int sums[2][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64;
+    int32_t* const c = counts + (int64_t)blockIdx.x * parts;
+    int before = 0, slot = 0;
+    for (int p0 = 0; p0 < parts; p0 += blockDim.x) {
+        const int p = p0 + threadIdx.x, v = p < parts ? c[p] : 0, incl = scan64(v);
+        if (lane == 63) sums[slot][wave] = incl;
+        __syncthreads();                                   // (two sets of sums in turn)
+        int front = 0, all = 0;
+        for (int w = 0; w < waves; w++) { const int n = sums[slot][w]; all += n; front += w < wave ? n : 0; }
+        if (p < parts) c[p] = before + front + incl - v;
+        before += all;
+        slot ^= 1;
     }
-    if (lane == 0) s.totals[b] = before;
+    if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
 __global__ __launch_bounds__(256) void sort_place_kernel(const SortPass s)
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(const SortPass s)
 }
 
 // ---- up to 2047 experts and 2^19 choices: places and rows in one launch, behind two short ones -----------------------------------------
-// The tokens go in `parts` parts, of 64 choices each where there are no more than a thousand of those.  One launch counts the experts of each part, a second one adds the counts of
+// The tokens go in `parts` parts of 64 choices, or more where the counts would pass 4 MB.  One launch counts the experts of each part, a second one adds the counts of
 // the parts in front (sort_scan_kernel).  In the third each wavefront finds its token's places by itself, from the counts and the choices of its part in front of its own, while
 // the piece of the token's row that it copies is on its way.
 struct Parts {
@@ -307,6 +313,63 @@ __global__ __launch_bounds__(256) void part_move_kernel(const Parts s, int64_t p
     }
 }
 
+// The same for rows of up to 256 bytes in parts of 64 choices and less: a wavefront for a part, whose lanes of one expert find each other; R lanes a row, 64 / R rows at a time.
+__global__ __launch_bounds__(256) void part_move_narrow_kernel(const Parts s, int R)
+{
+    const DispatchArgs& a = s.a;
+    const int lane = threadIdx.x & 63;
+    const int64_t part = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (part >= s.parts) {                                 // offsets, 64 a wavefront
+        const int64_t e = (part - s.parts) * 64 + lane;
+        if (e - lane > a.E) return;
+        const int start = rows_before(s, (int)e);
+        if (e <= a.E) a.offsets[e] = start;
+        return;
+    }
+    const int64_t t0 = part * s.tokens, first = t0 * a.top_k, bytes = (int64_t)a.N * a.size;
+    const int mine = (int)(min(a.T - t0, (int64_t)s.tokens) * a.top_k);
+    const int key = lane < mine ? key_of(a, first + lane) : a.E + 1;
+    const int front = lane < mine ? s.counts[(int64_t)key * s.parts + part] : 0;
+    uint64_t same = mine < 64 ? (1ull << mine) - 1 : ~0ull;
+    const int bits = 32 - __builtin_clz(a.E | 1);
+    for (int b = 0; b < bits; b++) {
+        const bool set = (key >> b) & 1;
+        const uint64_t m = __ballot(set);
+        same &= set ? m : ~m;
+    }
+    const int rank = rows_before(s, key) + front + __popcll(same & ((1ull << lane) - 1));
+    const int at = key < a.E ? rank : -1, token = lane / a.top_k;
+    if (lane < mine) {
+        a.place[first + lane] = at;
+        if (a.source) a.source[rank] = key < a.E ? (int32_t)(t0 + token) : -1;
+    }
+    if (!a.X) return;
+    if (at >= 0)
+        for (int64_t b = 0; b < a.blocks; b++) a.row_scale[b * a.ld_row_scale + at] = a.scale[b * a.ld_scale + t0 + token];
+    const int rows = 64 / R, sub = lane / R;
+    const int64_t byte = bytes < 16 ? 0 : min((int64_t)16 * (lane % R), bytes - 16);
+    constexpr int U = 4;
+    for (int c0 = 0; c0 < mine; c0 += U * rows) {
+        uintx4 v[U];
+        int to[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int c = c0 + u * rows + sub;
+            to[u] = __shfl(at, c & 63);
+            if (c >= mine) to[u] = -1;
+            if (bytes >= 16) v[u] = *(const uintx4_any*)((const char*)a.X + (t0 + __shfl(token, min(c, mine - 1))) * a.ldx * a.size + byte);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (to[u] < 0) continue;
+            char* const out = (char*)a.rows + (int64_t)to[u] * a.ld_rows * a.size + byte;
+            if (bytes >= 16) { *(uintx4_any*)out = v[u]; continue; }
+            const char* const in = (const char*)a.X + (t0 + (c0 + u * rows + sub) / a.top_k) * a.ldx * a.size;
+            for (int b = 0; b < bytes; b++) out[b] = in[b];
+        }
+    }
+}
+
 // offsets of sorted experts: the first row of each that is not below it
 __global__ __launch_bounds__(256) void sort_offsets_kernel(const int32_t* __restrict__ keys, int64_t n, int E, int32_t* __restrict__ offsets)
 {
@@ -328,8 +391,10 @@ __global__ __launch_bounds__(256) void zero_offsets_kernel(int32_t* offsets, int
 
 constexpr int FEW = 1024, ONE_DIGIT = 2047;                // choices of one launch; experts of one pass
 constexpr int MOST_PARTS = 256;
+// bytes of a row that is copied by part: 20000 tokens to 8 of 64, rows of 128 bytes 16.9 us, by token 31.5; of 256 20.6 | 31.9; of 512 38.9 | 35.1
+constexpr int64_t NARROW = 256;
 constexpr int64_t SOME = 1 << 19;                          // choices that are placed by part
-int64_t most_parts(int64_t E) { return E < 1024 ? 1024 : 512; }      // at most 4 MB of counts
+int64_t most_parts(int64_t E) { return (1 << 20) / (E + 1); }      // 4 MB of counts
 
 int parts_of(int64_t n, int& part_rows)
 {
@@ -342,10 +407,15 @@ int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 int launched() { return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH; }
 
+void launch_scan(int bins, int32_t* counts, int32_t* totals, int parts, hipStream_t stream)
+{
+    hipLaunchKernelGGL(sort_scan_kernel, dim3(bins), dim3(parts <= 256 ? 256 : 1024), 0, stream, counts, totals, parts);
+}
+
 int sort_pass(SortPass s, hipStream_t stream)
 {
     hipLaunchKernelGGL(sort_count_kernel, dim3(s.parts), dim3(256), s.bins * sizeof(int), stream, s);
-    hipLaunchKernelGGL(sort_scan_kernel, dim3((s.bins + 3) / 4), dim3(256), 0, stream, s);
+    launch_scan(s.bins, s.counts, s.totals, s.parts, stream);
     hipLaunchKernelGGL(sort_place_kernel, dim3(s.parts), dim3(256), 4 * s.bins * sizeof(int), stream, s);
     return launched();
 }
@@ -593,15 +663,18 @@ int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stre
         s.parts = (int)((a.T + s.tokens - 1) / s.tokens);
         s.totals = (int32_t*)workspace;
         s.counts = s.totals + bins;
-        SortPass scan = {};
-        scan.bins = bins; scan.parts = s.parts; scan.counts = s.counts; scan.totals = s.totals;
-        const int64_t waves = items + (bins + 63) / 64;
+        const bool narrow = bytes <= NARROW && (int64_t)s.tokens * a.top_k <= 64;
+        const int64_t waves = (narrow ? s.parts : items) + (bins + 63) / 64;
         if (!fits_a_launch((waves + 3) / 4, 256)) return GEMM_F16_ERR_SIZE;
         hipLaunchKernelGGL(part_count_kernel, dim3((s.parts + 3) / 4), dim3(256), 4 * bins * sizeof(int), stream, s);
-        hipLaunchKernelGGL(sort_scan_kernel, dim3((bins + 3) / 4), dim3(256), 0, stream, scan);
+        launch_scan(bins, s.counts, s.totals, s.parts, stream);
         // rows that are more than half of the 256 MB cache go past it: 8192 tokens to 2 of 16, bf16 rows of 4096, 37 us against 47, and 99 against 97 with a copy of the rows after it; below
         // that what reads them next is faster with them in the cache: 4096 tokens 54 against 49 with the copy, 5000 to 8 of 64, rows of 1000, 64 against 52
-        if (n * bytes >= 128e6) hipLaunchKernelGGL(part_move_kernel<true>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, pieces, items);
+        if (narrow) {
+            int R = 1;
+            while (16 * R < bytes) R *= 2;
+            hipLaunchKernelGGL(part_move_narrow_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, R);
+        } else if (n * bytes >= 128e6) hipLaunchKernelGGL(part_move_kernel<true>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, pieces, items);
         else hipLaunchKernelGGL(part_move_kernel<false>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, s, pieces, items);
         return launched();
     }
