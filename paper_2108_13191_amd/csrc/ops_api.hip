@@ -46,7 +46,7 @@ Form few_rows(int fm, int nb) { return {Form::FEW_ROWS, TILE_256, fm, nb}; }
 // Whether its workgroups are as many as one launch takes
 bool fits(const OpsGemm& g, const Form& f)
 {
-    const bool wide = f.tile == TILE_256 || f.tile == TILE_128x256, tall = f.tile == TILE_256 || f.tile == TILE_256x128;
+    const bool square = f.tile == TILE_256 || f.tile == TILE_256_LONG, wide = square || f.tile == TILE_128x256, tall = square || f.tile == TILE_256x128;
     const int bm = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.fm : tall ? 256 : 128;
     const int bn = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.nb : wide ? 256 : 128;
     const int64_t grid = tile_grid(g, bm, bn);
@@ -84,7 +84,12 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
             const int nb = (fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus) || (fm == 1 && expected_tiles(g, 16, 64) >= cus) ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
             return few_rows(fm, nb);
         }
-        return tiles(large ? TILE_256 : TILE_128);
+        if (!large) return tiles(TILE_128);
+        // 256 x 256 by four wavefronts, whose k steps are shorter (8192^3 394 | 436, (4096,8192,16384) 366 | 401) and whose tiles cost more around the loop, its code's first
+        // pass above all, from so many k steps of a compute unit on: (4096,4096,4096) 32: 53.6 | 56.1, (8192,8192,2048) 64: 130 | 131, f32 152 | 155, 16384 rows of 16 experts
+        // (4096,2048) 80: 161 | 165, (8192,1024) 72: 203 | 209; fewer: (8192,8192,1024) 32: 93 | 89, (3000,3000,4096) 18: 51 | 47, (16384,2304,768) 14: 53 | 49
+        const double steps = (g.K + 127) / 128, all = steps * expected_tiles(g, 256, 256) / cus;
+        return tiles(steps >= 8.0 && (all >= 48.0 || (steps >= 32.0 && all >= 31.0)) ? TILE_256_LONG : TILE_256);
     }
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
@@ -149,6 +154,7 @@ const char* name_of(const OpsGemm& g, const Form& f)
     const bool e4m3 = g.elem == ELEM_E4M3;
     switch (f.tile) {
     case TILE_256: return e4m3 ? "e4m3_256x256" : "256x256";
+    case TILE_256_LONG: return "256x256_long";
     case TILE_128_FAST: return "e4m3_128x128";
     case TILE_256x128: return "widened_256x128";
     case TILE_128_PAIR: return "widened_128x128_two";

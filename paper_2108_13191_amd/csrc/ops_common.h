@@ -59,11 +59,13 @@ int ops_launch_generic(const OpsGemm& g);
 
 // ops_tile_*.hip: 16-byte aligned operands (TILE_128_ANY: any) with pitches up to 2^22 elements (each takes the tiles that the choice in ops_api.hip has for it)
 // e4m3: TILE_256 and TILE_128_FAST on the e4m3 instructions, the others widened to f16 (_PAIR: two workgroups a compute unit, _SHORT: short groups of rows)
-enum OpsTile { TILE_256, TILE_256x128, TILE_128x256, TILE_128, TILE_128_ANY, TILE_128_FAST, TILE_128_PAIR, TILE_128_SHORT };
+enum OpsTile { TILE_256, TILE_256x128, TILE_128x256, TILE_128, TILE_128_ANY, TILE_128_FAST, TILE_128_PAIR, TILE_128_SHORT, TILE_256_LONG };
 int ops_launch_tiles_e4m3(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_f16(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_bf16(const OpsGemm& g, OpsTile tile);
 int ops_launch_tiles_i8(const OpsGemm& g, OpsTile tile);
+// ops_i8_long.hip: TILE_256_LONG, i8 on 256 x 256 tiles of four wavefronts; K >= 128
+int ops_launch_long_i8(const OpsGemm& g);
 
 // ops_skinny.hip: few rows, e4m3 and i8; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 1 x 4 (i8), 2 x 1, 2 x 2 or 2 x 4
 int ops_launch_skinny(const OpsGemm& g, int fm, int nb);

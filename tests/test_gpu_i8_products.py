@@ -21,7 +21,8 @@ def scales(rng, *shape):
 
 
 def expected(a, sa, b, sb):
-    return (a @ b.T).astype(np.float64) * sa[:, None] * sb[None, :]
+    """(sums below 2^31: exact in 64-bit floating point)"""
+    return (a.astype(np.float64) @ b.astype(np.float64).T) * sa[:, None] * sb[None, :]
 
 
 def bound(want, c):
