@@ -1,0 +1,66 @@
+"""The entry points of include/gemm_layer.h that expert_layer.py calls, on the host, as ops_emulation.py has those of gemm_ops.h.  (Rows are moved by torch there.)"""
+import torch
+
+from ops_emulation import KIND, at, mat
+from paper_2108_13191_amd import binding
+
+
+def quantize(y, Q, ldq, scale):
+    M, N = y.shape
+    s = y.abs().amax(1).clamp_min(2.0 ** -96) * torch.tensor(1 / 127.0)
+    at(scale, torch.float32, (M, 1)).copy_(s)
+    mat(Q, torch.int8, M, N, ldq).copy_((y.double() / s.double()[:, None]).round())
+
+
+def quantize_i8_rows(M, N, type, act, X, ldx, Q, ldq, scale, stream=0):
+    x = mat(X, KIND[type], M, 2 * N if act == binding.ACT_SWIGLU else N, ldx).float()
+    quantize(torch.nn.functional.silu(x[:, :N]) * x[:, N:] if act == binding.ACT_SWIGLU else x, Q, ldq, scale)
+    return binding.OK
+
+
+def layer_norm(M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream=0):
+    kind = KIND[type]
+    h = (mat(X, kind, M, N, ldx).float() + mat(R, kind, M, N, ldr).float()).to(kind)
+    mat(H, kind, M, N, ldh).copy_(h)
+    m = h.float().mean(1)
+    d = h.float() - m[:, None]
+    s = torch.rsqrt(d.square().mean(1) + eps)
+    at(mean, torch.float32, (M, 1)).copy_(m)
+    at(rstd, torch.float32, (M, 1)).copy_(s)
+    y = d * s[:, None] * at(gamma, kind, (N, 1)).float() + at(beta, kind, (N, 1)).float()
+    mat(Y, kind, M, N, ldy).copy_(y)
+    if Q is not None:
+        quantize(y, Q, ldq, scale)
+    return binding.OK
+
+
+def layer_norm_grad_workspace_bytes(M, N):
+    return 16
+
+
+def layer_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream=0):
+    kind = KIND[type]
+    r, m = at(rstd, torch.float32, (M, 1))[:, None], at(mean, torch.float32, (M, 1))[:, None]
+    dy, x = mat(dY, kind, M, N, lddy).float(), (mat(H, kind, M, N, ldh).float() - m) * r
+    g = dy * at(gamma, kind, (N, 1)).float()
+    mat(dX, kind, M, N, lddx).copy_(r * (g - g.mean(1, keepdim=True) - x * (g * x).mean(1, keepdim=True)) + mat(dH, kind, M, N, lddh).float())
+    at(dgamma, torch.float32, (N, 1)).copy_((dy * x).sum(0))
+    at(dbeta, torch.float32, (N, 1)).copy_(dy.sum(0))
+    return binding.OK
+
+
+def gemm_i8_grouped(T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream=0):
+    a, c = mat(A, torch.int8, T, K, lda).double(), mat(C, KIND[c_type], T, N, ldc)
+    b, s, r = at(B, torch.int8, (E, b_stride), (N, ldb), (K, 1)).double(), at(b_scale, torch.float32, (E, bs_stride), (N, 1)), at(a_scale, torch.float32, (T, 1))
+    off = offsets.tolist()
+    for e in range(E):
+        lo, hi = off[e], off[e + 1]
+        c[lo:hi] = ((a[lo:hi] @ b[e].t()).float() * r[lo:hi, None] * s[e]).to(c.dtype)
+    return binding.OK
+
+
+def gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream=0):
+    return gemm_i8_grouped(M, N, K, 1, torch.tensor([0, M]), A, lda, a_scale, B, ldb, 0, b_scale, 0, C, ldc, c_type)
+
+
+ENTRY_POINTS = (quantize_i8_rows, layer_norm, layer_norm_grad_workspace_bytes, layer_norm_grad, gemm_i8, gemm_i8_grouped)
