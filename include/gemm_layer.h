@@ -28,8 +28,8 @@ extern "C" {
  * Outputs, each of which may be NULL: H (h), Y (y in `type`), Q with scale (y as 8-bit integers with a scale for each row, as
  * quantize_i8_rows has them, from the f32 value), mean and rstd (M f32 each, as layer_norm_grad takes them).  H may be X or R
  * themselves.  gamma, beta: N elements of `type`.  Q without scale or scale without Q is GEMM_F16_ERR_NULL; eps that is
- * negative or no number is GEMM_F16_ERR_CONFIG.  N = 0 writes nothing.  A row whose sums pass f32's range, or that holds a NaN or an
- * infinity, is NaN (Q: the scale NaN, elements 0).  Pointers of 16-bit matrices: 2-byte aligned, any pitch.
+ * negative or no number is GEMM_F16_ERR_CONFIG.  N = 0 writes nothing.  A row that holds a NaN or an infinity, or whose sum passes f32's range, is
+ * NaN (Q: the scale NaN, elements 0); where only its sum of squares does, rstd is 0 and y is beta.  Pointers of 16-bit matrices: 2-byte aligned, any pitch.
  */
 int layer_norm(int64_t M, int64_t N, int64_t type,
                const void* X, int64_t ldx, const void* R, int64_t ldr,
@@ -101,7 +101,7 @@ const char* gemm_i8_form(int64_t T, int64_t N, int64_t K, int64_t E, int64_t lda
  *     rows[place[t][j]] = X[t]                       T * top_k rows of N elements of `size` bytes (1, 2 or 4)
  *     row_scale[b][place[t][j]] = scale[b][t]        `blocks` rows of scales (e4m3: ceil(N / 128), i8: 1, none: 0), ld_scale >= T and ld_row_scale >= T * top_k
  * X NULL: only the order is formed.  Rows from offsets[E] on and their scales are left alone.  T = 0 or top_k = 0 writes zeros to offsets.
- * T * top_k <= 2^31-1, E <= 65535.  workspace: expert_dispatch_workspace_bytes(T, top_k, E) bytes (0 for few choices; at most 8 T top_k +
+ * T * top_k <= 2^31-1, top_k and E <= 65535.  workspace: expert_dispatch_workspace_bytes(T, top_k, E) bytes (0 for few choices; at most 8 T top_k +
  * 2^22), 16-byte aligned; smaller: GEMM_F16_ERR_WORKSPACE.
  */
 enum { GEMM_INDEX_I32 = 0, GEMM_INDEX_I64 = 1 };
@@ -115,7 +115,7 @@ int expert_dispatch(int64_t T, int64_t top_k, int64_t E, int64_t index_type, con
 
 /*
  * And back: out[t] = add[t] + sum_j weight[t][j] * Y[place[t][j]], over the choices in their order, each product rounded to f32 and
- * then added, `add` last, rounded once to out_type.  Y: T * top_k rows of N elements of `type` (f16, bf16 or f32); weight: T x top_k f32, contiguous, NULL: 1; add (T rows of
+ * then added, `add` last, rounded once to out_type (T and top_k as above).  Y: T * top_k rows of N elements of `type` (f16, bf16 or f32); weight: T x top_k f32, contiguous, NULL: 1; add (T rows of
  * `type`): NULL: 0; out_type: `type` itself or f32.  A place outside 0 .. T*top_k-1 adds nothing (a row without any is `add`, or zeros).  out may be add
  * itself where both have one type.  With weight NULL this is the gradient of expert_dispatch's rows (and add the one that reaches X by another way).
  *

@@ -141,7 +141,7 @@ struct CombineGradArgs {
     void* dY; int64_t lddy;
     float* dweight;
 };
-int64_t ops_dispatch_workspace_bytes(int64_t choices, int64_t E);
+int64_t ops_dispatch_workspace_bytes(int64_t T, int64_t top_k, int64_t E);
 int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stream);
 int ops_launch_combine(int type, int out_type, const CombineArgs& a, hipStream_t stream);
 int ops_launch_combine_grad(int type, const CombineGradArgs& a, hipStream_t stream);

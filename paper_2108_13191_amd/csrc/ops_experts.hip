@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(const SortPass s)
     }
 }
 
-// ---- up to 2047 experts and 2^19 choices: places and rows in one launch, behind two short ones -----------------------------------------
+// ---- up to 2047 experts and 2^19 choices, 256 a token: places and rows in one launch, behind two short ones -----------------------------------------
 // The tokens go in `parts` parts of 64 choices, or more where the counts would pass 4 MB.  One launch counts the experts of each part, a second one adds the counts of
 // the parts in front (sort_scan_kernel).  In the third each wavefront finds its token's places by itself, from the counts and the choices of its part in front of its own, while
 // the piece of the token's row that it copies is on its way.
@@ -292,9 +292,9 @@ __global__ __launch_bounds__(256) void part_move_kernel(const Parts s, int64_t p
         for (int64_t i0 = part * s.tokens * a.top_k; i0 < first + mine - 1; i0 += 64) {
             const int64_t i = i0 + lane;
             const int key = i < n ? key_of(a, i) : a.E + 1;
-            const int64_t in_front = first - i0;           // lanes in front of the token's choice 0 here
+            const int64_t in_front = first - i0;           // lanes in front of the token's choice 0 here; below 0: the token began in the 64 choices before these
             for (int j = 0; j < mine; j++) {
-                const uint64_t front_of_j = in_front + j >= 64 ? ~0ull : (1ull << (in_front + j)) - 1;
+                const uint64_t front_of_j = in_front + j >= 64 ? ~0ull : in_front + j <= 0 ? 0ull : (1ull << (in_front + j)) - 1;
                 const int c = __popcll(__ballot(key == __builtin_amdgcn_readlane(own, j)) & front_of_j);
                 if (lane == j) at += c;
             }
@@ -394,6 +394,8 @@ constexpr int MOST_PARTS = 256;
 // bytes of a row that is copied by part: 20000 tokens to 8 of 64, rows of 128 bytes 16.9 us, by token 31.5; of 256 20.6 | 31.9; of 512 38.9 | 35.1
 constexpr int64_t NARROW = 256;
 constexpr int64_t SOME = 1 << 19;                          // choices that are placed by part
+constexpr int64_t SHORT_LIST = 256;                        // ... of a token: those in front of each are gone through for each, so that the work grows with their square
+bool by_part(int64_t n, int64_t top_k, int64_t E) { return E <= ONE_DIGIT && n <= SOME && top_k <= SHORT_LIST; }
 int64_t most_parts(int64_t E) { return (1 << 20) / (E + 1); }      // 4 MB of counts
 
 int parts_of(int64_t n, int& part_rows)
@@ -630,10 +632,11 @@ const char* ahead(const void* p, int64_t bytes) { return p ? (const char*)p + by
 
 }  // namespace
 
-int64_t ops_dispatch_workspace_bytes(int64_t n, int64_t E)
+int64_t ops_dispatch_workspace_bytes(int64_t T, int64_t top_k, int64_t E)
 {
+    const int64_t n = T * top_k;
     if (n <= FEW) return 0;
-    if (E <= ONE_DIGIT && n <= SOME) return up16(4 * (E + 1) * (most_parts(E) + 1));
+    if (by_part(n, top_k, E)) return up16(4 * (E + 1) * (most_parts(E) + 1));
     int part_rows;
     return up16(4 * 256 * ((int64_t)parts_of(n, part_rows) + 1)) + 2 * up16(4 * n);
 }
@@ -654,7 +657,7 @@ int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stre
         else hipLaunchKernelGGL(dispatch_few_kernel<16>, grid, dim3(256), 0, stream, a, pieces, items);
         return launched();
     }
-    if (a.E <= ONE_DIGIT && n <= SOME) {
+    if (by_part(n, a.top_k, a.E)) {
         Parts s = {};
         s.a = a;
         const int bins = a.E + 1;

@@ -7,8 +7,8 @@ namespace {
 constexpr int64_t MOST_K_I8 = 131071;                      // 2^14 K < 2^31: no sum of products leaves 32 bits
 
 bool bad_index(int64_t type) { return type != GEMM_INDEX_I32 && type != GEMM_INDEX_I64; }
-// T tokens of top_k choices; their number fits an int
-bool bad_choices(int64_t T, int64_t top_k) { return bad_size(T) || bad_size(top_k) || (T > 0 && top_k > INT32_MAX / T); }
+// T tokens of top_k choices, whose number fits an int.  A token's choices go one after another, which takes a wavefront some 20 ms at 65535 and would not end for minutes at 2^31
+bool bad_choices(int64_t T, int64_t top_k) { return bad_size(T) || top_k < 0 || top_k > 65535 || (T > 0 && top_k > INT32_MAX / T); }
 
 OpsGemm shaped_i8(int64_t M, int64_t N, int64_t K, int64_t E, const int32_t* offsets, int64_t c_type, void* stream)
 {
@@ -117,7 +117,7 @@ const char* gemm_i8_form(int64_t T, int64_t N, int64_t K, int64_t E, int64_t lda
 int64_t expert_dispatch_workspace_bytes(int64_t T, int64_t top_k, int64_t E)
 {
     if (bad_choices(T, top_k) || E < 0 || E > 65535) return 0;
-    return ops_dispatch_workspace_bytes(T * top_k, E);
+    return ops_dispatch_workspace_bytes(T, top_k, E);
 }
 
 int expert_dispatch(int64_t T, int64_t top_k, int64_t E, int64_t index_type, const void* expert, int32_t* offsets, int32_t* source, int32_t* place,
@@ -135,7 +135,7 @@ int expert_dispatch(int64_t T, int64_t top_k, int64_t E, int64_t index_type, con
     if (n > 0) {
         if (unaligned(expert, index_type == GEMM_INDEX_I64 ? 8 : 4) || unaligned(source, 4) || unaligned(place, 4) ||
             (moved && (unaligned(X, (uintptr_t)size) || unaligned(rows, (uintptr_t)size) || (blocks > 0 && (unaligned(scale, 4) || unaligned(row_scale, 4)))))) return GEMM_F16_ERR_ALIGN;
-        const int64_t need = ops_dispatch_workspace_bytes(n, E);
+        const int64_t need = ops_dispatch_workspace_bytes(T, top_k, E);
         if (need > 0) {
             if (!workspace) return GEMM_F16_ERR_NULL;
             if (unaligned(workspace, 16)) return GEMM_F16_ERR_ALIGN;

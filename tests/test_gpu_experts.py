@@ -65,6 +65,39 @@ def test_order(T, k, E, index, drop):
     dispatch(choices(np.random.default_rng(T + k + E), T, k, E, drop), E, index, N=5, size=2)
 
 
+# parts of more than 64 choices, whose 64s end within a token's; the first ones' experts have few rows each and many, and the last part is short
+@pytest.mark.parametrize("T,k,E", [(20000, 3, 2047), (50000, 5, 300), (60000, 7, 1000), (33000, 10, 2000), (9000, 50, 2047)])
+@pytest.mark.parametrize("drop", [0.0, 0.3])
+def test_parts_that_end_within_a_token(T, k, E, drop):
+    expert = choices(np.random.default_rng(T + k), T, k, E, drop)
+    dispatch(expert, E, N=5, size=2)
+    dispatch(np.minimum(expert, expert % 3), E, N=0)
+
+
+# a token's choices: more than a lane each, more than are placed by part, all that a call takes
+@pytest.mark.parametrize("T,k,E", [(20, 65, 9), (30, 256, 9), (30, 257, 9), (1, 1024, 5), (1, 1100, 5), (3, 700, 64), (1, 65535, 70), (2, 65535, 3000)])
+def test_long_lists_of_choices(T, k, E):
+    dispatch(choices(np.random.default_rng(T + k), T, k, E, 0.2), E, N=9, size=2, blocks=1)
+
+
+def test_the_longest_list_comes_back():
+    T, k, N = 2, 65535, 16
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    Y, weight = torch.randn(T * k, N, device="cuda", generator=gen), torch.rand(T, k, device="cuda", generator=gen)
+    place = torch.randperm(T * k, device="cuda", generator=gen).to(I32)
+    out = torch.zeros(T, N, device="cuda")
+    binding.check(binding.expert_combine(T, k, N, TYPE["f32"], place, Y, N, weight, None, 0, out, N, TYPE["f32"], stream()))
+    terms = Y.double()[place.long()].view(T, k, N) * weight.double()[..., None]
+    # each of k additions and each product rounded once in f32
+    assert bool(((out.double() - terms.sum(1)).abs() <= (k + 1) * 2.0 ** -24 * terms.abs().sum(1)).all())
+    b16, dY, dweight = Y.bfloat16(), torch.zeros(T * k, N, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, k, device="cuda")
+    dout = torch.randn(T, N, device="cuda", generator=gen).bfloat16()
+    binding.check(binding.expert_combine_grad(T, k, N, TYPE["bf16"], place, dout, N, weight, b16, N, dY, N, dweight, stream()))
+    dots = b16.double()[place.long()].view(T, k, N) * dout.double()[:, None]
+    assert bool(((dweight.double() - dots.sum(-1)).abs() <= (N + 1) * 2.0 ** -24 * dots.abs().sum(-1)).all())
+    assert torch.equal(dY[place.long()].view(T, k, N), (weight[..., None] * dout[:, None].float()).bfloat16())
+
+
 @pytest.mark.parametrize("T,k", [(5, 2), (64, 4), (700, 3)])
 @pytest.mark.parametrize("case", ["all one", "none", "last", "reversed", "the same twice"])
 def test_orders_at_the_edges(T, k, case):

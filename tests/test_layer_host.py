@@ -71,15 +71,15 @@ REFUSED = {
                each(ALIGN, C=P + 2, a_scale=P + 2, b_scale=P + 1) + [(ALIGN, dict(c_type=F16, C=P + 1)), (NULL, dict(K=0, lda=0, ldb=0, A=0, B=0, b_scale=0))],
     "gemm_i8_grouped": each(SIZE, T=[-1, BIG], N=[-1, BIG], K=[-1, 131072], E=[-1, 65536]) + each(CONFIG, c_type=[3, 5]) + each(PITCH, lda=15, ldb=15, b_stride=-1, bs_stride=-1, ldc=7) +
                        each(NULL, offsets=0, A=0, B=0, C=0, a_scale=0, b_scale=0) + each(ALIGN, offsets=P + 2, C=P + 1, a_scale=P + 1, b_scale=P + 2),
-    "expert_dispatch": each(SIZE, T=[-1, BIG, BIG // 2], top_k=[-1, BIG], E=[-1, 65536], N=[-1, BIG], blocks=[-1, BIG]) + each(CONFIG, index_type=[2, -1], size=[0, 3, 8]) +
+    "expert_dispatch": each(SIZE, T=[-1, BIG, BIG // 2], top_k=[-1, 65536, BIG], E=[-1, 65536], N=[-1, BIG], blocks=[-1, BIG]) + each(CONFIG, index_type=[2, -1], size=[0, 3, 8]) +
                        each(PITCH, ldx=7, ld_rows=[7, BIG], ld_scale=1999, ld_row_scale=3999) + each(NULL, expert=0, offsets=0, place=0, rows=0, scale=0, row_scale=0, workspace=0) +
                        each(ALIGN, expert=P + 4, offsets=P + 2, source=P + 2, place=P + 2, X=P + 1, rows=P + 1, scale=P + 2, row_scale=P + 2, workspace=P + 8) +
                        [(ALIGN, dict(index_type=0, expert=P + 2)), (ALIGN, dict(size=4, X=P + 2)), (NULL, dict(T=0, offsets=0)), (ALIGN, dict(top_k=0, offsets=P + 1))] +
                        each(WORKSPACE, workspace_bytes=[0, -1, 100]),
-    "expert_combine": each(SIZE, T=[-1, BIG, BIG // 2], top_k=[-1, BIG], N=[-1, BIG]) + each(CONFIG, type=[3, -1], out_type=[BF16, 3]) + [(CONFIG, dict(type=F32, out_type=F16))] +
+    "expert_combine": each(SIZE, T=[-1, BIG, BIG // 2], top_k=[-1, 65536, BIG], N=[-1, BIG]) + each(CONFIG, type=[3, -1], out_type=[BF16, 3]) + [(CONFIG, dict(type=F32, out_type=F16))] +
                       each(PITCH, ldy=7, ld_add=7, ldo=[7, BIG]) + each(NULL, place=0, Y=0, out=0) + each(ALIGN, place=P + 2, Y=P + 1, weight=P + 2, add=P + 1, out=P + 2) +
                       [(ALIGN, dict(type=F32, Y=P + 2))],
-    "expert_combine_grad": each(SIZE, T=[-1, BIG], top_k=[-1, BIG], N=[-1, BIG]) + each(CONFIG, type=[F32, 3]) + each(PITCH, lddo=7, ldy=7, lddy=7) + each(NULL, place=0, dOut=0, Y=0) +
+    "expert_combine_grad": each(SIZE, T=[-1, BIG], top_k=[-1, 65536, BIG], N=[-1, BIG]) + each(CONFIG, type=[F32, 3]) + each(PITCH, lddo=7, ldy=7, lddy=7) + each(NULL, place=0, dOut=0, Y=0) +
                            each(ALIGN, place=P + 2, dOut=P + 1, weight=P + 2, Y=P + 1, dY=P + 1, dweight=P + 2) + [(NULL, dict(N=0, place=0))],
 }
 # nothing to compute: no pointer is looked at
@@ -174,7 +174,8 @@ def test_workspaces():
             assert 8 * N <= w(M, N) <= 8 * N * min(M, 256)
     d = binding.expert_dispatch_workspace_bytes
     assert d(0, 2, 8) == d(2, 0, 8) == d(-1, 2, 8) == d(2**31 - 1, 2, 8) == d(5000, 2, 65536) == d(5000, 2, -1) == 0 == d(32, 2, 16)
-    for T, k in ((5000, 2), (16384, 8), (2**30, 1), (2**31 - 1, 1)):
+    assert d(1, 65536, 8) == 0
+    for T, k in ((5000, 2), (16384, 8), (2**30, 1), (2**31 - 1, 1), (1, 65535), (2000, 256), (2000, 257)):
         for E in (0, 1, 64, 2047, 2048, 65535):
             assert 0 < d(T, k, E) <= 8 * T * k + (1 << 22) and d(T, k, E) % 16 == 0
 
