@@ -529,12 +529,12 @@ __global__ __launch_bounds__(256) void layer_norm_columns_long_kernel(const Laye
     for (int i = 0; i < 8; i++) if (c + i < a.N) { out[i] = dg[i]; out[a.N + i] = db[i]; }
 }
 
-// dgamma[j] and dbeta[j]: sums of `parts` rows of 2 N floats of the workspace, 64 columns a workgroup, wavefront w takes rows w, w + 16, ...
-__global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restrict__ ws, int parts, int N, float* __restrict__ dgamma, float* __restrict__ dbeta)
+// dgamma[j] and dbeta[j]: sums of `parts` rows of 2 N floats of the workspace, from column `first` on, 64 columns a workgroup, wavefront w takes rows w, w + 16, ...
+__global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restrict__ ws, int parts, int N, int64_t first, float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
     __shared__ float lds[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t c = first + (int64_t)blockIdx.x * 64 + lane;
     float* const out = blockIdx.y ? dbeta : dgamma;
     if (!out) return;
     float s = 0.0f;
@@ -550,6 +550,8 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* __restri
         out[c] = s;
     }
 }
+
+constexpr int64_t LAUNCH_COLUMNS = 1 << 27;              // 16 threads each: 2^31 of the 2^32 of a launch
 
 // threads that share a row in the gradient, and rows that a workgroup takes at a time
 inline int grad_rows(int64_t N) { return N <= 64 ? 64 : N <= 128 ? 32 : N <= 512 ? 16 : N <= 1024 ? 8 : N <= 2048 ? 4 : N <= 4096 ? 2 : 1; }
@@ -614,8 +616,12 @@ int norm_grad_of_type(const LayerNormGradArgs& a, hipStream_t stream)
         if (rc != GEMM_F16_OK) return rc;
     }
     if (!columns || (parts == 1 && a.N <= 16384)) return rc;
-    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)(((int64_t)a.N + 63) / 64), 2), dim3(1024), 0, stream, a.ws, parts, a.N, a.dgamma, a.dbeta);
-    return launched();
+    for (int64_t first = 0; first < a.N && rc == GEMM_F16_OK; first += LAUNCH_COLUMNS) {
+        const int64_t left = a.N - first;
+        hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)(((left < LAUNCH_COLUMNS ? left : LAUNCH_COLUMNS) + 63) / 64), 2), dim3(1024), 0, stream, a.ws, parts, a.N, first, a.dgamma, a.dbeta);
+        rc = launched();
+    }
+    return rc;
 }
 
 // ---- rows to 8-bit integers ----------------------------------------------------------------------------------------------------------

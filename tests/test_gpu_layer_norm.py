@@ -325,3 +325,37 @@ def test_more_rows_than_a_launch():
     assert np.array_equal(q2[rows].cpu().numpy(), qw) and np.array_equal(scale2[rows].cpu().numpy(), sw)
     assert bool((scale > 0).all()) and bool((scale2 > 0).all()) and bool((rstd > 0).all())
     assert LEAST[type] > 0
+
+
+def test_rows_beyond_the_range():
+    """Sums that pass f32's range: NaN; squares only: beta.  Neighbouring rows keep their values."""
+    M, N, type = 5, 300, "bf16"
+    rng = np.random.default_rng(4)
+    x = rng.standard_normal((M, N))
+    x[1] = 3e38                                              # the sum
+    x[3] = rng.choice([-1e30, 1e30], N)                      # squares
+    X, G, B = Mat(type, M, N, None, 0, x), Mat(type, 1, N, None, 0, rng.standard_normal((1, N))), Mat(type, 1, N, None, 0, rng.standard_normal((1, N)))
+    Y, Q, S, mean, rstd = Mat(type, M, N), Ints(I8, M, N), Mat("f32", 1, M), Mat("f32", 1, M), Mat("f32", 1, M)
+    assert binding.layer_norm(M, N, TYPE[type], X.ptr, N, None, 0, G.ptr, B.ptr, EPS, None, 0, Y.ptr, N, Q.ptr, N, S.ptr, mean.ptr, rstd.ptr, stream()) == binding.OK
+    torch.cuda.synchronize()
+    y, q, s, r = Y.fetch(), Q.fetch(), S.fetch()[0], rstd.fetch()[0]
+    assert np.isnan(y[1]).all() and np.isnan(s[1]) and (q[1] == 0).all()
+    assert r[3] == 0 and np.array_equal(y[3], B.values()[0]) and np.array_equal(q[3:4], quantized(B.values())[0])
+    rows = [0, 2, 4]
+    _, _, want, off = layer_norm(X.values()[rows], G.values(), B.values(), EPS)
+    assert_within(y[rows], want, rounding(want, off, type), "y")
+
+
+def test_more_columns_than_a_launch():
+    """The columns' sums of one row of more than 2^28, 16 threads a column."""
+    N, type = (1 << 28) + 72, "bf16"
+    h = torch.randint(-3, 4, (N,), dtype=torch.int8, device="cuda").bfloat16()
+    dy = torch.roll(h, 1) + 0.5
+    gamma, dx = torch.ones_like(h), torch.zeros_like(h)
+    mean, rstd = torch.full((1,), 0.25, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    dgamma, dbeta = torch.zeros(N, device="cuda"), torch.zeros(N, device="cuda")
+    need = binding.layer_norm_grad_workspace_bytes(1, N)
+    work = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    binding.check(binding.layer_norm_grad(1, N, TYPE[type], dy, N, h, N, gamma, mean, rstd, None, 0, dx, N, dgamma, dbeta, work, need, stream()))
+    assert torch.equal(dbeta, dy.float()) and torch.equal(dgamma, dy.float() * ((h.float() - 0.25) * 0.5))       # exact: few bits each
+    assert bool(dx.isfinite().all()) and bool((dx[-72:] != 0).any())
