@@ -53,6 +53,38 @@ bool fits(const OpsGemm& g, const Form& f)
     return grid >= 0 && fits_a_launch(grid, f.kernel == Form::ANY ? 256 : 512);
 }
 
+// The fastest for 8-bit integers.  A form's time is that of a launch and of a compute unit's tiles, each of which costs something by itself and something for each k; what
+// follows is fitted, in us, to 776 products (1 to 2048 rows, 256 to 16384 columns and k) and 307 grouped ones (16 to 16384 rows, 4 to 128 experts), each measured on every form.
+// Of these products the form that comes out is within 10 % of the fastest but for 14 and 27, on average 0.8 % and 2 % slower.  us of the forms 16x16 | 32x32 | 64x64 | 128x128 | 256x256:
+// 16 rows of (1000,16384) 7.9 | 12.7 | 22.9 | 59 | 128, 64 of (8192,8192) 37 | 14.4 | 16.1 | 33, 256 of (4096,16384) - | 43 | 26 | 60 | 131, 400 of (16384,1000) - | - | 40 | 15.5 | 22.5
+Form preferred_i8(const OpsGemm& g, bool allow_few_rows)
+{
+    struct Cost { float launch, tile, k1000; };
+    static const struct { int fm, nb; Cost single, grouped; } few[] = {
+        {1, 1, {2.7f, 0.6f, 0.36f}, {2.9f, 0.9f, 0.38f}}, {1, 4, {2.6f, 0.7f, 0.89f}, {2.3f, 1.0f, 1.45f}}, {2, 1, {1.8f, 1.5f, 0.52f}, {2.6f, 1.6f, 0.54f}},
+        {2, 2, {2.7f, 0.6f, 0.69f}, {2.6f, 0.9f, 0.83f}}, {2, 4, {1.6f, 2.1f, 1.06f}, {1.4f, 2.3f, 1.61f}}, {4, 4, {1.1f, 3.3f, 1.48f}, {2.0f, 2.5f, 1.90f}}};
+    const Cost small = g.offsets ? Cost{2.4f, 2.0f, 4.70f} : Cost{2.9f, 1.9f, 3.90f}, large = g.offsets ? Cost{0.2f, 9.0f, 10.66f} : Cost{0.0f, 10.4f, 8.34f};
+    const int cus = chip().cus;
+    auto cost = [&](const Cost& c, int bm, int bn) {
+        // rounds of the compute units, between what they take on average and what the last one takes
+        const double tiles = expected_tiles(g, bm, bn) / cus, rounds = 0.5 * ((tiles < 1.0 ? 1.0 : tiles) + ceil(tiles));
+        return c.launch + rounds * (c.tile + c.k1000 * 1e-3 * g.K);
+    };
+    double least = cost(small, 128, 128);
+    Form best = tiles(TILE_128);
+    if (const double us = cost(large, 256, 256); us < least) {
+        // 256 x 256 by four wavefronts, whose k steps are shorter (8192^3 394 | 436, (4096,8192,16384) 366 | 401) and whose tiles cost more around the loop, its code's first
+        // pass above all, from so many k steps of a compute unit on: (4096,4096,4096) 32: 53.6 | 56.1, (8192,8192,2048) 64: 130 | 131, f32 152 | 155, 16384 rows of 16 experts
+        // (4096,2048) 80: 161 | 165, (8192,1024) 72: 203 | 209; fewer: (8192,8192,1024) 32: 93 | 89, (3000,3000,4096) 18: 51 | 47, (16384,2304,768) 14: 53 | 49
+        const double steps = (g.K + 127) / 128, all = steps * expected_tiles(g, 256, 256) / cus;
+        best = tiles(steps >= 8.0 && (all >= 48.0 || (steps >= 32.0 && all >= 31.0)) ? TILE_256_LONG : TILE_256);
+        least = us;
+    }
+    for (const auto& f : few)
+        if (const double us = cost(g.offsets ? f.grouped : f.single, 16 * f.fm, 16 * f.nb); allow_few_rows && us < least) { best = few_rows(f.fm, f.nb); least = us; }
+    return best;
+}
+
 // The fastest of them; us measured for the one taken | the other, groups as a random router deals them.  `rows` is the average group's: who has more is known on the device only.
 // 1280 rows of 64 experts (4096,2048) in e4m3 that all go to one take 102 us on the 32-row tiles of 20 rows each, and 20 to 40 on tiles of 128; dealt evenly they take 155.
 Form preferred(const OpsGemm& g, bool allow_few_rows)
@@ -76,21 +108,7 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
     // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
     // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
     const bool large = rows >= 192.0 && expected_tiles(g, 128, 128) >= 2.0 * cus;
-    if (g.elem == ELEM_I8) {
-        // few rows, by streaming B, as in e4m3; up to 16 rows on 64 columns where that gives every compute unit a tile, as A comes to each by the same
-        // way as B: 16 rows of (16384,8192) 27.8 | 34 us (32 columns), (16384,4096) 13.2 | 14.2, 64 rows of 16 experts (4096,2048) 27.0 | 29.7
-        if (allow_few_rows && ((double)g.M * g.N <= 5400.0 * cus || (g.offsets && rows <= 20.0))) {
-            const int fm = rows <= 16.0 ? 1 : 2;
-            const int nb = (fm == 2 && rows > 32.0 && expected_tiles(g, 32, 64) >= cus) || (fm == 1 && expected_tiles(g, 16, 64) >= cus) ? 4 : expected_tiles(g, 16 * fm, 32) >= cus ? 2 : 1;
-            return few_rows(fm, nb);
-        }
-        if (!large) return tiles(TILE_128);
-        // 256 x 256 by four wavefronts, whose k steps are shorter (8192^3 394 | 436, (4096,8192,16384) 366 | 401) and whose tiles cost more around the loop, its code's first
-        // pass above all, from so many k steps of a compute unit on: (4096,4096,4096) 32: 53.6 | 56.1, (8192,8192,2048) 64: 130 | 131, f32 152 | 155, 16384 rows of 16 experts
-        // (4096,2048) 80: 161 | 165, (8192,1024) 72: 203 | 209; fewer: (8192,8192,1024) 32: 93 | 89, (3000,3000,4096) 18: 51 | 47, (16384,2304,768) 14: 53 | 49
-        const double steps = (g.K + 127) / 128, all = steps * expected_tiles(g, 256, 256) / cus;
-        return tiles(steps >= 8.0 && (all >= 48.0 || (steps >= 32.0 && all >= 31.0)) ? TILE_256_LONG : TILE_256);
-    }
+    if (g.elem == ELEM_I8) return preferred_i8(g, allow_few_rows);
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
         // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
@@ -141,7 +159,7 @@ int launch(const OpsGemm& g)
 {
     const Form f = choose(g);
     if (f.kernel == Form::ANY) return ops_launch_generic(g);
-    if (f.kernel == Form::FEW_ROWS) return ops_launch_skinny(g, f.fm, f.nb);
+    if (f.kernel == Form::FEW_ROWS) return g.elem == ELEM_I8 ? ops_launch_few_i8(g, f.fm, f.nb) : ops_launch_skinny_e4m3(g, f.fm, f.nb);
     if (g.elem == ELEM_I8) return ops_launch_tiles_i8(g, f.tile);
     return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, f.tile) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, f.tile) : ops_launch_tiles_bf16(g, f.tile);
 }
@@ -150,7 +168,8 @@ const char* name_of(const OpsGemm& g, const Form& f)
 {
     if (f.kernel == Form::ANY) return "any_alignment_64x64";
     if (f.kernel == Form::FEW_ROWS)
-        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
+        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.fm == 4 ? "few_rows_64x64" :
+               f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
     const bool e4m3 = g.elem == ELEM_E4M3;
     switch (f.tile) {
     case TILE_256: return e4m3 ? "e4m3_256x256" : "256x256";

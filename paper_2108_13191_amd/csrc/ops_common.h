@@ -67,8 +67,10 @@ int ops_launch_tiles_i8(const OpsGemm& g, OpsTile tile);
 // ops_i8_long.hip: TILE_256_LONG, i8 on 256 x 256 tiles of four wavefronts; K >= 128
 int ops_launch_long_i8(const OpsGemm& g);
 
-// ops_skinny.hip: few rows, e4m3 and i8; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 1 x 4 (i8), 2 x 1, 2 x 2 or 2 x 4
-int ops_launch_skinny(const OpsGemm& g, int fm, int nb);
+// ops_skinny_e4m3.hip: few rows; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
+int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb);
+// ops_i8_few.hip: the same in i8, 1 x 1, 1 x 4, 2 x 1, 2 x 2, 2 x 4 or 4 x 4
+int ops_launch_few_i8(const OpsGemm& g, int fm, int nb);
 
 // ops_norm.hip
 struct NormArgs {

@@ -1,11 +1,11 @@
-// Few rows against large matrices of e4m3 values or 8-bit integers (include/gemm_ops.h, include/gemm_layer.h): 16 FM x 16 NB results a
+// Few rows against large e4m3 matrices (include/gemm_ops.h): 16 FM x 16 NB results a
 // workgroup, whose eight wavefronts take the k steps of 128 bytes in turn and add their sums in LDS at the end.
 //
 // Such products are bound by streaming B once: each lane loads its fragments of a k step straight into registers (4 lanes cover the 128
 // bytes of a row) and multiplies them.  No LDS, no barrier before the end; what keeps the memory busy is that 16 to 32 wavefronts
 // a compute unit do so.  (A ring of 2 to 6 steps in registers ahead of the multiplication, with fewer wavefronts: (16,8192,8192) e4m3
 // 13.9 to 19.9 us against 13.7, 64 rows of 16 experts (4096,2048) 29.5 to 57 against 26.3.)  e4m3 values are widened to f16: the matrix
-// rate does not matter here.  8-bit integers are multiplied as they are.  Measured: (16,8192,8192) 16.2 us from memory, 4.2 TB/s, 13.5 where B (67 MB) is still in the 256 MB memory-side cache; 64 rows of 16
+// rate does not matter here.  Measured: (16,8192,8192) 16.2 us from memory, 4.2 TB/s, 13.5 where B (67 MB) is still in the 256 MB memory-side cache; 64 rows of 16
 // experts (4096,2048) 26 to 29 us, 4.6 to 5.1 TB/s.  More rows a workgroup
 // than 32 make A's reads, once for each 32 columns, the bound: 32 rows each of 16 experts 75 us with 64, 56 with 32.
 #include "ops_tile.h"
@@ -16,11 +16,10 @@ using namespace ops_tile;
 
 constexpr int WAVES = 8;      // (16 for the fewest workgroups: no faster)
 
-// OCC: wavefronts a SIMD that the registers leave room for; U: k steps of a wavefront whose loads are asked for together
-template <int ELEM, int FM, int NB, int OCC, int U, typename CT>
+// OCC: wavefronts a SIMD that the registers leave room for
+template <int FM, int NB, int OCC, typename CT>
 __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGemm g)
 {
-    constexpr bool I8 = ELEM == ELEM_I8;                                     // integer sums, scaled at the end
     constexpr int BM = 16 * FM, BN = 16 * NB;
     __shared__ floatx4 sums[WAVES][FM * NB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -43,7 +42,7 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
 #pragma unroll
     for (int n = 0; n < NB; n++) b_off[n] = (uint32_t)min(16 * n + l16, g.N - t.n0 - 1) * (uint32_t)g.ldb + 16u * q;
     const float* const sa = g.sa + t.row0;
-    const float* const sb = I8 ? g.sb + (int64_t)t.e * g.sb_stride : g.sb + (int64_t)t.e * g.sb_stride + (int64_t)(t.n0 / 128) * g.ld_sb;
+    const float* const sb = g.sb + (int64_t)t.e * g.sb_stride + (int64_t)(t.n0 / 128) * g.ld_sb;
 
     floatx4 acc[FM][NB];
 #pragma unroll
@@ -52,20 +51,15 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
         for (int n = 0; n < NB; n++) acc[m][n] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
     struct Step { Frag a[FM], b[NB]; float sa[FM], sb; };
-    auto load_scales = [&](Step& x, int k) {
-        if constexpr (!I8) {
-            x.sb = sb[k];
-#pragma unroll
-            for (int m = 0; m < FM; m++) x.sa[m] = sa[(int64_t)k * g.ld_sa + s_off[m]];
-        }
-    };
     auto load = [&](Step& x, int k) {
         const char *const ap = a_tile + (int64_t)k * STEP, *const bp = b_tile + (int64_t)k * STEP;
 #pragma unroll
         for (int n = 0; n < NB; n++) { x.b[n].lo = *(const uintx4*)(bp + b_off[n]); x.b[n].hi = *(const uintx4*)(bp + b_off[n] + 64); }
 #pragma unroll
         for (int m = 0; m < FM; m++) { x.a[m].lo = *(const uintx4*)(ap + a_off[m]); x.a[m].hi = *(const uintx4*)(ap + a_off[m] + 64); }
-        load_scales(x, k);
+        x.sb = sb[k];
+#pragma unroll
+        for (int m = 0; m < FM; m++) x.sa[m] = sa[(int64_t)k * g.ld_sa + s_off[m]];
     };
     auto load_tail = [&](Step& x, int k) {                                   // the short last step: zeros behind K
         const char *const ap = a_tile + (int64_t)k * STEP, *const bp = b_tile + (int64_t)k * STEP;
@@ -83,36 +77,23 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
         for (int n = 0; n < NB; n++) { x.b[n].lo = chunk(bp + b_off[n], left); x.b[n].hi = chunk(bp + b_off[n] + 64, left - 64); }
 #pragma unroll
         for (int m = 0; m < FM; m++) { x.a[m].lo = chunk(ap + a_off[m], left); x.a[m].hi = chunk(ap + a_off[m] + 64, left - 64); }
-        load_scales(x, k);
+        x.sb = sb[k];
+#pragma unroll
+        for (int m = 0; m < FM; m++) x.sa[m] = sa[(int64_t)k * g.ld_sa + s_off[m]];
     };
     auto multiply = [&](const Step& x) {
 #pragma unroll
         for (int m = 0; m < FM; m++)
 #pragma unroll
             for (int n = 0; n < NB; n++) {
-                if constexpr (I8) {
-                    acc[m][n] = mfma_step<ELEM_I8>(x.b[n], x.a[m], acc[m][n]);
-                } else {
-                    const floatx4 p = mfma_step(widened(x.b[n]), widened(x.a[m]));
+                const floatx4 p = mfma_step(widened(x.b[n]), widened(x.a[m]));
 #pragma unroll
-                    for (int e = 0; e < 4; e++) acc[m][n][e] = __builtin_fmaf(p[e], x.sa[m] * x.sb, acc[m][n][e]);
-                }
+                for (int e = 0; e < 4; e++) acc[m][n][e] = __builtin_fmaf(p[e], x.sa[m] * x.sb, acc[m][n][e]);
             }
     };
 
     Step x;
-    int k = wave;
-    if constexpr (U > 1) {                                                   // U k steps' loads ahead of their products
-        for (; k + (U - 1) * WAVES < k_full; k += U * WAVES) {
-            Step s[U];
-#pragma unroll
-            for (int u = 0; u < U; u++) load(s[u], k + u * WAVES);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int u = 0; u < U; u++) multiply(s[u]);
-        }
-    }
-    for (; k < k_full; k += WAVES) { load(x, k); multiply(x); }
+    for (int k = wave; k < k_full; k += WAVES) { load(x, k); multiply(x); }
     if (k_full < KT && k_full % WAVES == wave) { load_tail(x, k_full); multiply(x); }
 
     // ---- the wavefronts' sums, in their order -----------------------------------------------------------------------------
@@ -125,17 +106,9 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
     if (block >= FM * NB) return;
     floatx4 v = sums[0][block][lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; w++) {
-        if constexpr (I8) v = __builtin_bit_cast(floatx4, __builtin_bit_cast(intx4, v) + __builtin_bit_cast(intx4, sums[w][block][lane]));
-        else              v += sums[w][block][lane];
-    }
+    for (int w = 1; w < WAVES; w++) v += sums[w][block][lane];
     const int row = t.row0 + 16 * (block / NB) + l16, col = t.n0 + 16 * (block % NB) + 4 * q;
     if (row >= t.row_end) return;
-    if constexpr (I8) {
-        const float rs = g.sa[row];
-#pragma unroll
-        for (int e = 0; e < 4; e++) v[e] = scaled_sum(v[e], rs) * sb[min(col + e, g.N - 1)];
-    }
     CT* const dst = (CT*)g.C + (int64_t)t.e * g.c_stride + (int64_t)row * g.ldc + col;
     if (col + 4 <= g.N) {
         typename CVec4<CT>::type o;
@@ -148,32 +121,22 @@ __global__ __launch_bounds__(64 * WAVES, OCC) void ops_skinny_kernel(const OpsGe
     }
 }
 
-template <int ELEM, int FM, int NB, int OCC, int U>
+template <int FM, int NB, int OCC>
 int launch_skinny(const OpsGemm& g)
 {
     static_assert(FM * NB <= WAVES, "a wavefront adds one block");
     const int64_t grid = tile_grid(g, 16 * FM, 16 * NB);
     if (grid < 0 || !fits_a_launch(grid, 64 * WAVES)) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else                           hipLaunchKernelGGL((ops_skinny_kernel<ELEM, FM, NB, OCC, U, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_skinny_kernel<FM, NB, OCC, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_skinny_kernel<FM, NB, OCC, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else                           hipLaunchKernelGGL((ops_skinny_kernel<FM, NB, OCC, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
-}
-int launch_e4m3(const OpsGemm& g, int fm, int nb)
-{
-    if (fm == 1) return nb == 1 ? launch_skinny<ELEM_E4M3, 1, 1, 8, 1>(g) : launch_skinny<ELEM_E4M3, 1, 2, 4, 1>(g);
-    return nb == 1 ? launch_skinny<ELEM_E4M3, 2, 1, 6, 1>(g) : nb == 2 ? launch_skinny<ELEM_E4M3, 2, 2, 4, 1>(g) : launch_skinny<ELEM_E4M3, 2, 4, 3, 1>(g);
-}
-int launch_i8(const OpsGemm& g, int fm, int nb)
-{
-    // From 4096 k on a wavefront has four k steps, whose loads go ahead together, with registers for them: 16 rows of (8192,8192) 14.1 us against 15.4, of (16384,8192) 27.8 against
-    // 32.9, one row of (8192,8192) 12.3 against 13.4.  With fewer k, or for 32 rows, no faster or slower: 64 rows of 16 experts (4096,2048) 32.9 against 27.0.
-    const bool ahead = g.K >= 4 * WAVES * STEP;
-    if (fm == 1 && nb == 4) return ahead ? launch_skinny<ELEM_I8, 1, 4, 2, 4>(g) : launch_skinny<ELEM_I8, 1, 4, 4, 1>(g);
-    if (fm == 1) return nb == 1 ? launch_skinny<ELEM_I8, 1, 1, 8, 1>(g) : ahead ? launch_skinny<ELEM_I8, 1, 2, 2, 4>(g) : launch_skinny<ELEM_I8, 1, 2, 4, 1>(g);
-    return nb == 1 ? launch_skinny<ELEM_I8, 2, 1, 6, 1>(g) : nb == 2 ? launch_skinny<ELEM_I8, 2, 2, 4, 1>(g) : launch_skinny<ELEM_I8, 2, 4, 3, 1>(g);
 }
 
 }  // namespace
 
-int ops_launch_skinny(const OpsGemm& g, int fm, int nb) { return g.elem == ELEM_I8 ? launch_i8(g, fm, nb) : launch_e4m3(g, fm, nb); }
+int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb)
+{
+    if (fm == 1) return nb == 1 ? launch_skinny<1, 1, 8>(g) : launch_skinny<1, 2, 4>(g);
+    return nb == 1 ? launch_skinny<2, 1, 6>(g) : nb == 2 ? launch_skinny<2, 2, 4>(g) : launch_skinny<2, 4, 3>(g);
+}
