@@ -55,14 +55,15 @@ bool fits(const OpsGemm& g, const Form& f)
 
 // The fastest for 8-bit integers.  A form's time is that of a launch and of a compute unit's tiles, each of which costs something by itself and something for each k; what
 // follows is fitted, in us, to 776 products (1 to 2048 rows, 256 to 16384 columns and k) and 307 grouped ones (16 to 16384 rows, 4 to 128 experts), each measured on every form.
-// Of these products the form that comes out is within 10 % of the fastest but for 14 and 27, on average 0.8 % and 2 % slower.  us of the forms 16x16 | 32x32 | 64x64 | 128x128 | 256x256:
+// Of these products the form that comes out is within 10 % of the fastest but for 6 and 25, on average 0.8 % and 2 % slower.  us of the forms 16x16 | 32x32 | 64x64 | 128x128 | 256x256:
 // 16 rows of (1000,16384) 7.9 | 12.7 | 22.9 | 59 | 128, 64 of (8192,8192) 37 | 14.4 | 16.1 | 33, 256 of (4096,16384) - | 43 | 26 | 60 | 131, 400 of (16384,1000) - | - | 40 | 15.5 | 22.5
 Form preferred_i8(const OpsGemm& g, bool allow_few_rows)
 {
     struct Cost { float launch, tile, k1000; };
     static const struct { int fm, nb; Cost single, grouped; } few[] = {
         {1, 1, {2.7f, 0.6f, 0.36f}, {2.9f, 0.9f, 0.38f}}, {1, 4, {2.6f, 0.7f, 0.89f}, {2.3f, 1.0f, 1.45f}}, {2, 1, {1.8f, 1.5f, 0.52f}, {2.6f, 1.6f, 0.54f}},
-        {2, 2, {2.7f, 0.6f, 0.69f}, {2.6f, 0.9f, 0.83f}}, {2, 4, {1.6f, 2.1f, 1.06f}, {1.4f, 2.3f, 1.61f}}, {4, 4, {1.1f, 3.3f, 1.48f}, {2.0f, 2.5f, 1.90f}}};
+        {2, 2, {2.7f, 0.6f, 0.69f}, {2.6f, 0.9f, 0.83f}}, {2, 4, {1.6f, 2.1f, 1.06f}, {1.4f, 2.3f, 1.61f}}, {4, 4, {1.1f, 3.3f, 1.48f}, {2.0f, 2.5f, 1.90f}},
+        {8, 4, {0.3f, 5.6f, 2.39f}, {1.5f, 7.0f, 2.20f}}};
     const Cost small = g.offsets ? Cost{2.4f, 2.0f, 4.70f} : Cost{2.9f, 1.9f, 3.90f}, large = g.offsets ? Cost{0.2f, 9.0f, 10.66f} : Cost{0.0f, 10.4f, 8.34f};
     const int cus = chip().cus;
     auto cost = [&](const Cost& c, int bm, int bn) {
@@ -168,7 +169,7 @@ const char* name_of(const OpsGemm& g, const Form& f)
 {
     if (f.kernel == Form::ANY) return "any_alignment_64x64";
     if (f.kernel == Form::FEW_ROWS)
-        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.fm == 4 ? "few_rows_64x64" :
+        return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.fm == 8 ? "few_rows_128x64" : f.fm == 4 ? "few_rows_64x64" :
                f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";
     const bool e4m3 = g.elem == ELEM_E4M3;
     switch (f.tile) {

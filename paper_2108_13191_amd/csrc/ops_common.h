@@ -69,7 +69,7 @@ int ops_launch_long_i8(const OpsGemm& g);
 
 // ops_skinny_e4m3.hip: few rows; fm x nb: 16 x 16 blocks of a workgroup's tile, 1 x 1, 1 x 2, 2 x 1, 2 x 2 or 2 x 4
 int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb);
-// ops_i8_few.hip: the same in i8, 1 x 1, 1 x 4, 2 x 1, 2 x 2, 2 x 4 or 4 x 4
+// ops_i8_few.hip: the same in i8, 1 x 1, 1 x 4, 2 x 1, 2 x 2, 2 x 4, 4 x 4 or 8 x 4
 int ops_launch_few_i8(const OpsGemm& g, int fm, int nb);
 
 // ops_norm.hip

@@ -1,26 +1,25 @@
 // Products of 8-bit integers (include/gemm_layer.h) whose tiles of 128 x 128 would leave compute units idle: 16 FM x 16 NB results a workgroup, whose wavefronts take the k steps
-// of 128 bytes in turn, each through two stages of its own in LDS, and add their sums there at the end.  No barrier before that.
+// of 128 bytes in turn, each through S stages of its own in LDS, and add their sums there at the end.  No barrier before that.
 //
 // Bound by what a compute unit loads, (FM + NB) * 16 rows of K bytes a tile.  Loaded straight into registers, as fragments have them, neighbouring lanes read different rows, and a
 // load of 1 KB takes the 64 cycles of 64 requests: 16 bytes a cycle whatever is asked for ahead (16 to 64 k steps).  Copied to LDS eight lanes read one row's 128 bytes, and
 // fragments come from there: twice to three times that.  us, here | by registers: (16,8192,8192) 12.2 | 14.4, (16,1000,16384) 7.9 | 16.8, (64,8192,8192) 14.0 | 25.5 (from memory 13.5),
-// (256,4096,16384) 26 | 88, (700,1000,16384) 25 | 88, (300,300,300) 3.2 | 3.2.  Tried: three and four stages, twice or half the wavefronts, 64 x 128 and 32 x 128 tiles: no
-// faster, but for 100 to 200 rows of (16384,8192), 64 x 128, three wavefronts, 38 | 47.
+// (256,4096,16384) 26 | 88, (700,1000,16384) 25 | 88, (300,300,300) 3.2 | 3.2.  128 x 64 in one stage, as a wavefront's products (64 MFMAs) are as long as the copies of its next
+// step: (400,4096,16384) 42 us, 64 x 64 in two rounds 48, 128 x 128 of the tiled kernel 60.  Tried: three and four stages, twice or half the wavefronts, 32 x 128, 64 x 128 and 128 x 128 tiles: no faster.
 #include "ops_tile.h"
 
 namespace {
 
 using namespace ops_tile;
 
-constexpr int S = 2;                                       // stages of a wavefront
-
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
-template <int FM, int NB, int WAVES, typename CT>
+template <int FM, int NB, int WAVES, int S, typename CT>
 __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
 {
     constexpr int BM = 16 * FM, BN = 16 * NB, COPIES = 2 * (FM + NB), STAGE = COPIES * 1024, RING = S * STAGE;
-    static_assert(FM * NB * 1024 <= RING && WAVES * RING <= 160 * 1024 && S == 2);
+    constexpr int PASS = FM * NB * 1024 <= RING ? FM * NB : FM * NB / 2;       // blocks of sums that a ring holds
+    static_assert(PASS * 1024 <= RING && FM * NB % PASS == 0 && WAVES * RING <= 160 * 1024 && (S == 1 || S == 2));
     __shared__ __attribute__((aligned(1024))) char smem[WAVES * RING];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q = lane >> 4;
@@ -66,11 +65,11 @@ __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
         for (int n = 0; n < NB; n++) { b[n].lo = get(stage + (FM + n) * 2048 + rd0); b[n].hi = get(stage + (FM + n) * 2048 + rd1); }
     };
 
-    uint32_t stage = ring, other = ring + STAGE;
+    uint32_t stage = ring, other = ring + (S - 1) * STAGE;
     if (wave < k_full) copy(wave, stage);
-    if (wave + WAVES < k_full) copy(wave + WAVES, other);
+    if (S > 1 && wave + WAVES < k_full) copy(wave + WAVES, other);
     for (int k = wave; k < k_full; k += WAVES) {
-        if (k + WAVES < k_full) wait_copies<COPIES>();                        // the next step's may be on their way
+        if (S > 1 && k + WAVES < k_full) wait_copies<COPIES>();                        // the next step's may be on their way
         else                    wait_copies<0>();
         read(stage);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // before the stage is written again
@@ -101,43 +100,47 @@ __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
     // ---- the wavefronts' sums: each into its ring, then each adds some of the 16 x 16 blocks -----------------------------------
     auto sums = [&](int w, int block) { return (__attribute__((address_space(3))) floatx4*)(uintptr_t)(smem_base + w * RING + block * 1024 + 16 * lane); };
 #pragma unroll
-    for (int m = 0; m < FM; m++)
+    for (int p0 = 0; p0 < FM * NB; p0 += PASS) {
+        if (p0) __syncthreads();
 #pragma unroll
-        for (int n = 0; n < NB; n++) *sums(wave, m * NB + n) = acc[m][n];
-    __syncthreads();
+        for (int i = 0; i < PASS; i++) *sums(wave, i) = acc[(p0 + i) / NB][(p0 + i) % NB];
+        __syncthreads();
 #pragma unroll
-    for (int block = wave; block < FM * NB; block += WAVES) {
-        intx4 sum = __builtin_bit_cast(intx4, *sums(0, block));
+        for (int i = 0; i < PASS; i += WAVES) {
+            const int block = p0 + i + wave;
+            if (i + wave >= PASS) break;
+            intx4 sum = __builtin_bit_cast(intx4, *sums(0, i + wave));
 #pragma unroll
-        for (int w = 1; w < WAVES; w++) sum += __builtin_bit_cast(intx4, *sums(w, block));
-        const int row = t.row0 + 16 * (block / NB) + l16, col = t.n0 + 16 * (block % NB) + 4 * q;
-        if (row >= t.row_end) continue;
-        const float rs = g.sa[row];
-        const float* const cs = g.sb + (int64_t)t.e * g.sb_stride;
-        floatx4 v;
+            for (int w = 1; w < WAVES; w++) sum += __builtin_bit_cast(intx4, *sums(w, i + wave));
+            const int row = t.row0 + 16 * (block / NB) + l16, col = t.n0 + 16 * (block % NB) + 4 * q;
+            if (row >= t.row_end) continue;
+            const float rs = g.sa[row];
+            const float* const cs = g.sb + (int64_t)t.e * g.sb_stride;
+            floatx4 v;
 #pragma unroll
-        for (int e = 0; e < 4; e++) v[e] = (float)sum[e] * rs * cs[min(col + e, g.N - 1)];
-        CT* const dst = (CT*)g.C + (int64_t)row * g.ldc + col;
-        if (col + 4 <= g.N) {
-            typename CVec4<CT>::type o;
+            for (int e = 0; e < 4; e++) v[e] = (float)sum[e] * rs * cs[min(col + e, g.N - 1)];
+            CT* const dst = (CT*)g.C + (int64_t)row * g.ldc + col;
+            if (col + 4 <= g.N) {
+                typename CVec4<CT>::type o;
 #pragma unroll
-            for (int e = 0; e < 4; e++) o[e] = (CT)v[e];
-            *(typename CVec4<CT>::type*)dst = o;
-        } else {
+                for (int e = 0; e < 4; e++) o[e] = (CT)v[e];
+                *(typename CVec4<CT>::type*)dst = o;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++) if (col + e < g.N) dst[e] = (CT)v[e];
+                for (int e = 0; e < 4; e++) if (col + e < g.N) dst[e] = (CT)v[e];
+            }
         }
     }
 }
 
-template <int FM, int NB, int WAVES>
+template <int FM, int NB, int WAVES, int S = 2>
 int launch_few(const OpsGemm& g)
 {
     const int64_t grid = tile_grid(g, 16 * FM, 16 * NB);
     if (grid < 0 || !fits_a_launch(grid, 64 * WAVES)) return GEMM_F16_ERR_SIZE;
-    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
-    else                           hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    if (g.c_type == ELEM_F32)      hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, S, float>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else if (g.c_type == ELEM_F16) hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, S, half_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
+    else                           hipLaunchKernelGGL((ops_i8_few_kernel<FM, NB, WAVES, S, bf16_t>), dim3((unsigned)grid), dim3(64 * WAVES), 0, g.stream, g);
     return hipGetLastError() == hipSuccess ? GEMM_F16_OK : GEMM_F16_ERR_LAUNCH;
 }
 
@@ -147,5 +150,5 @@ int ops_launch_few_i8(const OpsGemm& g, int fm, int nb)
 {
     if (fm == 1) return nb == 1 ? launch_few<1, 1, 8>(g) : launch_few<1, 4, 4>(g);
     if (fm == 2) return nb == 1 ? launch_few<2, 1, 8>(g) : nb == 2 ? launch_few<2, 2, 4>(g) : launch_few<2, 4, 4>(g);
-    return launch_few<4, 4, 4>(g);
+    return fm == 4 ? launch_few<4, 4, 4>(g) : launch_few<8, 4, 4, 1>(g);
 }
