@@ -13,5 +13,5 @@ FORMS = [("few_rows_16x16", 5, 1000, 300), ("few_rows_16x16", 16, 700, 9001), ("
          ("128x128", 300, 9000, 390), ("128x128", 2500, 3000, 1170), ("256x256", 4000, 6000, 700), ("256x256", 2500, 6000, 130), ("256x256_long", 4093, 4091, 4099), ("256x256_long", 4096, 5000, 4096)]
 # form, rows of each expert, N, K
 GROUPED = [("few_rows_16x16", [3, 0, 5, 1], 500, 9000), ("few_rows_16x64", [3, 0, 5, 1], 500, 260), ("few_rows_16x64", [18] * 30, 520, 150), ("few_rows_32x32", [20, 17, 19, 20], 1000, 2200),
-           ("few_rows_32x32", [1, 119], 1000, 3000), ("few_rows_64x64", [299, 0, 1], 2000, 1300), ("few_rows_32x64", [259, 1], 1500, 2100), ("few_rows_128x64", [500, 0, 100, 99, 1], 1400, 1200), ("few_rows_128x64", [100, 399, 1], 2500, 5003), ("128x128", [100, 0, 333, 20, 150], 2500, 400),
+           ("few_rows_32x32", [1, 119], 1000, 3000), ("few_rows_64x64", [299, 0, 1], 2000, 1300), ("few_rows_32x64", [259, 1], 1500, 2100), ("few_rows_64x64", [500, 0, 100, 99, 1], 1400, 1200), ("few_rows_128x64", [100, 399, 1], 2500, 5003), ("128x128", [100, 0, 333, 20, 150], 2500, 400),
            ("256x256", [3000, 300, 6100, 7], 4300, 260), ("256x256_long", [4000, 0, 300, 8100, 7], 2300, 4500)]
