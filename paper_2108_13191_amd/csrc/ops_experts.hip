@@ -125,6 +125,90 @@ __global__ __launch_bounds__(256) void dispatch_few_kernel(const DispatchArgs a,
     }
 }
 
+// sums of all lanes up to and with this one: within rows of 16 lanes, then the last lane of a row to the next, then of the first two rows to the others
+__device__ __forceinline__ int scan64(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// ---- some choices: still one launch ----------------------------------------------------------------------------------------------------
+// Every workgroup counts all choices in LDS, those in front of its tokens' by themselves, so that a choice's row is what lies before its expert, what of its expert lies in front, and
+// the equal ones of its own 64.  `tokens` tokens a workgroup, 64 choices at most.
+__global__ __launch_bounds__(256) void dispatch_some_kernel(const DispatchArgs a, int tokens, int64_t pieces)
+{
+    extern __shared__ int counts[];                        // [expert]: in front, then the others
+    __shared__ int wave_sums[2][4], places[64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), bins = a.E + 1, n = (int)a.T * a.top_k;
+    const int t0 = (int)blockIdx.x * tokens, own = min((int)a.T - t0, tokens), first = t0 * a.top_k, mine = own * a.top_k;
+    const int64_t bytes = (int64_t)a.N * a.size;
+    // pieces of rows, a wavefront each; where those are few `shared` wavefronts take a piece, each to some of its places
+    const int rows = own * (int)pieces, shared = rows >= 4 ? 1 : rows >= 2 ? 2 : 4, items = rows * shared;
+    RowPiece row;
+    auto load = [&](int item) { row.load((const char*)a.X + (t0 + item / shared / (int)pieces) * a.ldx * a.size, item / shared % (int)pieces * PIECE, bytes); };
+    if (a.X && wave < items) load(wave);                   // the first while choices are counted
+    for (int b = threadIdx.x; b < 2 * bins; b += 256) counts[b] = 0;
+    __syncthreads();
+    constexpr int U = 4;
+    for (int i0 = threadIdx.x; i0 < n; i0 += 256 * U) {
+        int key[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) key[u] = i0 + 256 * u < n ? key_of(a, i0 + 256 * u) : -1;
+#pragma unroll
+        for (int u = 0; u < U; u++) if (key[u] >= 0) atomicAdd(&counts[key[u] + (i0 + 256 * u < first ? 0 : bins)], 1);
+    }
+    __syncthreads();
+    // where each expert begins, and the part's choices of it
+    int run = 0;
+    for (int b0 = 0, slot = 0; b0 < bins; b0 += 256, slot ^= 1) {
+        const int b = b0 + threadIdx.x, front = b < bins ? counts[b] : 0, sum = b < bins ? front + counts[bins + b] : 0, incl = scan64(sum);
+        if (lane == 63) wave_sums[slot][wave] = incl;
+        __syncthreads();
+        int before = run;
+        for (int w = 0; w < 4; w++) { const int s = wave_sums[slot][w]; before += w < wave ? s : 0; run += s; }
+        if (b < bins) {
+            counts[b] = before + incl - sum + front;
+            if (blockIdx.x == 0) a.offsets[b] = before + incl - sum;
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        const int key = lane < mine ? key_of(a, first + lane) : a.E + 1;
+        uint64_t same = mine < 64 ? (1ull << mine) - 1 : ~0ull;
+        const int bits = 32 - __builtin_clz(a.E | 1);
+        for (int b = 0; b < bits; b++) {
+            const bool set = (key >> b) & 1;
+            const uint64_t m = __ballot(set);
+            same &= set ? m : ~m;
+        }
+        if (lane < mine) {
+            const int at = counts[key] + __popcll(same & ((1ull << lane) - 1));
+            places[lane] = key < a.E ? at : -1;
+            a.place[first + lane] = key < a.E ? at : -1;
+            if (a.source) a.source[at] = key < a.E ? t0 + lane / a.top_k : -1;
+        }
+    }
+    if (!a.X) return;
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < mine * a.blocks; i += 256) {
+        const int c = (int)(i % mine), at = places[c];
+        if (at >= 0) a.row_scale[i / mine * a.ld_row_scale + at] = a.scale[i / mine * a.ld_scale + t0 + c / a.top_k];
+    }
+    for (int item = wave; item < items; item += 4) {
+        if (item != wave) load(item);
+        const int at = places[item / shared / (int)pieces * a.top_k + min(lane, a.top_k - 1)];
+        for (int j = item % shared; j < a.top_k; j += shared) {
+            const int place = __builtin_amdgcn_readlane(at, j);
+            if (place >= 0) row.store((char*)a.rows + (int64_t)place * a.ld_rows * a.size, bytes);
+        }
+    }
+}
+
 // ---- more choices or experts: counting sorts by two digits ------------------------------------------------------------------------------------
 // `parts` workgroups of part_rows choices each count their digits; a second launch makes of each digit's counts the sums of those before;
 // a third one finds each choice's place.  The choices are sorted by the experts' low 8 bits and then by the rest.
@@ -147,18 +231,6 @@ __global__ __launch_bounds__(256) void sort_count_kernel(const SortPass s)
     for (int64_t i = first + threadIdx.x; i < end; i += 256) atomicAdd(&hist[digit_of(s, key_of(s.a, s.seq ? s.seq[i] : i))], 1);
     __syncthreads();
     for (int b = threadIdx.x; b < s.bins; b += 256) s.counts[(int64_t)b * s.parts + blockIdx.x] = hist[b];
-}
-
-// sums of all lanes up to and with this one: within rows of 16 lanes, then the last lane of a row to the next, then of the first two rows to the others
-__device__ __forceinline__ int scan64(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
 }
 
 // a workgroup for each digit
@@ -394,6 +466,11 @@ constexpr int MOST_PARTS = 256;
 // bytes of a row that is copied by part: 20000 tokens to 8 of 64, rows of 128 bytes 16.9 us, by token 31.5; of 256 20.6 | 31.9; of 512 38.9 | 35.1
 constexpr int64_t NARROW = 256;
 constexpr int64_t SOME = 1 << 19;                          // choices that are placed by part
+// Choices that every workgroup counts, us | a wavefront for each choice's comparisons up to 1024, or three launches; calls in a row, in a graph: 32 tokens to 2 of 16 experts, rows of 2048 bytes 5.2, 3.9 | 5.1, 3.3
+// (which costs less up to some 256 comparisons of a token's choices), 125 to 8 of 64 5.3, 4.7 | 10.9, 11.0, 600 to 2 of 16, rows of 8192 bytes 6.4, 6.2 | 11.9, 9.4, 2000 13.9, 14.3 | 14.6, 14.6, 4000 to 1 of 8, rows of 2048
+// bytes 8.4, 8.5 | 11.7, 9.5; more: 3000 to 2 of 16, 8192 bytes 20 | 18, 8000 to 2 of 32, 512 bytes 18 | 13
+constexpr int64_t COUNTED = 4096, COMPARED = 256;
+bool at_once(int64_t n, int64_t top_k, int64_t E) { return n <= COUNTED && n * top_k > COMPARED && E <= ONE_DIGIT && top_k <= 64; }
 constexpr int64_t SHORT_LIST = 256;                        // ... of a token: those in front of each are gone through for each, so that the work grows with their square
 bool by_part(int64_t n, int64_t top_k, int64_t E) { return E <= ONE_DIGIT && n <= SOME && top_k <= SHORT_LIST; }
 int64_t most_parts(int64_t E) { return (1 << 20) / (E + 1); }      // 4 MB of counts
@@ -635,7 +712,7 @@ const char* ahead(const void* p, int64_t bytes) { return p ? (const char*)p + by
 int64_t ops_dispatch_workspace_bytes(int64_t T, int64_t top_k, int64_t E)
 {
     const int64_t n = T * top_k;
-    if (n <= FEW) return 0;
+    if (n <= FEW || at_once(n, top_k, E)) return 0;
     if (by_part(n, top_k, E)) return up16(4 * (E + 1) * (most_parts(E) + 1));
     int part_rows;
     return up16(4 * 256 * ((int64_t)parts_of(n, part_rows) + 1)) + 2 * up16(4 * n);
@@ -649,6 +726,12 @@ int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stre
         return launched();
     }
     const int64_t bytes = (int64_t)a.N * a.size, pieces = a.X && bytes > PIECE ? (bytes + PIECE - 1) / PIECE : 1, items = a.T * pieces;
+    if (at_once(n, a.top_k, a.E)) {
+        const int64_t most = 64 / a.top_k, each = (a.T + 511) / 512;         // 512 workgroups: two a compute unit count at the same time
+        const int tokens = (int)(each < most ? each : most);
+        hipLaunchKernelGGL(dispatch_some_kernel, dim3((unsigned)((a.T + tokens - 1) / tokens)), dim3(256), 2 * (a.E + 1) * sizeof(int), stream, a, tokens, pieces);
+        return launched();
+    }
     if (n <= FEW) {
         if (!fits_a_launch((items + 3) / 4 + ((int64_t)a.E + 8) / 8, 256)) return GEMM_F16_ERR_SIZE;
         const dim3 grid((unsigned)((items + ((int64_t)a.E + 8) / 8 + 3) / 4));

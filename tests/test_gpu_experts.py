@@ -55,7 +55,7 @@ def dispatch(expert, E, index=I64, N=0, size=2, blocks=0, seed=0, with_source=Tr
         assert np.array_equal(RS.fetch().reshape(blocks, n), scale)
 
 
-SIZES = [(1, 1, 1), (1, 4, 4), (3, 2, 5), (7, 1, 300), (32, 2, 16), (64, 1, 8), (13, 5, 7), (128, 2, 64), (257, 1, 3), (300, 3, 1000), (128, 8, 256), (1023, 1, 5), (512, 2, 65535),
+SIZES = [(300, 3, 5000), (10, 70, 9), (256, 1, 7), (16, 4, 3), (8, 8, 2047), (65, 64, 2047), (64, 64, 1), (1000, 4, 256), (2049, 2, 30), (4096, 1, 2047), (4097, 1, 2047), (1, 1, 1), (1, 4, 4), (3, 2, 5), (7, 1, 300), (32, 2, 16), (64, 1, 8), (13, 5, 7), (128, 2, 64), (257, 1, 3), (300, 3, 1000), (128, 8, 256), (1023, 1, 5), (512, 2, 65535),
          (1025, 1, 5), (205, 5, 64), (700, 2, 2047), (700, 2, 2048), (5000, 3, 17), (4096, 8, 64), (3000, 2, 65535), (20000, 4, 128), (40000, 6, 5000), (70001, 1, 1)]
 
 
@@ -98,7 +98,7 @@ def test_the_longest_list_comes_back():
     assert torch.equal(dY[place.long()].view(T, k, N), (weight[..., None] * dout[:, None].float()).bfloat16())
 
 
-@pytest.mark.parametrize("T,k", [(5, 2), (64, 4), (700, 3)])
+@pytest.mark.parametrize("T,k", [(5, 2), (64, 4), (700, 3), (1500, 3)])
 @pytest.mark.parametrize("case", ["all one", "none", "last", "reversed", "the same twice"])
 def test_orders_at_the_edges(T, k, case):
     E = 9
@@ -119,19 +119,20 @@ def test_no_tokens_no_choices_and_no_experts():
 # bytes a row: below a chunk, at its ends, at a piece's ends (4096), odd ones
 @pytest.mark.parametrize("N,size", [(1, 1), (1, 2), (7, 1), (7, 2), (15, 1), (3, 4), (16, 1), (17, 1), (31, 1), (9, 2), (2048, 1), (1000, 2), (2047, 2), (2048, 2), (2049, 2), (1024, 4),
                                     (4097, 1), (3001, 4), (10007, 1)])
-@pytest.mark.parametrize("T,k", [(9, 3), (600, 2)])
+@pytest.mark.parametrize("T,k", [(9, 3), (3, 20), (600, 2), (2100, 2)])
 def test_rows_of_any_width(N, size, T, k):
     dispatch(choices(np.random.default_rng(N), T, k, 6, 0.2), 6, N=N, size=size, pad=3, offset=1)
 
 
 @pytest.mark.parametrize("blocks", [1, 3, 64, 65, 130])
-@pytest.mark.parametrize("T,k", [(9, 3), (600, 2)])
+@pytest.mark.parametrize("T,k", [(9, 3), (3, 20), (600, 2), (2100, 2)])
 def test_scales_go_with_their_rows(blocks, T, k):
     dispatch(choices(np.random.default_rng(blocks), T, k, 6, 0.2), 6, N=40, size=1, blocks=blocks, with_source=False)
 
 
 def test_only_the_order():
     dispatch(choices(np.random.default_rng(1), 40, 3, 6, 0.2), 6, N=0)
+    dispatch(choices(np.random.default_rng(1), 1000, 3, 6, 0.2), 6, N=0)
     dispatch(choices(np.random.default_rng(1), 4000, 3, 6, 0.2), 6, N=0, with_source=False)
 
 

@@ -44,8 +44,8 @@ GOOD = {
     "quantize_i8_rows": dict(M=4, N=8, type=F16, act=2, X=P, ldx=16, Q=P, ldq=8, scale=P),
     "gemm_i8": dict(M=4, N=8, K=16, A=P, lda=16, a_scale=P, B=P, ldb=16, b_scale=P, C=P, ldc=8, c_type=F32),
     "gemm_i8_grouped": dict(T=4, N=8, K=16, E=2, offsets=P, A=P, lda=16, a_scale=P, B=P, ldb=16, b_stride=128, b_scale=P, bs_stride=8, C=P, ldc=8, c_type=BF16),
-    "expert_dispatch": dict(T=2000, top_k=2, E=5, index_type=1, expert=P, offsets=P, source=P, place=P, N=8, size=2, X=P, ldx=8, blocks=1, scale=P, ld_scale=2000, rows=P, ld_rows=8,
-                            row_scale=P, ld_row_scale=4000, workspace=P, workspace_bytes=1 << 24),
+    "expert_dispatch": dict(T=3000, top_k=2, E=5, index_type=1, expert=P, offsets=P, source=P, place=P, N=8, size=2, X=P, ldx=8, blocks=1, scale=P, ld_scale=3000, rows=P, ld_rows=8,
+                            row_scale=P, ld_row_scale=6000, workspace=P, workspace_bytes=1 << 24),
     "expert_combine": dict(T=4, top_k=2, N=8, type=F16, place=P, Y=P, ldy=8, weight=P, add=P, ld_add=8, out=P, ldo=8, out_type=F32),
     "expert_combine_grad": dict(T=4, top_k=2, N=8, type=BF16, place=P, dOut=P, lddo=8, weight=P, Y=P, ldy=8, dY=P, lddy=8, dweight=P),
 }
@@ -72,7 +72,7 @@ REFUSED = {
     "gemm_i8_grouped": each(SIZE, T=[-1, BIG], N=[-1, BIG], K=[-1, 131072], E=[-1, 65536]) + each(CONFIG, c_type=[3, 5]) + each(PITCH, lda=15, ldb=15, b_stride=-1, bs_stride=-1, ldc=7) +
                        each(NULL, offsets=0, A=0, B=0, C=0, a_scale=0, b_scale=0) + each(ALIGN, offsets=P + 2, C=P + 1, a_scale=P + 1, b_scale=P + 2),
     "expert_dispatch": each(SIZE, T=[-1, BIG, BIG // 2], top_k=[-1, 65536, BIG], E=[-1, 65536], N=[-1, BIG], blocks=[-1, BIG]) + each(CONFIG, index_type=[2, -1], size=[0, 3, 8]) +
-                       each(PITCH, ldx=7, ld_rows=[7, BIG], ld_scale=1999, ld_row_scale=3999) + each(NULL, expert=0, offsets=0, place=0, rows=0, scale=0, row_scale=0, workspace=0) +
+                       each(PITCH, ldx=7, ld_rows=[7, BIG], ld_scale=2999, ld_row_scale=5999) + each(NULL, expert=0, offsets=0, place=0, rows=0, scale=0, row_scale=0, workspace=0) +
                        each(ALIGN, expert=P + 4, offsets=P + 2, source=P + 2, place=P + 2, X=P + 1, rows=P + 1, scale=P + 2, row_scale=P + 2, workspace=P + 8) +
                        [(ALIGN, dict(index_type=0, expert=P + 2)), (ALIGN, dict(size=4, X=P + 2)), (NULL, dict(T=0, offsets=0)), (ALIGN, dict(top_k=0, offsets=P + 1))] +
                        each(WORKSPACE, workspace_bytes=[0, -1, 100]),
