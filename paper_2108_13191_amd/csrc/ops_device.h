@@ -23,6 +23,13 @@ __device__ __forceinline__ floatx4 mfma_i8(uintx4 a, uintx4 b, floatx4 c)
 }
 // a sum (bits of an integer) times the scales of its row and column, in this order: the scales' own product may leave f32's range
 __device__ __forceinline__ float scaled_sum(float bits, float row) { return (float)__builtin_bit_cast(int, bits) * row; }
+// ... times the column's, rounded to f32 (kept from the conversion to f16 that follows, with which it may become one instruction of one rounding in one kernel and not in another)
+__device__ __forceinline__ float scaled_column(float x, float column)
+{
+    float y = x * column;
+    asm("" : "+v"(y));
+    return y;
+}
 
 // magnitude as an integer: ordered as the magnitudes are, infinity above every number and NaN above infinity
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void ops_generic_kernel(const OpsGemm g)
             for (int r = 0; r < 4; r++) {
                 const int64_t col = n0 + wn + 16 * j + 4 * kq + r;
                 if (col >= g.N) continue;
-                if constexpr (ELEM == ELEM_I8) C[row * g.ldc + col] = (CT)(scaled_sum(part[i][j][r], g.sa[row]) * g.sb[(int64_t)e * g.sb_stride + col]);
+                if constexpr (ELEM == ELEM_I8) C[row * g.ldc + col] = (CT)scaled_column(scaled_sum(part[i][j][r], g.sa[row]), g.sb[(int64_t)e * g.sb_stride + col]);
                 else C[row * g.ldc + col] = (CT)(ELEM == ELEM_E4M3 ? acc[i][j][r] : part[i][j][r]);
             }
     }

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
             const float* const cs = g.sb + (int64_t)t.e * g.sb_stride;
             floatx4 v;
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = (float)sum[e] * rs * cs[min(col + e, g.N - 1)];
+            for (int e = 0; e < 4; e++) v[e] = scaled_column((float)sum[e] * rs, cs[min(col + e, g.N - 1)]);
             CT* const dst = (CT*)g.C + (int64_t)row * g.ldc + col;
             if (col + 4 <= g.N) {
                 typename CVec4<CT>::type o;

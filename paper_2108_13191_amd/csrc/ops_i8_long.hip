@@ -126,7 +126,9 @@ __global__ __launch_bounds__(256) void ops_i8_long_kernel(const OpsGemm g)
             }
 #pragma unroll
         for (int p = 0; p < 16; p++) {
-            const floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (2 * p + (lane >> 5)) * PITCH + 16 * (lane & 31)) * col_scale;
+            floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (2 * p + (lane >> 5)) * PITCH + 16 * (lane & 31));
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = scaled_column(v[e], col_scale[e]);
             const int r = 32 * m2 + 2 * p;
             if (r >= rows) continue;
             CT* const dst = C + (int64_t)r * g.ldc;

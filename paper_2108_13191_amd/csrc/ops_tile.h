@@ -593,7 +593,10 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && F
 #pragma unroll
         for (int ps = 0; ps < 32 / RPP; ps++) {
             floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (RPP * ps + orow) * PITCH + ocol * 4);
-            if constexpr (ELEM == ELEM_I8) v *= col_scale;
+            if constexpr (ELEM == ELEM_I8) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = scaled_column(v[e], col_scale[e]);
+            }
             const int r = 32 * m2 + RPP * ps;
             if (row_first + r < t.row_end) {
                 CT* const dst = C + (int64_t)r * g.ldc;

@@ -9,7 +9,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 from paper_2108_13191_amd import binding                                                  # noqa: E402
-from ops_util import LEAST, TYPE, UNIT, Mat, assert_within, offsets_of, stream            # noqa: E402
+from ops_util import DT, LEAST, TYPE, UNIT, Mat, assert_within, offsets_of, stream            # noqa: E402
 from layer_util import Ints                                                               # noqa: E402
 from i8_form_cases import FORMS, GROUPED, up                                              # noqa: E402
 
@@ -180,3 +180,19 @@ def test_one_matrix_for_all_experts_and_strides_of_scales():
     off = torch.tensor([0, 20, 50, 90], dtype=torch.int32, device="cuda")
     binding.check(binding.gemm_i8_grouped(T, N, K, E, off, a, K, sa, b, K, 0, sb, 0, c, N, TYPE["f32"], stream()))
     assert torch.equal(c.double(), 2 * (a.double() @ b.double().t()))
+
+
+# every form, small sums, and operands that only the kernel for any alignment takes
+@pytest.mark.parametrize("form,M,N,K,odd", [f + (0,) for f in FORMS if f[1] * f[2] * f[3] < 2e10] + [("any_alignment_64x64", 300, 700, 1100, 1), ("any_alignment_64x64", 5, 40, 17, 3)])
+@pytest.mark.parametrize("c", ["f16", "bf16", "f32"])
+def test_every_form_gives_the_same_bits(form, M, N, K, odd, c):
+    """Those of the definition: the exact sum to f32, times the row's scale, times the column's, each rounded to f32, and once to the result's type."""
+    gen = torch.Generator(device="cuda").manual_seed(M + N + K)
+    lda, ldb = up(K, 16) + odd, up(K, 16)
+    assert binding.i8_form(M, N, K, -1, lda, ldb, TYPE[c]) == form
+    a, b = (torch.randint(-128, 128, (rows, ld), dtype=I8, device="cuda", generator=gen) for rows, ld in ((M, lda), (N, ldb)))
+    sa, sb = (torch.rand(n, device="cuda", generator=gen) * s for n, s in ((M, 1.0), (N, 1e-3)))
+    out = torch.zeros(M, N, dtype=DT[c], device="cuda")
+    binding.check(binding.gemm_i8(M, N, K, a, lda, sa, b, ldb, sb, out, N, TYPE[c], stream()))
+    sums = (a[:, :K].double() @ b[:, :K].double().t()).float()              # exact in 64 bits
+    assert torch.equal(out, (sums * sa[:, None] * sb).to(DT[c]))
