@@ -73,7 +73,8 @@ int quantize_i8_rows(int64_t M, int64_t N, int64_t type, int64_t act,
  * The sum is exact, in 32-bit integers; it becomes f32 (one rounding, of sums beyond 2^24), is multiplied by the two scales in this order and
  * rounded once to c_type.  K <= 131071, so that no sum of products of any 8-bit integers (-128 to 127) leaves 32 bits; larger:
  * GEMM_F16_ERR_SIZE.  K = 0 gives zeros (a scale that is NaN or infinite gives NaN all the same).  Any alignment is
- * accepted; A and B 16-byte aligned with pitches that are multiples of 16 run the fast kernels (K and N of any size).
+ * accepted; A and B 16-byte aligned with pitches that are multiples of 16 run the fastest kernels (K and N of any size), others take up to twice (few
+ * rows) or four times (large products) as long, with pitches above 2^22 more.
  *
  * gemm_i8_grouped: the same grouped by expert as in gemm_e4m3_block_grouped: rows offsets[e] .. offsets[e+1]-1 of A (T rows) with B[e], which begins
  * b_stride * e elements behind B, and scales that begin bs_stride * e floats behind b_scale (strides from 0 on).  Rows in no group are left alone.

@@ -35,7 +35,7 @@ double padded(int64_t M, int64_t N, int bm, int bn) { return (double)((M + bm - 
 
 // What a product runs on: the kernel for any alignment, the tiled one, or the one for few rows on 16 fm x 16 nb results a workgroup.
 struct Form {
-    enum Kernel { ANY, TILES, FEW_ROWS } kernel;
+    enum Kernel { ANY, TILES, FEW_ROWS, FEW_ANY } kernel;
     OpsTile tile;
     int fm, nb;
 };
@@ -47,8 +47,9 @@ Form few_rows(int fm, int nb) { return {Form::FEW_ROWS, TILE_256, fm, nb}; }
 bool fits(const OpsGemm& g, const Form& f)
 {
     const bool square = f.tile == TILE_256 || f.tile == TILE_256_LONG, wide = square || f.tile == TILE_128x256, tall = square || f.tile == TILE_256x128;
-    const int bm = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.fm : tall ? 256 : 128;
-    const int bn = f.kernel == Form::ANY ? 64 : f.kernel == Form::FEW_ROWS ? 16 * f.nb : wide ? 256 : 128;
+    const bool few = f.kernel == Form::FEW_ROWS || f.kernel == Form::FEW_ANY;
+    const int bm = f.kernel == Form::ANY ? 64 : few ? 16 * f.fm : tall ? 256 : 128;
+    const int bn = f.kernel == Form::ANY ? 64 : few ? 16 * f.nb : wide ? 256 : 128;
     const int64_t grid = tile_grid(g, bm, bn);
     return grid >= 0 && fits_a_launch(grid, f.kernel == Form::ANY ? 256 : 512);
 }
@@ -71,6 +72,10 @@ Form preferred_i8(const OpsGemm& g, bool allow_few_rows)
         const double tiles = expected_tiles(g, bm, bn) / cus, rounds = 0.5 * ((tiles < 1.0 ? 1.0 : tiles) + ceil(tiles));
         return c.launch + rounds * (c.tile + c.k1000 * 1e-3 * g.K);
     };
+    if (!is_aligned(g)) {                                  // 32 x 32 or 64 x 64, by the same costs
+        const int f = allow_few_rows && cost(g.offsets ? few[3].grouped : few[3].single, 32, 32) < cost(g.offsets ? few[5].grouped : few[5].single, 64, 64) ? 2 : 4;
+        return {Form::FEW_ANY, TILE_256, f, f};
+    }
     double least = cost(small, 128, 128);
     Form best = tiles(TILE_128);
     if (const double us = cost(large, 256, 256); us < least) {
@@ -92,7 +97,8 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
 {
     if (!tiles_take(g)) return any_alignment();
     // (a form that loads 8 elements at any alignment needs rows that have them)
-    if (!is_aligned(g)) return is_8bit(g) || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8 ? any_alignment() : tiles(TILE_128_ANY);
+    if (g.elem == ELEM_I8) return preferred_i8(g, allow_few_rows);
+    if (!is_aligned(g)) return g.elem == ELEM_E4M3 || g.N < 8 || (g.k_ragged ? g.M : g.K) < 8 ? any_alignment() : tiles(TILE_128_ANY);
     const int cus = chip().cus;
     const double rows = (double)g.M / g.E;                                  // of a group
     if (g.k_ragged) {
@@ -109,7 +115,6 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
     // 256 x 256: groups that fill three quarters of one, and where 128 x 128 ones, two a compute unit, need a second round; 16 bits, 4 experts (2048,2048): rounds
     // of the smaller ones 1.04: 39 | 45 (gradient of A) and 55 (forward), 1.28: 41 | 47 and 55, 0.79: 39 | 30; 8 experts (2304,768) 1.15: 44 | 61, 0.96: 21 | 18.5
     const bool large = rows >= 192.0 && expected_tiles(g, 128, 128) >= 2.0 * cus;
-    if (g.elem == ELEM_I8) return preferred_i8(g, allow_few_rows);
     if (g.elem == ELEM_E4M3) {
         // few rows, by streaming B: where 64 x 32 tiles are at most some 2.6 a compute unit: 128 rows of (8192,8192) 49 | 64 (128 x 128 tiles), 256 rows
         // of (4096,4096) 27 | 34, 256 of (8192,8192) 95 | 64; groups of up to 20 rows: 16 rows each of 16 experts (4096,2048) 41 | 45, 32 each 56 | 46
@@ -151,7 +156,8 @@ Form preferred(const OpsGemm& g, bool allow_few_rows)
 Form choose(const OpsGemm& g)
 {
     Form f = preferred(g, true);
-    if (f.kernel == Form::FEW_ROWS && !fits(g, f)) f = preferred(g, false);
+    if ((f.kernel == Form::FEW_ROWS || f.kernel == Form::FEW_ANY) && !fits(g, f)) f = preferred(g, false);
+    if (f.kernel == Form::FEW_ANY && !fits(g, f)) f = any_alignment();
     if (f.kernel == Form::TILES && f.tile != TILE_128_ANY && !fits(g, f)) f = tiles(g.elem == ELEM_E4M3 && f.tile != TILE_128_FAST ? TILE_256x128 : TILE_256);
     return f;
 }
@@ -160,6 +166,7 @@ int launch(const OpsGemm& g)
 {
     const Form f = choose(g);
     if (f.kernel == Form::ANY) return ops_launch_generic(g);
+    if (f.kernel == Form::FEW_ANY) return ops_launch_few_i8_any(g, f.fm);
     if (f.kernel == Form::FEW_ROWS) return g.elem == ELEM_I8 ? ops_launch_few_i8(g, f.fm, f.nb) : ops_launch_skinny_e4m3(g, f.fm, f.nb);
     if (g.elem == ELEM_I8) return ops_launch_tiles_i8(g, f.tile);
     return g.elem == ELEM_E4M3 ? ops_launch_tiles_e4m3(g, f.tile) : g.elem == ELEM_F16 ? ops_launch_tiles_f16(g, f.tile) : ops_launch_tiles_bf16(g, f.tile);
@@ -168,6 +175,7 @@ int launch(const OpsGemm& g)
 const char* name_of(const OpsGemm& g, const Form& f)
 {
     if (f.kernel == Form::ANY) return "any_alignment_64x64";
+    if (f.kernel == Form::FEW_ANY) return f.fm == 2 ? "few_rows_32x32_any_alignment" : "few_rows_64x64_any_alignment";
     if (f.kernel == Form::FEW_ROWS)
         return f.fm == 1 ? (f.nb == 1 ? "few_rows_16x16" : f.nb == 2 ? "few_rows_16x32" : "few_rows_16x64") : f.fm == 8 ? "few_rows_128x64" : f.fm == 4 ? "few_rows_64x64" :
                f.nb == 1 ? "few_rows_32x16" : f.nb == 2 ? "few_rows_32x32" : "few_rows_32x64";

@@ -71,6 +71,8 @@ int ops_launch_long_i8(const OpsGemm& g);
 int ops_launch_skinny_e4m3(const OpsGemm& g, int fm, int nb);
 // ops_i8_few.hip: the same in i8, 1 x 1, 1 x 4, 2 x 1, 2 x 2, 2 x 4, 4 x 4 or 8 x 4
 int ops_launch_few_i8(const OpsGemm& g, int fm, int nb);
+// ... at any alignment, 2 x 2 or 4 x 4
+int ops_launch_few_i8_any(const OpsGemm& g, int fm);
 
 // ops_norm.hip
 struct NormArgs {

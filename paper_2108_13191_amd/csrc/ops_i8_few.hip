@@ -12,14 +12,19 @@ namespace {
 
 using namespace ops_tile;
 
+typedef uintx4 uintx4_any __attribute__((aligned(1)));
+
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
+// S = 0: operands of any alignment, a k step ahead in registers and one stage in LDS.  us, here | the kernel for any alignment of ops_generic.hip: 16 rows of (8192,8190) 17.7 | 541,
+// (300,700,1100) 6.6 | 70, (2000,2000,2001) 39 | 365, (4000,4000,4001) 225 | 3165
 template <int FM, int NB, int WAVES, int S, typename CT>
 __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
 {
-    constexpr int BM = 16 * FM, BN = 16 * NB, COPIES = 2 * (FM + NB), STAGE = COPIES * 1024, RING = S * STAGE;
+    constexpr bool ANY = S == 0;
+    constexpr int BM = 16 * FM, BN = 16 * NB, COPIES = 2 * (FM + NB), STAGE = COPIES * 1024, RING = (ANY ? 1 : S) * STAGE;
     constexpr int PASS = FM * NB * 1024 <= RING ? FM * NB : FM * NB / 2;       // blocks of sums that a ring holds
-    static_assert(PASS * 1024 <= RING && FM * NB % PASS == 0 && WAVES * RING <= 160 * 1024 && (S == 1 || S == 2));
+    static_assert(PASS * 1024 <= RING && FM * NB % PASS == 0 && WAVES * RING <= 160 * 1024 && S <= 2);
     __shared__ __attribute__((aligned(1024))) char smem[WAVES * RING];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q = lane >> 4;
@@ -65,23 +70,51 @@ __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
         for (int n = 0; n < NB; n++) { b[n].lo = get(stage + (FM + n) * 2048 + rd0); b[n].hi = get(stage + (FM + n) * 2048 + rd1); }
     };
 
-    uint32_t stage = ring, other = ring + (S - 1) * STAGE;
-    if (wave < k_full) copy(wave, stage);
-    if (S > 1 && wave + WAVES < k_full) copy(wave + WAVES, other);
-    for (int k = wave; k < k_full; k += WAVES) {
-        if (S > 1 && k + WAVES < k_full) wait_copies<COPIES>();                        // the next step's may be on their way
-        else                    wait_copies<0>();
-        read(stage);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                    // before the stage is written again
-        if (k + S * WAVES < k_full) copy(k + S * WAVES, stage);
-        const uint32_t s = stage;
-        stage = other;
-        other = s;
-        multiply();
+    if constexpr (ANY) {
+        uintx4 v[COPIES];                                                     // the next step
+        auto fetch = [&](int k) {
+            const char *const ap = a_tile + (int64_t)k * STEP, *const bp = b_tile + (int64_t)k * STEP;
+#pragma unroll
+            for (int i = 0; i < COPIES; i++) v[i] = *(const uintx4_any*)((i < 2 * FM ? ap : bp) + off[i]);
+        };
+        if (wave < k_full) fetch(wave);
+        for (int k = wave; k < k_full; k += WAVES) {                          // (a wavefront's LDS accesses are in order)
+#pragma unroll
+            for (int i = 0; i < COPIES; i++) *(__attribute__((address_space(3))) uintx4*)(uintptr_t)(ring + 1024 * i + 16 * lane) = v[i];
+            if (k + WAVES < k_full) fetch(k + WAVES);
+            read(ring);
+            multiply();
+        }
+    } else {
+        uint32_t stage = ring, other = ring + (S - 1) * STAGE;
+        if (wave < k_full) copy(wave, stage);
+        if (S > 1 && wave + WAVES < k_full) copy(wave + WAVES, other);
+        for (int k = wave; k < k_full; k += WAVES) {
+            if (S > 1 && k + WAVES < k_full) wait_copies<COPIES>();           // the next step's may be on their way
+            else                             wait_copies<0>();
+            read(stage);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                // before the stage is written again
+            if (k + S * WAVES < k_full) copy(k + S * WAVES, stage);
+            const uint32_t s = stage;
+            stage = other;
+            other = s;
+            multiply();
+        }
     }
     if (left > 0 && k_full % WAVES == wave) {                                 // the short last step, straight into registers: zeros behind K
         auto chunk = [&](const char* p, int n) {
             uintx4 v = {0u, 0u, 0u, 0u};
+            if constexpr (ANY) {                                              // nothing behind the row's end is read: its last 16 bytes, moved down, or byte by byte
+                if (n >= 16) v = *(const uintx4_any*)p;
+                else if (n > 0 && K >= 16) {
+                    typedef uint64_t pair __attribute__((ext_vector_type(2)));
+                    const pair x = __builtin_bit_cast(pair, *(const uintx4_any*)(p - (16 - n)));
+                    const int s = 8 * (16 - n);
+                    v = __builtin_bit_cast(uintx4, s >= 64 ? pair{x[1] >> (s - 64), 0ull} : pair{(x[0] >> s) | (x[1] << (64 - s)), x[1] >> s});
+                } else
+                    for (int i = 0; i < n; i++) v[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+                return v;
+            }
             if (n > 0) {
                 v = *(const uintx4*)p;
 #pragma unroll
@@ -146,6 +179,7 @@ int launch_few(const OpsGemm& g)
 
 }  // namespace
 
+int ops_launch_few_i8_any(const OpsGemm& g, int fm) { return fm == 2 ? launch_few<2, 2, 4, 0>(g) : launch_few<4, 4, 4, 0>(g); }
 int ops_launch_few_i8(const OpsGemm& g, int fm, int nb)
 {
     if (fm == 1) return nb == 1 ? launch_few<1, 1, 8>(g) : launch_few<1, 4, 4>(g);
