@@ -297,11 +297,6 @@ def product_form(product, T, N, K, E, lda, ldb, c_type):
 INDEX_I32, INDEX_I64 = 0, 1
 
 
-def _call_layer(name, *args) -> int:
-    rc = _layer_words(getattr(load(), name + "_address"), _LAYER_OPS[name], *args)
-    return rc if rc is not NotImplemented else _general(name, args)
-
-
 def layer_norm(M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream=0) -> int:
     """H = X + R, Y = (H - mean) * rstd * gamma + beta in 16 bits and / or as 8-bit integers in Q and scale; R, beta and any output may be None."""
     args = (M, N, type, X, ldx, R, ldr, gamma, beta, eps, H, ldh, Y, ldy, Q, ldq, scale, mean, rstd, stream)
@@ -316,22 +311,30 @@ def layer_norm_grad_workspace_bytes(M, N) -> int:
 
 def layer_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream=0) -> int:
     """dX (of x and of the residual alike), dgamma and dbeta (f32, None: not formed) from dY and dH (None: no gradient of h itself)."""
-    return _call_layer("layer_norm_grad", M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream)
+    args = (M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, dX, lddx, dgamma, dbeta, workspace, workspace_bytes, stream)
+    rc = _layer_words(load().layer_norm_grad_address, _LAYER_OPS["layer_norm_grad"], *args)
+    return rc if rc is not NotImplemented else _general("layer_norm_grad", args)
 
 
 def quantize_i8_rows(M, N, type, act, X, ldx, Q, ldq, scale, stream=0) -> int:
     """Q (8-bit integers), scale[row] = X (M x N of `type`; M x 2N for ACT_SWIGLU) after `act`, a scale for each row."""
-    return _call_layer("quantize_i8_rows", M, N, type, act, X, ldx, Q, ldq, scale, stream)
+    args = (M, N, type, act, X, ldx, Q, ldq, scale, stream)
+    rc = _layer_words(load().quantize_i8_rows_address, _LAYER_OPS["quantize_i8_rows"], *args)
+    return rc if rc is not NotImplemented else _general("quantize_i8_rows", args)
 
 
 def gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream=0) -> int:
     """C (M x N of `c_type`) = A (M x K, a scale a row) @ B (N x K, a scale a row) transposed, 8-bit integers."""
-    return _call_layer("gemm_i8", M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream)
+    args = (M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream)
+    rc = _layer_words(load().gemm_i8_address, _LAYER_OPS["gemm_i8"], *args)
+    return rc if rc is not NotImplemented else _general("gemm_i8", args)
 
 
 def gemm_i8_grouped(T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream=0) -> int:
     """gemm_i8 of rows offsets[e] .. offsets[e + 1] (int32 on the device) with B[e], for E experts."""
-    return _call_layer("gemm_i8_grouped", T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream)
+    args = (T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream)
+    rc = _layer_words(load().gemm_i8_grouped_address, _LAYER_OPS["gemm_i8_grouped"], *args)
+    return rc if rc is not NotImplemented else _general("gemm_i8_grouped", args)
 
 
 def i8_form(T, N, K, E, lda, ldb, c_type):
@@ -348,18 +351,24 @@ def expert_dispatch_workspace_bytes(T, top_k, E) -> int:
 def expert_dispatch(T, top_k, E, index_type, expert, offsets, source, place, N, size, X, ldx, blocks, scale, ld_scale, rows, ld_rows, row_scale, ld_row_scale,
                     workspace, workspace_bytes, stream=0) -> int:
     """Sorts the choices `expert` (T x top_k) by expert into offsets, source (None: not written) and place, and copies X's rows and scales to their places (X None: only sorts)."""
-    return _call_layer("expert_dispatch", T, top_k, E, index_type, expert, offsets, source, place, N, size, X, ldx, blocks, scale, ld_scale, rows, ld_rows,
-                       row_scale, ld_row_scale, workspace, workspace_bytes, stream)
+    args = (T, top_k, E, index_type, expert, offsets, source, place, N, size, X, ldx, blocks, scale, ld_scale, rows, ld_rows,
+            row_scale, ld_row_scale, workspace, workspace_bytes, stream)
+    rc = _layer_words(load().expert_dispatch_address, _LAYER_OPS["expert_dispatch"], *args)
+    return rc if rc is not NotImplemented else _general("expert_dispatch", args)
 
 
 def expert_combine(T, top_k, N, type, place, Y, ldy, weight, add, ld_add, out, ldo, out_type, stream=0) -> int:
     """out[t] = add[t] + sum over j of weight[t][j] * Y[place[t][j]]; weight None: 1, add None: 0."""
-    return _call_layer("expert_combine", T, top_k, N, type, place, Y, ldy, weight, add, ld_add, out, ldo, out_type, stream)
+    args = (T, top_k, N, type, place, Y, ldy, weight, add, ld_add, out, ldo, out_type, stream)
+    rc = _layer_words(load().expert_combine_address, _LAYER_OPS["expert_combine"], *args)
+    return rc if rc is not NotImplemented else _general("expert_combine", args)
 
 
 def expert_combine_grad(T, top_k, N, type, place, dOut, lddo, weight, Y, ldy, dY, lddy, dweight, stream=0) -> int:
     """dY[place[t][j]] = weight[t][j] * dOut[t] and dweight[t][j] = dOut[t] . Y[place[t][j]] (f32); dY or dweight None: not formed."""
-    return _call_layer("expert_combine_grad", T, top_k, N, type, place, dOut, lddo, weight, Y, ldy, dY, lddy, dweight, stream)
+    args = (T, top_k, N, type, place, dOut, lddo, weight, Y, ldy, dY, lddy, dweight, stream)
+    rc = _layer_words(load().expert_combine_grad_address, _LAYER_OPS["expert_combine_grad"], *args)
+    return rc if rc is not NotImplemented else _general("expert_combine_grad", args)
 
 
 def strerror(code: int) -> str:
