@@ -70,8 +70,14 @@ def _place(route):
     return route.place.to(torch.int32).contiguous()
 
 
-def _weight(w):
-    return None if w is None else w.float().contiguous()
+def _weight(w, tokens, top_k):
+    """The weights of a route, as many as the kernels read.  A router of the caller's own may have one for each token, for each choice or for all."""
+    if w is None:
+        return None
+    shape = (tokens, top_k)
+    if w.is_complex() or w.dim() > 2 or any(n not in (1, of) for n, of in zip(w.shape[::-1], shape[::-1])):
+        raise ValueError(f"weights of a route: {tokens} x {top_k} or what is broadcast to that expected, got {tuple(w.shape)} of {w.dtype}")
+    return w.float().expand(shape).contiguous()
 
 
 def _on_gpu(t):
@@ -181,7 +187,7 @@ class ExpertLayer:
             return ((rows if weight is None else rows * weight[..., None]).sum(1) + add.float()).to(dtype)
         T, N = add.shape
         out = torch.empty(T, N, dtype=dtype, device=rows.device)
-        check(binding.expert_combine(T, self.top_k, N, TYPES[rows.dtype], _place(route), rows, N, _weight(weight), add, _pitch(add), out, N, TYPES[dtype], _stream(out)))
+        check(binding.expert_combine(T, self.top_k, N, TYPES[rows.dtype], _place(route), rows, N, _weight(weight, T, self.top_k), add, _pitch(add), out, N, TYPES[dtype], _stream(out)))
         return out
 
     def _combine_grad(self, rows, route, dout):
@@ -193,7 +199,7 @@ class ExpertLayer:
             weight[route.place] = route.weight.flatten()
             return (dout[route.source].float() * weight[:, None]).to(self.dtype), dweight
         drows, dweight = torch.empty_like(rows), torch.empty(T, self.top_k, dtype=torch.float32, device=rows.device)
-        check(binding.expert_combine_grad(T, self.top_k, N, TYPES[rows.dtype], _place(route), dout, _pitch(dout), _weight(route.weight), rows, N, drows, N, dweight, _stream(rows)))
+        check(binding.expert_combine_grad(T, self.top_k, N, TYPES[rows.dtype], _place(route), dout, _pitch(dout), _weight(route.weight, T, self.top_k), rows, N, drows, N, dweight, _stream(rows)))
         return drows, dweight
 
     def _rows(self, name, t, tokens):

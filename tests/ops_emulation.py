@@ -29,7 +29,7 @@ def quotients(y, scale):
 
 def block_max(y):
     """Largest magnitudes of 128 neighbours of each row."""
-    return torch.nn.functional.pad(y, (0, -y.shape[1] % 128)).view(y.shape[0], -1, 128).abs().amax(2).clamp_min(2.0 ** -96)
+    return torch.nn.functional.pad(y, (0, -y.shape[1] % 128)).view(y.shape[0], ceil128(y.shape[1]), 128).abs().amax(2).clamp_min(2.0 ** -96)
 
 
 def quantize_e4m3_rows(M, N, type, act, X, ldx, Q, ldq, scale, ld_scale, stream=0):
