@@ -65,9 +65,29 @@ def _rows_of(source, rows, scale):
     return moved, None if scale is None else scale[..., source].contiguous()
 
 
-def _place(route):
-    """As the kernels read it; a router of the caller's own may have its 64-bit indices."""
-    return route.place.to(torch.int32).contiguous()
+class _Route(SimpleNamespace):
+    """A route that the layer has made itself: every row is some choice's."""
+
+
+def _places(route, tokens, top_k):
+    """The row of each choice (tokens x top_k), of which a router of the caller's own may have others than the kernels can read."""
+    place = route.place
+    if place.numel() != tokens * top_k or place.dtype == torch.bool or place.is_floating_point() or place.is_complex():
+        raise ValueError(f"places of a route: {tokens} x {top_k} integers expected, got {tuple(place.shape)} of {place.dtype}")
+    return place.reshape(tokens, top_k)
+
+
+def _places32(place):
+    """As the kernels read them; one outside the rows stays there."""
+    return (place if place.dtype == torch.int32 else place.long().clamp(-1, place.numel()).to(torch.int32)).contiguous()
+
+
+def _placed(rows, place):
+    """Which choices have a row of `rows`, and each choice's row in f32, zeros without one."""
+    there = (place >= 0) & (place < rows.shape[0])
+    if rows.shape[0] == 0:
+        rows = rows.new_zeros(1, rows.shape[1])
+    return there, torch.where(there[..., None], rows[torch.where(there, place, 0).long()].float(), 0.0)
 
 
 def _weight(w, tokens, top_k):
@@ -148,8 +168,9 @@ class ExpertLayer:
 
     def route(self, y):
         """The top_k experts of each token: `source`, the token of each of the tokens * top_k rows in the experts' order; `place`, where
-        row j of token t went; `offsets`, the rows of each expert, and the weights.  Another one in its place decides itself; rows then move by its `source` and `place`."""
-        return self._route(y)[0]
+        row j of token t went; `offsets`, the rows of each expert, and the weights.  Another one in its place decides itself; rows then move by its `source` and `place`, which
+        may be more (groups filled up with rows of any token) or fewer than the choices: a choice whose place is no row (-1) adds nothing.  Places are different from each other."""
+        return SimpleNamespace(**vars(self._route(y)[0]))
 
     def _route(self, y, rows=None, scale=None):
         """route(y), and the tokens' rows and scales (blocks x tokens, or one for each token) in the experts' order."""
@@ -165,7 +186,7 @@ class ExpertLayer:
             place[order] = torch.arange(order.numel(), device=device)
             bounds = torch.arange(self.experts + 1, device=device)
             offsets = torch.searchsorted(expert.flatten()[order], bounds).to(torch.int32)
-            route = SimpleNamespace(weight=weight, expert=expert, source=order // k, place=place, offsets=offsets)
+            route = _Route(weight=weight, expert=expert, source=order // k, place=place, offsets=offsets)
             return route, *((None, None) if rows is None else _rows_of(route.source, rows, scale))
         expert = expert.contiguous()
         offsets, source, place = (torch.empty(n, dtype=torch.int32, device=device) for n in (self.experts + 1, T * k, T * k))
@@ -178,28 +199,34 @@ class ExpertLayer:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         check(binding.expert_dispatch(T, k, self.experts, binding.INDEX_I64, expert, offsets, source, place, N, size, rows, 0 if rows is None else _pitch(rows), blocks, scale, T,
                                       moved, 0 if rows is None else _pitch(moved), moved_scale, T * k, workspace, need, _stream(y)))
-        return SimpleNamespace(weight=weight, expert=expert, source=source, place=place, offsets=offsets), moved, moved_scale
+        return _Route(weight=weight, expert=expert, source=source, place=place, offsets=offsets), moved, moved_scale
+
+    def _moved_by_torch(self, rows, place):
+        """The kernels take as many rows as there are choices; a router of the caller's own may have more (groups filled up) or fewer."""
+        return not _on_gpu(rows) or rows.shape[0] != place.numel()
 
     def _combine(self, rows, route, add, weight, dtype):
-        """add + the sum over each token's rows (times its weights, if there are any), in a fixed order, f32, rounded to dtype."""
-        if not _on_gpu(rows):
-            rows = rows[route.place].float().view(-1, self.top_k, rows.shape[1])
-            return ((rows if weight is None else rows * weight[..., None]).sum(1) + add.float()).to(dtype)
+        """add + the sum over each token's rows (times its weights, if there are any), in a fixed order, f32, rounded to dtype.  A choice without a row adds nothing."""
         T, N = add.shape
+        place, weight = _places(route, T, self.top_k), _weight(weight, T, self.top_k)
+        if self._moved_by_torch(rows, place):
+            rows = _placed(rows, place)[1]
+            return ((rows if weight is None else rows * weight[..., None]).sum(1) + add.float()).to(dtype)
         out = torch.empty(T, N, dtype=dtype, device=rows.device)
-        check(binding.expert_combine(T, self.top_k, N, TYPES[rows.dtype], _place(route), rows, N, _weight(weight, T, self.top_k), add, _pitch(add), out, N, TYPES[dtype], _stream(out)))
+        check(binding.expert_combine(T, self.top_k, N, TYPES[rows.dtype], _places32(place), rows, N, weight, add, _pitch(add), out, N, TYPES[dtype], _stream(out)))
         return out
 
     def _combine_grad(self, rows, route, dout):
-        """The gradients of _combine's rows and weights."""
+        """The gradients of _combine's rows and weights; zeros for a row of no choice, as products over whole groups read it."""
         T, N = dout.shape
-        if not _on_gpu(rows):
-            dweight = (rows[route.place].view(-1, self.top_k, N).float() * dout[:, None].float()).sum(-1)
-            weight = torch.empty(route.place.numel(), dtype=torch.float32, device=dout.device)
-            weight[route.place] = route.weight.flatten()
-            return (dout[route.source].float() * weight[:, None]).to(self.dtype), dweight
-        drows, dweight = torch.empty_like(rows), torch.empty(T, self.top_k, dtype=torch.float32, device=rows.device)
-        check(binding.expert_combine_grad(T, self.top_k, N, TYPES[rows.dtype], _place(route), dout, _pitch(dout), _weight(route.weight, T, self.top_k), rows, N, drows, N, dweight, _stream(rows)))
+        place, weight = _places(route, T, self.top_k), _weight(route.weight, T, self.top_k)
+        if self._moved_by_torch(rows, place):
+            there, y = _placed(rows, place)
+            drows = torch.zeros(rows.shape[0] + 1, N, dtype=self.dtype, device=rows.device)          # the last one: of choices without a row
+            drows[torch.where(there, place, rows.shape[0]).long()] = (dout[:, None].float() * weight[..., None]).to(self.dtype)
+            return drows[:-1], (y * dout[:, None].float()).sum(-1)
+        drows, dweight = torch.empty_like(rows) if isinstance(route, _Route) else torch.zeros_like(rows), torch.empty(T, self.top_k, dtype=torch.float32, device=rows.device)
+        check(binding.expert_combine_grad(T, self.top_k, N, TYPES[rows.dtype], _places32(place), dout, _pitch(dout), weight, rows, N, drows, N, dweight, _stream(rows)))
         return drows, dweight
 
     def _rows(self, name, t, tokens):
