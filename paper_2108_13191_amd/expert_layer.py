@@ -69,12 +69,12 @@ class _Route(SimpleNamespace):
     """A route that the layer has made itself: every row is some choice's."""
 
 
-def _places(route, tokens, top_k):
+def _places(route, tokens, top_k, device):
     """The row of each choice (tokens x top_k), of which a router of the caller's own may have others than the kernels can read."""
     place = route.place
     if place.numel() != tokens * top_k or place.dtype == torch.bool or place.is_floating_point() or place.is_complex():
         raise ValueError(f"places of a route: {tokens} x {top_k} integers expected, got {tuple(place.shape)} of {place.dtype}")
-    return place.reshape(tokens, top_k)
+    return place.reshape(tokens, top_k).to(device)
 
 
 def _places32(place):
@@ -90,14 +90,14 @@ def _placed(rows, place):
     return there, torch.where(there[..., None], rows[torch.where(there, place, 0).long()].float(), 0.0)
 
 
-def _weight(w, tokens, top_k):
+def _weight(w, tokens, top_k, device):
     """The weights of a route, as many as the kernels read.  A router of the caller's own may have one for each token, for each choice or for all."""
     if w is None:
         return None
     shape = (tokens, top_k)
     if w.is_complex() or w.dim() > 2 or any(n not in (1, of) for n, of in zip(w.shape[::-1], shape[::-1])):
         raise ValueError(f"weights of a route: {tokens} x {top_k} or what is broadcast to that expected, got {tuple(w.shape)} of {w.dtype}")
-    return w.float().expand(shape).contiguous()
+    return w.to(device, torch.float32).expand(shape).contiguous()
 
 
 def _on_gpu(t):
@@ -169,7 +169,8 @@ class ExpertLayer:
     def route(self, y):
         """The top_k experts of each token: `source`, the token of each of the tokens * top_k rows in the experts' order; `place`, where
         row j of token t went; `offsets`, the rows of each expert, and the weights.  Another one in its place decides itself; rows then move by its `source` and `place`, which
-        may be more (groups filled up with rows of any token) or fewer than the choices: a choice whose place is no row (-1) adds nothing.  Places are different from each other."""
+        may be more (groups filled up with rows of any token) or fewer than the choices: a choice whose place is no row (-1) adds nothing.  Places are different from each other.
+        `place`, `weight` and `source` may be on the host (they are copied then, which waits for it)."""
         return SimpleNamespace(**vars(self._route(y)[0]))
 
     def _route(self, y, rows=None, scale=None):
@@ -208,7 +209,7 @@ class ExpertLayer:
     def _combine(self, rows, route, add, weight, dtype):
         """add + the sum over each token's rows (times its weights, if there are any), in a fixed order, f32, rounded to dtype.  A choice without a row adds nothing."""
         T, N = add.shape
-        place, weight = _places(route, T, self.top_k), _weight(weight, T, self.top_k)
+        place, weight = _places(route, T, self.top_k, add.device), _weight(weight, T, self.top_k, add.device)
         if self._moved_by_torch(rows, place):
             rows = _placed(rows, place)[1]
             return ((rows if weight is None else rows * weight[..., None]).sum(1) + add.float()).to(dtype)
@@ -219,7 +220,7 @@ class ExpertLayer:
     def _combine_grad(self, rows, route, dout):
         """The gradients of _combine's rows and weights; zeros for a row of no choice, as products over whole groups read it."""
         T, N = dout.shape
-        place, weight = _places(route, T, self.top_k), _weight(route.weight, T, self.top_k)
+        place, weight = _places(route, T, self.top_k, dout.device), _weight(route.weight, T, self.top_k, dout.device)
         if self._moved_by_torch(rows, place):
             there, y = _placed(rows, place)
             drows = torch.zeros(rows.shape[0] + 1, N, dtype=self.dtype, device=rows.device)          # the last one: of choices without a row

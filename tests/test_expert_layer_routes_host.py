@@ -198,3 +198,11 @@ def test_places_that_are_none_are_refused(layer, make):
     for call in (lambda: layer.serve(x, r), lambda: layer.train_forward(x, r), lambda: layer.backward(s, dout, dh)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_parts_of_a_route_go_to_the_rows_device():
+    """The kernels get addresses: what lies elsewhere is copied there first."""
+    route = SimpleNamespace(place=torch.arange(T * TOP))
+    place, weight = expert_layer._places(route, T, TOP, torch.device("meta")), expert_layer._weight(torch.ones(T, 1), T, TOP, torch.device("meta"))
+    assert place.device.type == weight.device.type == expert_layer._places32(place).device.type == "meta"
+    assert place.shape == weight.shape == (T, TOP) and weight.is_contiguous()
