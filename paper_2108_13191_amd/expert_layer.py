@@ -77,6 +77,14 @@ def _places(route, tokens, top_k, device):
     return place.reshape(tokens, top_k).to(device)
 
 
+def _offsets(route, experts, device):
+    """Where each expert's rows begin, as the products read it."""
+    offsets = route.offsets
+    if tuple(offsets.shape) != (experts + 1,) or offsets.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"offsets of a route: {experts + 1} integers of 32 or 64 bits expected, got {tuple(offsets.shape)} of {offsets.dtype}")
+    return (offsets if offsets.dtype == torch.int32 else offsets.clamp(0, 2 ** 31 - 1)).to(device, torch.int32).contiguous()
+
+
 def _places32(place):
     """As the kernels read them; one outside the rows stays there."""
     return (place if place.dtype == torch.int32 else place.long().clamp(-1, place.numel()).to(torch.int32)).contiguous()
@@ -170,7 +178,7 @@ class ExpertLayer:
         """The top_k experts of each token: `source`, the token of each of the tokens * top_k rows in the experts' order; `place`, where
         row j of token t went; `offsets`, the rows of each expert, and the weights.  Another one in its place decides itself; rows then move by its `source` and `place`, which
         may be more (groups filled up with rows of any token) or fewer than the choices: a choice whose place is no row (-1) adds nothing.  Places are different from each other.
-        `place`, `weight` and `source` may be on the host (they are copied then, which waits for it)."""
+        Its parts may be on the host (they are copied then, which waits for it)."""
         return SimpleNamespace(**vars(self._route(y)[0]))
 
     def _route(self, y, rows=None, scale=None):
@@ -297,8 +305,9 @@ class ExpertLayer:
         """h and out of x and the residual r (tokens x hidden)."""
         w, n = self.quantized, self._norm(x, r, self.format)
         route, rows, scale = self._route(n.y, n.q, n.scale)
-        up = self._product8(rows, scale, w.up, route.offsets)
-        out = self._product8(*self._swiglu8(up), w.down, route.offsets)
+        offsets = _offsets(route, self.experts, n.y.device)
+        up = self._product8(rows, scale, w.up, offsets)
+        out = self._product8(*self._swiglu8(up), w.down, offsets)
         shared = self._product8(*self._swiglu8(self._product8(n.q, n.scale, w.shared_up)), w.shared_down)
         return SimpleNamespace(h=n.h, out=self._combine(out, route, shared, route.weight, self.dtype), route=route)
 
@@ -323,9 +332,10 @@ class ExpertLayer:
         s.route, s.a, _ = self._route(s.y, s.y)
         s.all = torch.arange(2, dtype=torch.int32, device=x.device) * x.shape[0]      # the shared expert: one group
         s.shared_a = s.y
-        s.u, s.shared_u = self._product(s.a, self.up, s.route.offsets), self._product(s.shared_a, self.shared_up, s.all)
+        offsets = _offsets(s.route, self.experts, x.device)
+        s.u, s.shared_u = self._product(s.a, self.up, offsets), self._product(s.shared_a, self.shared_up, s.all)
         s.s, s.shared_s = swiglu(s.u), swiglu(s.shared_u)
-        s.d, shared = self._product(s.s, self.down, s.route.offsets), self._product(s.shared_s, self.shared_down, s.all)
+        s.d, shared = self._product(s.s, self.down, offsets), self._product(s.shared_s, self.shared_down, s.all)
         s.out = self._combine(s.d, s.route, shared, s.route.weight, self.dtype)
         return s
 
@@ -350,7 +360,7 @@ class ExpertLayer:
         route, tokens = s.route, s.h.shape[0]
         dout, dh = self._rows("dout", dout, tokens), self._rows("dh", dh, tokens)
         dd, dweight = self._combine_grad(s.d, route, dout)
-        da, dup, ddown = expert(s.a, s.u, s.s, self.up, self.down, dd, route.offsets)
+        da, dup, ddown = expert(s.a, s.u, s.s, self.up, self.down, dd, _offsets(route, self.experts, dd.device))
         dy, dshared_up, dshared_down = expert(s.shared_a, s.shared_u, s.shared_s, self.shared_up, self.shared_down, dout, s.all)
         # what reaches y through its rows' copies, and through the shared expert
         dy, router = self._combine(da, route, dy, None, torch.float32 if through_router else self.dtype), {}

@@ -53,7 +53,7 @@ def layer_norm_grad(M, N, type, dY, lddy, H, ldh, gamma, mean, rstd, dH, lddh, d
 def gemm_i8_grouped(T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_scale, bs_stride, C, ldc, c_type, stream=0):
     a, c = mat(A, torch.int8, T, K, lda).double(), mat(C, KIND[c_type], T, N, ldc)
     b, s, r = at(B, torch.int8, (E, b_stride), (N, ldb), (K, 1)).double(), at(b_scale, torch.float32, (E, bs_stride), (N, 1)), at(a_scale, torch.float32, (T, 1))
-    off = offsets.tolist()
+    off = at(offsets, torch.int32, (E + 1, 1)).tolist()
     for e in range(E):
         lo, hi = off[e], off[e + 1]
         c[lo:hi] = ((a[lo:hi] @ b[e].t()).float() * r[lo:hi, None] * s[e]).to(c.dtype)
@@ -61,7 +61,7 @@ def gemm_i8_grouped(T, N, K, E, offsets, A, lda, a_scale, B, ldb, b_stride, b_sc
 
 
 def gemm_i8(M, N, K, A, lda, a_scale, B, ldb, b_scale, C, ldc, c_type, stream=0):
-    return gemm_i8_grouped(M, N, K, 1, torch.tensor([0, M]), A, lda, a_scale, B, ldb, 0, b_scale, 0, C, ldc, c_type)
+    return gemm_i8_grouped(M, N, K, 1, torch.tensor([0, M], dtype=torch.int32), A, lda, a_scale, B, ldb, 0, b_scale, 0, C, ldc, c_type)
 
 
 ENTRY_POINTS = (quantize_i8_rows, layer_norm, layer_norm_grad_workspace_bytes, layer_norm_grad, gemm_i8, gemm_i8_grouped)

@@ -83,7 +83,7 @@ def gemm_e4m3_block_grouped(T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb,
     a, c = spread(A, a_scale, T, K, lda, ld_as), mat(C, KIND[c_type & ~binding.EXACT], T, N, ldc)
     b = at(B, E4M3, (E, b_stride), (N, ldb), (K, 1)).float()
     s = at(b_scale, torch.float32, (E, bs_stride), (ceil128(N), ld_bs), (ceil128(K), 1))
-    off = offsets.tolist()
+    off = at(offsets, torch.int32, (E + 1, 1)).tolist()
     for e in range(E):
         w = b[e] * s[e].repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
         c[off[e]:off[e + 1]] = (a[off[e]:off[e + 1]] @ w.t()).to(c.dtype)
@@ -91,12 +91,12 @@ def gemm_e4m3_block_grouped(T, N, K, E, offsets, A, lda, a_scale, ld_as, B, ldb,
 
 
 def gemm_e4m3_block(M, N, K, A, lda, a_scale, ld_as, B, ldb, b_scale, ld_bs, C, ldc, c_type, stream=0):
-    return gemm_e4m3_block_grouped(M, N, K, 1, torch.tensor([0, M]), A, lda, a_scale, ld_as, B, ldb, 0, b_scale, ld_bs, 0, C, ldc, c_type)
+    return gemm_e4m3_block_grouped(M, N, K, 1, torch.tensor([0, M], dtype=torch.int32), A, lda, a_scale, ld_as, B, ldb, 0, b_scale, ld_bs, 0, C, ldc, c_type)
 
 
 def gemm_grouped(T, N, K, E, offsets, type, A, lda, B, ldb, b_stride, C, ldc, c_type, stream=0):
     a, b, c = mat(A, KIND[type], T, K, lda).float(), at(B, KIND[type], (E, b_stride), (K, ldb), (N, 1)).float(), mat(C, KIND[c_type], T, N, ldc)
-    off = offsets.tolist()
+    off = at(offsets, torch.int32, (E + 1, 1)).tolist()
     for e in range(E):
         c[off[e]:off[e + 1]] = (a[off[e]:off[e + 1]] @ b[e]).to(c.dtype)
     return binding.OK
@@ -104,7 +104,7 @@ def gemm_grouped(T, N, K, E, offsets, type, A, lda, B, ldb, b_stride, C, ldc, c_
 
 def gemm_grouped_grad_a(T, N, K, E, offsets, type, dC, lddc, B, ldb, b_stride, dA, ldda, a_type, stream=0):
     d, b, a = mat(dC, KIND[type], T, N, lddc).float(), at(B, KIND[type], (E, b_stride), (K, ldb), (N, 1)).float(), mat(dA, KIND[a_type], T, K, ldda)
-    off = offsets.tolist()
+    off = at(offsets, torch.int32, (E + 1, 1)).tolist()
     for e in range(E):
         a[off[e]:off[e + 1]] = (d[off[e]:off[e + 1]] @ b[e].t()).to(a.dtype)
     return binding.OK
@@ -112,7 +112,7 @@ def gemm_grouped_grad_a(T, N, K, E, offsets, type, dC, lddc, B, ldb, b_stride, d
 
 def gemm_grouped_grad_b(T, N, K, E, offsets, type, A, lda, dC, lddc, dB, lddb, db_stride, b_type, stream=0):
     a, d, b = mat(A, KIND[type], T, K, lda).float(), mat(dC, KIND[type], T, N, lddc).float(), at(dB, KIND[b_type], (E, db_stride), (K, lddb), (N, 1))
-    off = offsets.tolist()
+    off = at(offsets, torch.int32, (E + 1, 1)).tolist()
     for e in range(E):
         b[e] = (a[off[e]:off[e + 1]].t() @ d[off[e]:off[e + 1]]).to(b.dtype)
     return binding.OK

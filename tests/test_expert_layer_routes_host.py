@@ -206,3 +206,31 @@ def test_parts_of_a_route_go_to_the_rows_device():
     place, weight = expert_layer._places(route, T, TOP, torch.device("meta")), expert_layer._weight(torch.ones(T, 1), T, TOP, torch.device("meta"))
     assert place.device.type == weight.device.type == expert_layer._places32(place).device.type == "meta"
     assert place.shape == weight.shape == (T, TOP) and weight.is_contiguous()
+
+
+@pytest.mark.parametrize("make", [lambda o: o.long(), lambda o: torch.stack([o, o], 1)[:, 0]], ids=["64 bits", "apart"])
+def test_offsets_of_a_route_in_other_forms(layer, make):
+    given = inputs()
+    want = everything(layer, given)
+
+    def change(route):
+        route.offsets = make(route.offsets)
+    equal(everything(replaced(layer, change), given), want)
+
+
+@pytest.mark.parametrize("make", [lambda o: o[1:], lambda o: torch.cat([o, o[-1:]]), lambda o: o[None], lambda o: o.float(), lambda o: o.short()], ids=["fewer", "more", "two", "f32", "16 bits"])
+def test_offsets_that_are_none_are_refused(layer, make):
+    x, r, dout, dh = inputs()
+    s = layer.train_forward(x, r)
+
+    def change(route):
+        route.offsets = make(route.offsets)
+    replaced(layer, change)
+    change(s.route)
+    for call in (lambda: layer.serve(x, r), lambda: layer.train_forward(x, r), lambda: layer.backward(s, dout, dh)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_offsets_go_to_the_rows_device():
+    assert expert_layer._offsets(SimpleNamespace(offsets=torch.arange(E + 1)), E, torch.device("meta")).device.type == "meta"

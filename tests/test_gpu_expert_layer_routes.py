@@ -37,7 +37,7 @@ def on_the_host(*names):
 
 
 @FORMS
-@pytest.mark.parametrize("names", [("place",), ("source",), ("weight",), ("place", "source", "weight")], ids=" ".join)
+@pytest.mark.parametrize("names", [("place",), ("source",), ("weight",), ("offsets",), ("place", "source", "weight", "offsets")], ids=" ".join)
 def test_parts_of_a_route_on_the_host(made, norm, form, names):
     layer, given = made(norm, form)
     want = everything(layer, given)
