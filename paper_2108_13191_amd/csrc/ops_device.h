@@ -13,6 +13,14 @@ template <> struct Elem<ELEM_F32> { typedef float type; static constexpr int siz
 template <> struct Elem<ELEM_E4M3> { typedef uint8_t type; static constexpr int size = 1; };
 template <> struct Elem<ELEM_I8> { typedef int8_t type; static constexpr int size = 1; };
 
+// Between what lanes of a wavefront write to LDS and what others of it read there, and before it is written again.  The accesses of a wavefront are in order, so that nothing is waited
+// for; it keeps the compiler, which sees one lane, from another order.
+__device__ __forceinline__ void wave_exchange()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // 8 elements of 16 bits at element alignment (one 16-byte access)
 template <typename T> struct Vec8 { typedef T type __attribute__((ext_vector_type(8), aligned(2))); };
 

@@ -318,11 +318,11 @@ __global__ __launch_bounds__(256) void part_count_kernel(const Parts s)
     const int64_t part = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     int* const own = hist + (threadIdx.x >> 6) * bins;
     for (int b = lane; b < bins; b += 64) own[b] = 0;
-    __builtin_amdgcn_wave_barrier();                       // a wavefront's LDS accesses are in order
+    wave_exchange();
     if (part >= s.parts) return;
     const int64_t rows = (int64_t)s.tokens * s.a.top_k, first = part * rows, end = min(s.a.T * s.a.top_k, first + rows);
     for (int64_t i = first + lane; i < end; i += 64) atomicAdd(&own[key_of(s.a, i)], 1);
-    __builtin_amdgcn_wave_barrier();
+    wave_exchange();
     for (int b = lane; b < bins; b += 64) s.counts[(int64_t)b * s.parts + part] = own[b];
 }
 

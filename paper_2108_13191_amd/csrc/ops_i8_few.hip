@@ -78,11 +78,13 @@ __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
             for (int i = 0; i < COPIES; i++) v[i] = *(const uintx4_any*)((i < 2 * FM ? ap : bp) + off[i]);
         };
         if (wave < k_full) fetch(wave);
-        for (int k = wave; k < k_full; k += WAVES) {                          // (a wavefront's LDS accesses are in order)
+        for (int k = wave; k < k_full; k += WAVES) {
 #pragma unroll
             for (int i = 0; i < COPIES; i++) *(__attribute__((address_space(3))) uintx4*)(uintptr_t)(ring + 1024 * i + 16 * lane) = v[i];
+            wave_exchange();
             if (k + WAVES < k_full) fetch(k + WAVES);
             read(ring);
+            wave_exchange();
             multiply();
         }
     } else {

@@ -124,6 +124,7 @@ __global__ __launch_bounds__(256) void ops_i8_long_kernel(const OpsGemm g)
                 for (int e = 0; e < 4; e++) v[e] = scaled_sum(acc[2 * m2 + r][n][e], row_scale[2 * m2 + r]);
                 *(__attribute__((address_space(3))) floatx4*)(uintptr_t)(buf + (16 * r + l16) * PITCH + (16 * n + 4 * q) * 4) = v;
             }
+        wave_exchange();
 #pragma unroll
         for (int p = 0; p < 16; p++) {
             floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (2 * p + (lane >> 5)) * PITCH + 16 * (lane & 31));
@@ -142,6 +143,7 @@ __global__ __launch_bounds__(256) void ops_i8_long_kernel(const OpsGemm g)
                 for (int e = 0; e < 4; e++) if (col + e < g.N) dst[e] = (CT)v[e];
             }
         }
+        wave_exchange();
     }
 }
 

@@ -590,6 +590,7 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && F
                 }
                 *(__attribute__((address_space(3))) floatx4*)(uintptr_t)(buf + (16 * r + l16) * PITCH + (16 * n + 4 * q) * 4) = acc[2 * m2 + r][n];
             }
+        wave_exchange();
 #pragma unroll
         for (int ps = 0; ps < 32 / RPP; ps++) {
             floatx4 v = *(__attribute__((address_space(3))) const floatx4*)(uintptr_t)(buf + (RPP * ps + orow) * PITCH + ocol * 4);
@@ -611,6 +612,7 @@ __global__ __launch_bounds__(512, BM == 128 && BN == 128 && FORM != WIDENED && F
                 }
             }
         }
+        wave_exchange();
     }
 }
 
