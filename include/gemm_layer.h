@@ -29,7 +29,7 @@ extern "C" {
  * quantize_i8_rows has them, from the f32 value), mean and rstd (M f32 each, as layer_norm_grad takes them).  H may be X or R
  * themselves.  gamma, beta: N elements of `type`.  Q without scale or scale without Q is GEMM_F16_ERR_NULL; eps that is
  * negative or no number is GEMM_F16_ERR_CONFIG.  N = 0 writes nothing.  A row that holds a NaN or an infinity, or whose sum passes f32's range, is
- * NaN (Q: the scale NaN, elements 0); where only its sum of squares does, rstd is 0 and y is beta.  Pointers of 16-bit matrices: 2-byte aligned, any pitch.
+ * NaN (Q: the scale NaN, elements 0; mean and rstd too); where only its sum of squares does, or sums of parts of it or differences from its mean, rstd is 0 and y is beta.  Pointers of 16-bit matrices: 2-byte aligned, any pitch.
  */
 int layer_norm(int64_t M, int64_t N, int64_t type,
                const void* X, int64_t ldx, const void* R, int64_t ldr,
@@ -40,7 +40,7 @@ int layer_norm(int64_t M, int64_t N, int64_t type,
 
 /*
  * Gradients of layer_norm's Y.  From dY, the stored H, gamma, mean and rstd:
- *     xhat = (h - mean) * rstd,  g = dy * gamma
+ *     xhat = (h - mean) * rstd,  g = dy * gamma                     (NaN where a difference passes f32's range)
  *     dX = rstd * (g - mean(g) - xhat * mean(g * xhat)) + dH        (of x and of r alike)
  *     dgamma[j] = sum_i dy[i][j] * xhat[i][j],  dbeta[j] = sum_i dy[i][j]        (N f32 each)
  * dH: the gradient that reaches h by the residual's own way, or NULL.  dX may be dY or dH themselves.  dgamma, dbeta: NULL where one

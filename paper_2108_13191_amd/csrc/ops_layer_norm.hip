@@ -2,6 +2,7 @@
 //
 // Bound by memory: a row is read once, 8 elements of 16 bits a lane and access, and stays in registers for its mean, its squares about the mean and its
 // largest magnitude.
+#include <type_traits>
 #include "ops_rows.h"
 #include "../../include/gemm_layer.h"
 
@@ -49,6 +50,21 @@ __device__ __forceinline__ Moments row_moments(float own_mean, float squares, in
     const float at = pair[0], n = (float)n_of(w);
     const float mean = sum_waves<W>(n * at) / (float)N, d = at - mean;
     return {mean, sum_waves<W>(pair[1] + (n > 0.0f ? n * d * d : 0.0f))};
+}
+
+// The moments of a bf16 row whose squares, as they were summed, are not finite (f16 has no values whose sums could leave f32's range).  Its elements may be infinite or NaN, or sums of
+// parts, squares or differences from the mean have passed f32's range; which of them do depends on how the row is dealt to threads, what the row gives must not.  `scaled`: this thread's sum
+// of elements times 2^-31, which never passes it, of 2^31 elements.  Where the whole sum does not either, the squares do (so does any part's sum if the row's does not, where the elements
+// are not all alike), and rstd is 0; else the row is NaN.
+constexpr float DOWN = 0x1p-31f;
+template <int L>
+__device__ __forceinline__ Moments moments_beyond(float scaled, int N, float* lds)
+{
+    if constexpr (L > 64) scaled = sum_row<L / 64>(scaled, lds);
+    else scaled = sum_lanes<L>(scaled);
+    const float sum = scaled / DOWN;
+    if (!(__builtin_fabsf(sum) < __builtin_inff())) return {__builtin_nanf(""), __builtin_nanf("")};
+    return {sum / (float)N, __builtin_inff()};
 }
 
 // the largest of a row's magnitudes over its L threads; lds: a word for each wavefront of the workgroup, used for nothing else
@@ -152,7 +168,21 @@ __global__ __launch_bounds__(L * R) void layer_norm_kernel(const LayerNormArgs a
 #pragma unroll
         for (int i = 0; i < 8; i++) { const float d = (WHOLE ? left > 0 : i < left) ? v[p][i] - centre : 0.0f; squares += d * d; }
     }
-    const Moments m = row_moments<L>(centre, sum_lanes<L>(squares), a.N, lds, n_of);
+    Moments m = row_moments<L>(centre, sum_lanes<L>(squares), a.N, lds, n_of);
+    if constexpr (std::is_same_v<T, bf16_t>) {
+        if (__builtin_expect(!(m.squares < __builtin_inff()), false)) {      // (the same for all threads of a row)
+            float scaled = 0.0f;
+#pragma unroll
+            for (int p = 0; p < P; p++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) scaled += v[p][i] * DOWN;
+            m = moments_beyond<L>(scaled, a.N, lds);
+#pragma unroll
+            for (int p = 0; p < P; p++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[p][i] = m.mean;                // differences, which rstd makes 0, may pass the range
+        }
+    }
     const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
     if (live && lane == 0) {
         if (a.mean) a.mean[row] = m.mean;
@@ -225,7 +255,20 @@ __global__ __launch_bounds__(LONG) void layer_norm_long_kernel(const LayerNormAr
 #pragma unroll
         for (int i = 0; i < 8; i++) { const float d = c + i < a.N ? o[i] - centre : 0.0f; squares += d * d; }
     }
-    const Moments m = row_moments<LONG>(centre, sum64(squares), a.N, lds, n_of);
+    Moments m = row_moments<LONG>(centre, sum64(squares), a.N, lds, n_of);
+    bool beyond = false;
+    if constexpr (std::is_same_v<T, bf16_t>) {
+        beyond = !(m.squares < __builtin_inff());
+        if (beyond) {
+            float scaled = 0.0f;
+            for (int64_t c = first; c < a.N; c += step) {
+                again(c);
+#pragma unroll
+                for (int i = 0; i < 8; i++) scaled += o[i] * DOWN;
+            }
+            m = moments_beyond<LONG>(scaled, a.N, lds);
+        }
+    }
     const float rstd = 1.0f / sqrtf(m.squares / (float)a.N + a.eps);
     if (lane == 0) {
         if (a.mean) a.mean[row] = m.mean;
@@ -238,7 +281,7 @@ __global__ __launch_bounds__(LONG) void layer_norm_long_kernel(const LayerNormAr
         again(c);
         const Raw8<T> gm = load8_raw((const T*)a.gamma + c, left), bt = load8_raw((const T*)a.beta + c, a.beta ? left : 0);
 #pragma unroll
-        for (int i = 0; i < 8; i++) { const float y = (o[i] - m.mean) * rstd * (float)gm[i] + (float)bt[i]; o[i] = i < left ? y : 0.0f; }
+        for (int i = 0; i < 8; i++) { const float y = ((beyond ? m.mean : o[i]) - m.mean) * rstd * (float)gm[i] + (float)bt[i]; o[i] = i < left ? y : 0.0f; }
     };
     for (int64_t c = first; c < a.N; c += step) {
         output(c);
