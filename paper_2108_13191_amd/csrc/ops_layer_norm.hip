@@ -493,14 +493,16 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
     }
     const int lane = threadIdx.x & 7, sub = threadIdx.x >> 3;
     const int64_t c = ((int64_t)blockIdx.x - row_groups) * 64 + 8 * lane;
-    float dg[8] = {}, db[8] = {};
+    // Many rows (the widest form has up to 2^21, the others 768): sums are put aside every 2048, so that 32 and M / 2048 additions follow one another, not M / 64
+    constexpr bool MANY = 8 * L * P > 8192;
+    float dg[8] = {}, db[8] = {}, dg_all[8] = {}, db_all[8] = {};
     auto add = [&](Raw8<T> dy, Raw8<T> h, float mean, float rstd, bool live) {
         dy = settled<T, WHOLE>(dy, live ? c : (int64_t)a.N + 8, a.N);
         h = settled<T, WHOLE>(h, c, a.N);
 #pragma unroll
         for (int i = 0; i < 8; i++) { dg[i] += (float)dy[i] * (((float)h[i] - mean) * rstd); db[i] += (float)dy[i]; }
     };
-    constexpr int AT_ONCE = 4;
+    constexpr int AT_ONCE = 4, ASIDE = 2048;
     for (int64_t row0 = sub; row0 - sub < a.M; row0 += 64 * AT_ONCE) {
         Raw8<T> dy[AT_ONCE], h[AT_ONCE];
         float mean[AT_ONCE], rstd[AT_ONCE];
@@ -514,6 +516,14 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
         }
 #pragma unroll
         for (int u = 0; u < AT_ONCE; u++) add(dy[u], h[u], mean[u], rstd[u], row0 + 64 * u < a.M);
+        if (MANY && ((row0 - sub) & (ASIDE - 1)) == ASIDE - 64 * AT_ONCE) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) { dg_all[i] += dg[i]; db_all[i] += db[i]; dg[i] = db[i] = 0.0f; }
+        }
+    }
+    if constexpr (MANY) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) { dg[i] += dg_all[i]; db[i] += db_all[i]; }
     }
 #pragma unroll
     for (int i = 0; i < 8; i++) { lds[0][8 * lane + i][sub] = dg[i]; lds[1][8 * lane + i][sub] = db[i]; }
