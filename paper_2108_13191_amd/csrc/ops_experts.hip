@@ -754,8 +754,10 @@ int ops_launch_dispatch(const DispatchArgs& a, void* workspace, hipStream_t stre
         if (!fits_a_launch((waves + 3) / 4, 256)) return GEMM_F16_ERR_SIZE;
         hipLaunchKernelGGL(part_count_kernel, dim3((s.parts + 3) / 4), dim3(256), 4 * bins * sizeof(int), stream, s);
         launch_scan(bins, s.counts, s.totals, s.parts, stream);
-        // rows that are more than half of the 256 MB cache go past it: 8192 tokens to 2 of 16, bf16 rows of 4096, 37 us against 47, and 99 against 97 with a copy of the rows after it; below
-        // that what reads them next is faster with them in the cache: 4096 tokens 54 against 49 with the copy, 5000 to 8 of 64, rows of 1000, 64 against 52
+        // From half of the 256 MB cache on rows go past it.  That pays for the call by itself, and neither pays nor costs for it and what reads the rows next: us past | through the cache, 8192 tokens
+        // to 2 of 16, bf16 rows of 4096 (134 MB) 37 | 46, with a copy of the rows behind it 97 | 97, with a product of 768 columns 137 | 140, of 1024 209 | 201, of 4096 499 | 496; 16384 tokens (268 MB)
+        // 80 | 84, 188 | 183, 261 | 269, 288 | 290, 877 | 874; 16384 to 8 of 64, rows of 1024 63 | 70, 173 | 184, 267 | 269, 328 | 331, 1053 | 1048.  Below, a reader finds them in the cache:
+        // 4096 tokens (67 MB) 22 | 26, with a copy 50 | 46
         if (narrow) {
             int R = 1;
             while (16 * R < bytes) R *= 2;
