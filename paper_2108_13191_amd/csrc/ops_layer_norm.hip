@@ -493,8 +493,8 @@ __global__ __launch_bounds__(512) void layer_norm_grad_few_kernel(const LayerNor
     }
     const int lane = threadIdx.x & 7, sub = threadIdx.x >> 3;
     const int64_t c = ((int64_t)blockIdx.x - row_groups) * 64 + 8 * lane;
-    // Many rows (the widest form has up to 2^21, the others 768): sums are put aside every 2048, so that 32 and M / 2048 additions follow one another, not M / 64
-    constexpr bool MANY = 8 * L * P > 8192;
+    // Many rows (the widest form has up to 2^21 that are no whole chunks, the others 2047 at most): sums are put aside every 2048, so that 32 and M / 2048 additions follow one another, not M / 64
+    constexpr bool MANY = !WHOLE && 8 * L * P > 8192;
     float dg[8] = {}, db[8] = {}, dg_all[8] = {}, db_all[8] = {};
     auto add = [&](Raw8<T> dy, Raw8<T> h, float mean, float rstd, bool live) {
         dy = settled<T, WHOLE>(dy, live ? c : (int64_t)a.N + 8, a.N);
@@ -610,13 +610,15 @@ constexpr int64_t LAUNCH_COLUMNS = 1 << 27;              // 16 threads each: 2^3
 // threads that share a row in the gradient, and rows that a workgroup takes at a time
 inline int grad_rows(int64_t N) { return N <= 64 ? 64 : N <= 128 ? 32 : N <= 512 ? 16 : N <= 1024 ? 8 : N <= 2048 ? 4 : N <= 4096 ? 2 : 1; }
 // Whether one launch forms everything, us | two launches.  Up to 512 rows, 768 of more than 512 columns: (512,768) 6.0 | 7.7, (512,4096) 8.5 | 12.8, (768,8192) 15.6 | 18.2, (512,64) 5.7 | 5.9; more:
-// (700,64) 7.0 | 6.1, (1024,768) 9.2 | 8.4, (2048,4096) 28 | 20.  Rows of more than 8192, whose columns' sums leave no registers for the next row: (2048,16384) 70 | 93, (6000,10000) 141 | 193.
+// (700,64) 7.0 | 6.1, (1024,768) 9.2 | 8.4, (2048,4096) 28 | 20.  Rows of more than 8192, whose columns' sums leave no registers for the next row, up to 2047 of them: (800,16384) 28 | 36,
+// (1024,9000) 23 | 26; more: (2048,9000) 44 | 43, (2048,16384) 71 | 67, (6000,10000) 150 | 108, (20000,9000) 459 | 295; any number where they are no whole chunks of 8, whose shifts take more registers:
+// (1500,12001) 57 | 80, (2048,16383) 93 | 117, (20000,9001) 564 | 716.
 // Not where dX takes dY's place, which is read twice.
 inline bool grad_few(const LayerNormGradArgs& a)
 {
     if (a.N > 16384 || a.M > LAUNCH_ROWS) return false;
     if (!a.dgamma && !a.dbeta) return true;
-    return a.dX != a.dY && (a.M <= 512 || (a.N > 512 && a.M <= 768) || a.N > 8192);
+    return a.dX != a.dY && (a.M <= 512 || (a.N > 512 && a.M <= 768) || (a.N > 8192 && (a.M < 2048 || a.N % 8 != 0)));
 }
 
 template <typename T, int L, int P, int R>

@@ -10,9 +10,9 @@ CUS = 256
 NORM = [(65, 24), (65, 61), (33, 128), (33, 100), (17, 256), (17, 130), (9, 512), (9, 300), (9, 1024), (9, 777), (9, 2048), (9, 2047), (600, 4000), (600, 3001), (600, 8192), (600, 8191), (16, 8192), (16, 4001),
         (9, 16384), (9, 9001), (2, 16400), (2, 20001)]
 # ... of gradients row by row: three rows and more one after another in each of a workgroup's places
-GRAD = [(33000, 64), (33000, 61), (16500, 104), (16500, 100), (8300, 256), (8300, 203), (8300, 512), (8300, 300), (4200, 1024), (4200, 777), (2100, 1504), (2100, 1501), (1100, 4000), (1100, 4001), (800, 8192), (800, 8191)]
+GRAD = [(33000, 64), (33000, 61), (16500, 104), (16500, 100), (8300, 256), (8300, 203), (8300, 512), (8300, 300), (4200, 1024), (4200, 777), (2100, 1504), (2100, 1501), (1100, 4000), (1100, 4001), (800, 8192), (800, 8191), (2050, 8200)]
 GRAD_ONLY_IN_PLACE = [(600, 16384), (600, 9001)]
-GRAD_FEW = [(130, 64), (130, 61), (300, 256), (300, 203), (100, 512), (100, 300), (513, 1024), (513, 777), (700, 2048), (700, 1501), (500, 4000), (500, 4001), (700, 8192), (700, 8191), (1500, 9000), (1500, 8201), (300, 16384)]
+GRAD_FEW = [(130, 64), (130, 61), (300, 256), (300, 203), (100, 512), (100, 300), (513, 1024), (513, 777), (700, 2048), (700, 1501), (500, 4000), (500, 4001), (700, 8192), (700, 8191), (1500, 9000), (1500, 8201), (2050, 8201), (300, 16384)]
 # T, choices, N
 COMBINE = [(9, 3, 64), (9, 3, 61), (9, 3, 128), (9, 3, 100), (9, 5, 256), (9, 5, 203), (9, 3, 1024), (9, 3, 777)]
 COMBINE_GRAD = [(40, 3, 64), (40, 3, 61), (40, 3, 128), (40, 3, 100), (40, 5, 256), (40, 5, 203), (40, 3, 512), (40, 3, 300), (40, 3, 1024), (40, 3, 777), (600, 3, 2048), (600, 3, 2047), (700, 3, 4000), (700, 3, 3999),
