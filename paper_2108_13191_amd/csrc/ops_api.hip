@@ -56,7 +56,7 @@ bool fits(const OpsGemm& g, const Form& f)
 
 // The fastest for 8-bit integers.  A form's time is that of a launch and of a compute unit's tiles, each of which costs something by itself and something for each k; what
 // follows is fitted, in us, to 776 products (1 to 2048 rows, 256 to 16384 columns and k) and 307 grouped ones (16 to 16384 rows, 4 to 128 experts), each measured on every form.
-// Of these products the form that comes out is within 10 % of the fastest but for 6 and 25, on average 0.8 % and 2 % slower.  us of the forms 16x16 | 32x32 | 64x64 | 128x128 | 256x256:
+// Of these products the form that comes out is within 10 % of the fastest but for 6 and 24, on average 0.6 % and 1.9 % slower; of 514 larger ones (400 to 16384 rows), measured afterwards, but for 15, on average 0.9 %.  us of the forms 16x16 | 32x32 | 64x64 | 128x128 | 256x256:
 // 16 rows of (1000,16384) 7.9 | 12.7 | 22.9 | 59 | 128, 64 of (8192,8192) 37 | 14.4 | 16.1 | 33, 256 of (4096,16384) - | 43 | 26 | 60 | 131, 400 of (16384,1000) - | - | 40 | 15.5 | 22.5
 Form preferred_i8(const OpsGemm& g, bool allow_few_rows)
 {

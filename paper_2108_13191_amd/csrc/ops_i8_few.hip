@@ -5,7 +5,7 @@
 // load of 1 KB takes the 64 cycles of 64 requests: 16 bytes a cycle whatever is asked for ahead (16 to 64 k steps).  Copied to LDS eight lanes read one row's 128 bytes, and
 // fragments come from there: twice to three times that.  us, here | by registers: (16,8192,8192) 12.2 | 14.4, (16,1000,16384) 7.9 | 16.8, (64,8192,8192) 14.0 | 25.5 (from memory 13.5),
 // (256,4096,16384) 26 | 88, (700,1000,16384) 25 | 88, (300,300,300) 3.2 | 3.2.  128 x 64 in one stage, as a wavefront's products (64 MFMAs) are as long as the copies of its next
-// step: (400,4096,16384) 42 us, 64 x 64 in two rounds 48, 128 x 128 of the tiled kernel 60.  Tried: three and four stages, twice or half the wavefronts, 32 x 128, 64 x 128 and 128 x 128 tiles: no faster.
+// step: (400,4096,16384) 39 to 42 us by the card, 64 x 64 in two rounds 48, 128 x 128 of the tiled kernel 60.  Tried: three and four stages, twice or half the wavefronts, 32 x 128, 64 x 128 and 128 x 128 tiles: no faster.
 #include "ops_tile.h"
 
 namespace {
@@ -16,8 +16,8 @@ typedef uintx4 uintx4_any __attribute__((aligned(1)));
 
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
-// S = 0: operands of any alignment, a k step ahead in registers and one stage in LDS.  us, here | the kernel for any alignment of ops_generic.hip: 16 rows of (8192,8190) 17.7 | 541,
-// (300,700,1100) 6.6 | 70, (2000,2000,2001) 39 | 365, (4000,4000,4001) 225 | 3165
+// S = 0: operands of any alignment, a k step ahead in registers and one stage in LDS.  us, here | the kernel for any alignment of ops_generic.hip: 16 rows of (8192,8190) 15.0 | 541,
+// (300,700,1100) 5.6 | 70, (2000,2000,2001) 35 | 365, (4000,4000,4001) 208 | 3165
 template <int FM, int NB, int WAVES, int S, typename CT>
 __global__ __launch_bounds__(64 * WAVES) void ops_i8_few_kernel(const OpsGemm g)
 {

@@ -3,8 +3,8 @@
 //
 // Why this shape: 8-bit MFMAs are twice as fast as 16-bit ones on the same bytes, so that with eight wavefronts of 128 x 64 (ops_tile.h) the reads of fragments from
 // LDS take as long as the MFMAs; here A is read by two wavefronts instead of four, which leaves LDS a quarter of its time.  Measured: a k step (128 k) of a tile 1.35 us against 1.53;
-// 8192^3 to bf16 394 us, 2.8 POPS, with f32 results 391 (425 there).  MFMAs alone run at 3.9 POPS on such operands, at 4.8 on zeros: the chip's power.  What a tile takes around its
-// loop, 12 to 15 us, is stores of all compute units at once and latency that one wavefront a SIMD does not hide.  Tried: results straight from the registers, 64 bytes of a row a
+// 8192^3 to bf16 366 to 396 us by the card, 2.8 to 3.0 POPS; on one of them 394, with f32 results 391 (436 and 425 there).  MFMAs alone run at 3.9 POPS on such operands, at 4.8 on zeros: the chip's power.  What a tile takes around its
+// loop, 10 to 11 us, is stores of all compute units at once and latency that one wavefront a SIMD does not hide.  Tried: results straight from the registers, 64 bytes of a row a
 // store (8192^3 f32 460, (8192,8192,1024) 114 against 93 through LDS).
 #include "ops_tile.h"
 #include "ops_i8_loop.inc"
